@@ -381,6 +381,108 @@ FUSION_API int fusion_test_topk_compact_ws(const fusion_ragged* in, const float*
                                            const fusion_packed_out* out, void* ws,
                                            size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Long sequences and token caches, in the storage types of the two precision
+ * paths (precision 1: bfloat16, 0: fp32; sums and softmax statistics fp32).
+ * Head widths dh: multiples of 8 up to 128; heads a multiple of kv_heads,
+ * query head h reads key head h / (heads / kv_heads).  Strides count elements
+ * and are multiples of 16 bytes, the dh values of a head are contiguous, and
+ * every tensor's base is 16-byte aligned.  The calls neither allocate nor
+ * synchronise, and they can be captured into a graph.
+ * ------------------------------------------------------------------------ */
+
+/* Attention over packed ragged rows under a sliding window, for samples of
+ * any length: the rows of sample i are rows cu[i] .. cu[i+1]-1 (cu: HOST
+ * int32 [batch + 1], cu[0] = 0, not decreasing, read before the call returns;
+ * a captured call replays with those it was captured with).  Row i of a
+ * sample sees its row j when
+ *   causal:      j <= i and (i - j < window or j < sinks)
+ *   two-sided:   |i - j| < window or j < sinks
+ * (window 0: no limit; sinks: first rows that stay visible, such as CLS).
+ * size: device fp32 [M] or NULL; scores += ln(size of the key row), as in
+ * fusion_test_attention; a size that is not above 0 hides the row from all.
+ * A row that sees nothing gets zeros; a value of a row that a query does not
+ * see has no influence on its output, whatever it is.
+ * q: device [M][heads][dh], k, v: device [M][kv_heads][dh]; strides: HOST
+ * int64 [6], row and head strides of q, k and v; out: device
+ * [M][heads][dh], contiguous, apart from the inputs.  M = cu[batch].
+ * Errors: FUSION_E_INVALID_ARG, FUSION_E_HIP. */
+FUSION_API int fusion_window_attention(int precision, const void* q, const void* k, const void* v,
+                                       const int64_t* strides, const float* size,
+                                       const int32_t* cu, int batch, int heads, int kv_heads,
+                                       int dh, int window, int sinks, int causal, void* out,
+                                       void* stream);
+
+/* A paged cache of key and value rows with the attention weight that each
+ * cached token has drawn.  Slot x of sequence i is place x % page_size of page
+ * table[i][x / page_size] (entries outside 0 .. pages-1 hold no page: their
+ * slots are hidden and nothing is stored there); capacity = max_pages *
+ * page_size slots a sequence.  All pointers are device memory of the caller:
+ *   k, v    [pages][page_size][kv_heads][dh], strides of the first three
+ *   table   int32 [batch][max_pages], read only
+ *   len     int32 [batch]            slots in use (read as 0 .. capacity)
+ *   seen    int32 [batch]            tokens appended so far: the next position
+ *   weight  fp32  [batch][capacity]  attention weight drawn so far
+ *   pos     int32 [batch][capacity]  position of the token in each slot
+ * A sequence starts with len = seen = 0; while len equals seen nothing has
+ * left and pos[x] = x, which the attention relies on.  Sequences may share
+ * pages for reading; the pages that a call writes belong to one slot range of
+ * one sequence. */
+typedef struct fusion_cache {
+  void* k;
+  void* v;
+  int64_t k_strides[3]; /* page, place in the page, head */
+  int64_t v_strides[3];
+  const int32_t* table;
+  int32_t* len;
+  int32_t* seen;
+  float* weight;
+  int32_t* pos;
+  int32_t precision, batch, pages, page_size, max_pages, kv_heads, dh;
+} fusion_cache;
+
+/* Append rows of keys and values: sequence i gets rows cu[i] .. cu[i+1]-1 of
+ * k and v (cu: HOST int32 [batch + 1] as above; NULL: one row each), in its
+ * slots from len on, with positions from seen on and weight 0; len and seen
+ * grow.  Rows past the capacity are dropped and not counted.
+ * k, v: device [rows][kv_heads][dh]; strides: HOST int64 [4], row and head
+ * strides of k and v.  Errors: FUSION_E_INVALID_ARG, FUSION_E_HIP. */
+FUSION_API int fusion_cache_append(const fusion_cache* c, const void* k, const void* v,
+                                   const int64_t* strides, const int32_t* cu, void* stream);
+
+/* Attention of one query token per sequence, the newest (position seen - 1,
+ * already appended), over the cached tokens whose position is above
+ * seen - 1 - window or below sinks (window 0: all).  The work of all
+ * sequences is split evenly over the chip and the parts are joined.  With
+ * accumulate = 1 every slot's weight grows by the mean over the heads of its
+ * attention probability (the token score of Eq. 8).  A sequence with nothing
+ * visible gets zeros.
+ * q: device [batch][heads][dh], strides: HOST int64 [2]; out: device
+ * [batch][heads][dh], contiguous.  ws: device buffer of ws_bytes >=
+ * fusion_paged_attention_workspace_bytes, 256-byte aligned, any contents, not
+ * used by anything else until the call has finished.  Errors:
+ * FUSION_E_INVALID_ARG, FUSION_E_CAPACITY (small workspace), FUSION_E_HIP. */
+FUSION_API size_t fusion_paged_attention_workspace_bytes(const fusion_cache* c, int heads,
+                                                         int accumulate);
+FUSION_API int fusion_paged_attention(const fusion_cache* c, const void* q, const int64_t* strides,
+                                      int heads, int window, int sinks, int accumulate, void* out,
+                                      void* ws, size_t ws_bytes, void* stream);
+
+/* Eviction by accumulated weight: a sequence with more than `budget` tokens
+ * keeps those whose position is below sinks or among its last `recent`
+ * (sinks + recent <= budget), and of the others the ones with the most weight
+ * (ties to the lower slot; NaN below everything), budget in all.  Kept tokens
+ * in slots below the budget stay where they are; those beyond move, lowest
+ * slot first, into the slots that became free, lowest first, with their
+ * weight and position.  len becomes the budget; what slots past it hold is
+ * left as it was.  src: device int32 [batch][budget], the slot that each slot's
+ * token was in before the call, -1 past len.  ws as above
+ * (fusion_cache_evict_workspace_bytes).  Errors: FUSION_E_INVALID_ARG,
+ * FUSION_E_CAPACITY, FUSION_E_HIP. */
+FUSION_API size_t fusion_cache_evict_workspace_bytes(const fusion_cache* c, int budget);
+FUSION_API int fusion_cache_evict(const fusion_cache* c, int budget, int sinks, int recent,
+                                  int32_t* src, void* ws, size_t ws_bytes, void* stream);
+
 /* Message of the last failed call on this thread ("" if none). */
 FUSION_API const char* fusion_last_error(void);
 

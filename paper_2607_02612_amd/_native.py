@@ -57,6 +57,15 @@ class FusionPackedOut(ctypes.Structure):
                 ("cu", c_void_p), ("live", c_void_p), ("counts", c_void_p)]
 
 
+class FusionCache(ctypes.Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("k_strides", c_int64 * 3),
+                ("v_strides", c_int64 * 3), ("table", c_void_p), ("len", c_void_p),
+                ("seen", c_void_p), ("weight", c_void_p), ("pos", c_void_p),
+                ("precision", c_int32), ("batch", c_int32), ("pages", c_int32),
+                ("page_size", c_int32), ("max_pages", c_int32), ("kv_heads", c_int32),
+                ("dh", c_int32)]
+
+
 class FusionError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"{STATUS.get(code, code)}: {msg}")
@@ -111,6 +120,17 @@ SIGNATURES = [
                                             c_float, c_void_p, c_void_p, c_int, c_void_p,
                                             c_void_p, c_void_p, POINTER(FusionPackedOut),
                                             c_void_p, c_size_t, c_void_p]),
+    ("fusion_window_attention", c_int, [c_int, c_void_p, c_void_p, c_void_p, c_void_p,
+                                        c_void_p, c_void_p, c_int, c_int, c_int, c_int,
+                                        c_int, c_int, c_int, c_void_p, c_void_p]),
+    ("fusion_cache_append", c_int, [POINTER(FusionCache), c_void_p, c_void_p, c_void_p,
+                                    c_void_p, c_void_p]),
+    ("fusion_paged_attention_workspace_bytes", c_size_t, [POINTER(FusionCache), c_int, c_int]),
+    ("fusion_paged_attention", c_int, [POINTER(FusionCache), c_void_p, c_void_p, c_int, c_int,
+                                       c_int, c_int, c_void_p, c_void_p, c_size_t, c_void_p]),
+    ("fusion_cache_evict_workspace_bytes", c_size_t, [POINTER(FusionCache), c_int]),
+    ("fusion_cache_evict", c_int, [POINTER(FusionCache), c_int, c_int, c_int, c_void_p,
+                                   c_void_p, c_size_t, c_void_p]),
     ("fusion_last_error", c_char_p, []),
 ]
 

@@ -295,6 +295,60 @@ int topk_impl(const fusion_ragged* in, const float* scores, int heads, int tmax,
   return compact<float>(in, sc, T_ub, ln_g, ln_b, ln_out, out, fill, s);
 }
 
+// Arguments shared by the calls on long sequences and token caches.
+int check_heads(int precision, int heads, int kv_heads, int dh) {
+  if (precision != 0 && precision != 1) return bad("precision must be 0 (fp32) or 1 (bf16)");
+  if (kv_heads < 1 || heads < 1 || heads > 4096 || heads % kv_heads)
+    return bad("heads must be a multiple of kv_heads, at most 4096");
+  if (dh < 8 || dh > 128 || dh % 8) return bad("head width must be a multiple of 8 in 8 .. 128");
+  return FUSION_OK;
+}
+
+int check_rows(const int32_t* cu, int batch) {
+  if (!cu) return bad("offsets are null");
+  if (batch < 1 || batch > 65536) return bad("batch must be in 1 .. 65536");
+  if (cu[0] != 0) return bad("offsets must start at 0");
+  for (int i = 0; i < batch; i++)
+    if (cu[i + 1] < cu[i]) return bad("offsets must not decrease");
+  if (cu[batch] > (1 << 30)) return bad("more than 2^30 rows");
+  return FUSION_OK;
+}
+
+int check_strides(int precision, const int64_t* strides, int n) {
+  for (int i = 0; i < n; i++)
+    if (strides[i] < 0 || strides[i] % (precision == 1 ? 8 : 4))
+      return bad("strides must be multiples of 16 bytes, not negative");
+  return FUSION_OK;
+}
+
+int check_cache(const fusion_cache* c, CacheArgs* a) {
+  if (!c) return bad("cache is null");
+  if (int rc = check_heads(c->precision, c->kv_heads, c->kv_heads, c->dh)) return rc;
+  if (c->batch < 1 || c->batch > 65536) return bad("batch must be in 1 .. 65536");
+  if (c->pages < 1 || c->page_size < 1 || c->max_pages < 1)
+    return bad("pages, page_size and max_pages must be positive");
+  if ((int64_t)c->max_pages * c->page_size > (1 << 30)) return bad("capacity above 2^30 slots");
+  if (!c->k || !c->v || !c->table || !c->len || !c->seen || !c->weight || !c->pos)
+    return bad("null cache buffer");
+  if (((uintptr_t)c->k | (uintptr_t)c->v) % 16) return bad("buffers must be 16-byte aligned");
+  if (int rc = check_strides(c->precision, c->k_strides, 3)) return rc;
+  if (int rc = check_strides(c->precision, c->v_strides, 3)) return rc;
+  *a = CacheArgs{c->k, c->v, c->k_strides[0], c->k_strides[1], c->k_strides[2],
+                 c->v_strides[0], c->v_strides[1], c->v_strides[2], c->table, c->len, c->seen,
+                 c->weight, c->pos, c->batch, c->pages, c->max_pages,
+                 c->max_pages * c->page_size, c->kv_heads, c->dh,
+                 fast_div((uint32_t)c->page_size)};
+  return FUSION_OK;
+}
+
+int check_space(const void* ws, size_t bytes, size_t need) {
+  if (!ws || (uintptr_t)ws % 256) return bad("workspace is null or not 256-byte aligned");
+  if (bytes < need)
+    return api_fail(FUSION_E_CAPACITY, ("the call needs " + std::to_string(need) +
+                                        " bytes of workspace").c_str());
+  return FUSION_OK;
+}
+
 // Device address of `scratch` on the current device, looked up on the
 // first call on each device (with that device current) and kept.
 constexpr int kMaxDevices = 64;
@@ -463,6 +517,105 @@ FUSION_API int fusion_test_topk_compact_ws(const fusion_ragged* in, const float*
   return topk_impl(in, scores, heads, tmax, prune_w, prune_b, keep_ratio, exit_logits, classes,
                    delta, logits, exit_block, precision, ln_g, ln_b, ln_out, out, M, T_ub, (char*)ws,
                    true, s);
+}
+
+FUSION_API int fusion_window_attention(int precision, const void* q, const void* k, const void* v,
+                                       const int64_t* strides, const float* size,
+                                       const int32_t* cu, int batch, int heads, int kv_heads,
+                                       int dh, int window, int sinks, int causal, void* out,
+                                       void* stream) {
+  if (int rc = check_heads(precision, heads, kv_heads, dh)) return rc;
+  if (int rc = check_rows(cu, batch)) return rc;
+  if (window < 0 || sinks < 0) return bad("window and sinks must not be negative");
+  if (causal != 0 && causal != 1) return bad("causal must be 0 or 1");
+  if (cu[batch] == 0) return FUSION_OK;  // no rows
+  if (!q || !k || !v || !strides || !out) return bad("null buffer");
+  if (int rc = check_strides(precision, strides, 6)) return rc;
+  if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)out) % 16)
+    return bad("buffers must be 16-byte aligned");
+  WindowArgs a{};
+  a.q = q; a.k = k; a.v = v; a.size = size; a.out = out;
+  a.q_row = strides[0]; a.q_head = strides[1]; a.k_row = strides[2]; a.k_head = strides[3];
+  a.v_row = strides[4]; a.v_head = strides[5];
+  a.H = heads; a.group = heads / kv_heads; a.dh = dh;
+  a.window = window == 0 ? kNoWindow : std::min(window, kNoWindow);
+  a.sinks = std::min(sinks, kNoWindow); a.causal = causal;
+  a.scale = (float)(1.0 / std::sqrt((double)dh));
+  hipStream_t s = (hipStream_t)stream;
+  hipError_t err = precision == 1 ? launch_window_attention<bf16_t>(a, cu, batch, s)
+                                  : launch_window_attention<float>(a, cu, batch, s);
+  return err == hipSuccess ? FUSION_OK : hip_fail("launch_window_attention", err);
+}
+
+FUSION_API int fusion_cache_append(const fusion_cache* c, const void* k, const void* v,
+                                   const int64_t* strides, const int32_t* cu, void* stream) {
+  CacheArgs ca;
+  if (int rc = check_cache(c, &ca)) return rc;
+  if (cu) {
+    if (int rc = check_rows(cu, c->batch)) return rc;
+    if (cu[c->batch] == 0) return FUSION_OK;  // no rows
+  }
+  if (!k || !v || !strides) return bad("null buffer");
+  if (int rc = check_strides(c->precision, strides, 4)) return rc;
+  if (((uintptr_t)k | (uintptr_t)v) % 16) return bad("buffers must be 16-byte aligned");
+  const AppendArgs a{k, v, strides[0], strides[1], strides[2], strides[3]};
+  hipStream_t s = (hipStream_t)stream;
+  hipError_t err = c->precision == 1 ? launch_cache_append<bf16_t>(ca, a, cu, s)
+                                     : launch_cache_append<float>(ca, a, cu, s);
+  return err == hipSuccess ? FUSION_OK : hip_fail("launch_cache_append", err);
+}
+
+FUSION_API size_t fusion_paged_attention_workspace_bytes(const fusion_cache* c, int heads,
+                                                         int accumulate) {
+  CacheArgs ca;
+  if (check_cache(c, &ca) || check_heads(c->precision, heads, c->kv_heads, c->dh)) return 0;
+  return paged_workspace_bytes(ca, heads, accumulate);
+}
+
+FUSION_API int fusion_paged_attention(const fusion_cache* c, const void* q, const int64_t* strides,
+                                      int heads, int window, int sinks, int accumulate, void* out,
+                                      void* ws, size_t ws_bytes, void* stream) {
+  CacheArgs ca;
+  if (int rc = check_cache(c, &ca)) return rc;
+  if (int rc = check_heads(c->precision, heads, c->kv_heads, c->dh)) return rc;
+  if (window < 0 || sinks < 0) return bad("window and sinks must not be negative");
+  if (accumulate != 0 && accumulate != 1) return bad("accumulate must be 0 or 1");
+  if (!q || !strides || !out) return bad("null buffer");
+  if (int rc = check_strides(c->precision, strides, 2)) return rc;
+  if (((uintptr_t)q | (uintptr_t)out) % 16) return bad("buffers must be 16-byte aligned");
+  if (int rc = check_space(ws, ws_bytes, paged_workspace_bytes(ca, heads, accumulate))) return rc;
+  PagedArgs a{};
+  a.q = q; a.q_row = strides[0]; a.q_head = strides[1]; a.out = out;
+  a.H = heads; a.group = heads / c->kv_heads;
+  a.window = window == 0 ? kNoWindow : std::min(window, kNoWindow);
+  a.sinks = std::min(sinks, kNoWindow); a.accumulate = accumulate;
+  a.scale = (float)(1.0 / std::sqrt((double)c->dh)); a.ws = ws;
+  hipStream_t s = (hipStream_t)stream;
+  hipError_t err = c->precision == 1 ? launch_paged_attention<bf16_t>(ca, a, s)
+                                     : launch_paged_attention<float>(ca, a, s);
+  return err == hipSuccess ? FUSION_OK : hip_fail("launch_paged_attention", err);
+}
+
+FUSION_API size_t fusion_cache_evict_workspace_bytes(const fusion_cache* c, int budget) {
+  CacheArgs ca;
+  if (check_cache(c, &ca) || budget < 1) return 0;
+  return evict_workspace_bytes(ca, budget);
+}
+
+FUSION_API int fusion_cache_evict(const fusion_cache* c, int budget, int sinks, int recent,
+                                  int32_t* src, void* ws, size_t ws_bytes, void* stream) {
+  CacheArgs ca;
+  if (int rc = check_cache(c, &ca)) return rc;
+  if (budget < 1 || budget > kNoWindow) return bad("budget must be in 1 .. 2^30");
+  if (sinks < 0 || recent < 0 || (int64_t)sinks + recent > budget)
+    return bad("sinks and recent must not be negative and fit the budget together");
+  if (!src) return bad("null buffer");
+  if (int rc = check_space(ws, ws_bytes, evict_workspace_bytes(ca, budget))) return rc;
+  const EvictArgs a{budget, sinks, recent, src, ws};
+  hipStream_t s = (hipStream_t)stream;
+  hipError_t err = c->precision == 1 ? launch_cache_evict<bf16_t>(ca, a, s)
+                                     : launch_cache_evict<float>(ca, a, s);
+  return err == hipSuccess ? FUSION_OK : hip_fail("launch_cache_evict", err);
 }
 
 }  // extern "C"

@@ -184,6 +184,76 @@ constexpr int STEP_HOST_INTS = 896;
 hipError_t launch_step_init(const StepInit& a, const int32_t* cu_host, const int32_t* r_host,
                             hipStream_t s);
 
+// Windowed attention over packed ragged rows (strides in elements).
+struct WindowArgs {
+  const void *q, *k, *v;  // T
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head;
+  const float* size;  // fp32 [M] or null
+  void* out;          // T [M][H][dh]
+  int H, group, dh;   // query heads, query heads per key head
+  int window, sinks, causal;  // no limit: window = kNoWindow
+  float scale;
+};
+constexpr int kNoWindow = 1 << 30;
+template <typename T>
+hipError_t launch_window_attention(const WindowArgs& a, const int32_t* cu_host, int batch,
+                                   hipStream_t s);
+
+// Quotient by a divisor fixed on the host: n / d for 0 <= n < 2^31 as
+// (mulhi(n, mul) + n) >> shift with mul = floor(2^32 (2^shift - d) / d) + 1,
+// shift = ceil(log2 d) (Granlund and Montgomery's division by invariants).
+struct FastDiv {
+  uint32_t d, mul, shift;
+};
+inline FastDiv fast_div(uint32_t d) {
+  uint32_t l = 0;
+  while ((1ull << l) < d) l++;
+  return {d, (uint32_t)((((1ull << l) - d) << 32) / d + 1), l};
+}
+__device__ __forceinline__ uint32_t quot(uint32_t n, FastDiv f) {
+  return (__umulhi(n, f.mul) + n) >> f.shift;
+}
+
+// A paged token cache (strides in elements: page, place in the page, head).
+struct CacheArgs {
+  void *k, *v;  // T
+  int64_t k_page, k_row, k_head, v_page, v_row, v_head;
+  const int* table;  // [B][max_pages]
+  int *len, *seen;   // [B]
+  float* weight;     // [B][cap]
+  int* pos;          // [B][cap]
+  int B, pages, max_pages, cap, Hkv, dh;
+  FastDiv page;
+};
+struct AppendArgs {
+  const void *k, *v;  // T [rows][Hkv][dh]
+  int64_t k_row, k_head, v_row, v_head;
+};
+template <typename T>
+hipError_t launch_cache_append(const CacheArgs& c, const AppendArgs& a, const int32_t* cu_host,
+                               hipStream_t s);
+
+struct PagedArgs {
+  const void* q;  // T [B][H][dh]
+  int64_t q_row, q_head;
+  void* out;  // T [B][H][dh]
+  int H, group, window, sinks, accumulate;
+  float scale;
+  void* ws;
+};
+size_t paged_workspace_bytes(const CacheArgs& c, int H, int accumulate);
+template <typename T>
+hipError_t launch_paged_attention(const CacheArgs& c, const PagedArgs& a, hipStream_t s);
+
+struct EvictArgs {
+  int budget, sinks, recent;
+  int* src;  // [B][budget]
+  void* ws;
+};
+size_t evict_workspace_bytes(const CacheArgs& c, int budget);
+template <typename T>
+hipError_t launch_cache_evict(const CacheArgs& c, const EvictArgs& a, hipStream_t s);
+
 // Error channel of the C ABI (message returned by fusion_last_error).
 int api_fail(int code, const char* msg);
 

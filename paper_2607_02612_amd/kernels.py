@@ -7,6 +7,11 @@ on caller-supplied packed ragged buffers and returns device tensors, ordered
 on the current stream.  The scratch of a call is a tensor of torch's caching
 allocator, so a call neither allocates device memory itself nor waits for the
 stream; the caller's tensors are recorded on it, except by gemm.
+
+For long sequences and token caches: window_attention (a sliding window over
+packed rows), TokenCache with cache_append, paged_attention (one new token per
+sequence, adding up the attention weight of each cached token) and cache_evict
+(the tokens with the most weight stay).  They compute no gradients.
 """
 from __future__ import annotations
 
@@ -17,7 +22,7 @@ import numpy as np
 import torch
 
 from . import _native
-from ._native import FusionPackedOut, FusionRagged, check
+from ._native import FusionCache, FusionPackedOut, FusionRagged, check
 
 EPI = {"store": 0, "gelu": 1, "resid": 2, "f32": 3}
 
@@ -185,3 +190,258 @@ def topk_compact(x, size, origin, cu, keep_ratio, scores=None, heads=1, prune_w=
         _ptr(ln_g), _ptr(ln_b), _ptr(ln_out), byref(po), ws.data_ptr(), n,
         _stream(x, size, origin, scores, exit_logits, prune_w, prune_b, ln_g, ln_b)))
     return o, logits, exit_block, ln_out
+
+
+# ------------------------------------------- long sequences, token caches --
+_PREC = {torch.bfloat16: 1, torch.float32: 0}
+
+
+def _heads(t, name, dtype, heads, dh):
+    """Checks a [rows, heads, dh] tensor of any row and head strides in whole
+    16-byte pieces; returns the two strides."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dh:
+        raise ValueError(f"{name} must be a tensor [rows, {heads}, {dh}]")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}")
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient, and none is computed: detach it")
+    row, head, one = t.stride()
+    if one != 1 or (row | head) * t.element_size() % 16 or t.data_ptr() % 16:
+        raise ValueError(f"{name} must have contiguous heads, and strides and a base in whole "
+                         "16-byte pieces")
+    return row, head
+
+
+def _here(*tensors):
+    """All tensors on the current GPU, whose current stream the call uses."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"tensors must be on the current GPU (cuda:{dev}), got {t.device}")
+
+
+def _out(out, rows, heads, dh, like):
+    if out is None:
+        return torch.empty((rows, heads, dh), dtype=like.dtype, device=like.device)
+    _need(out, "out", like.dtype)
+    if tuple(out.shape) != (rows, heads, dh) or out.data_ptr() % 16:
+        raise ValueError(f"out must be a 16-byte aligned tensor [{rows}, {heads}, {dh}]")
+    _here(out)
+    return out
+
+
+def _offsets(cu):
+    """Host row offsets as int32 (the library checks their order)."""
+    a = np.asarray(cu)
+    if a.ndim != 1 or len(a) < 2 or a.dtype.kind not in "iu":
+        raise ValueError("offsets must be [batch + 1] whole numbers")
+    if a.dtype != np.int32 and (a.min() < 0 or a.max() > 1 << 30):
+        raise ValueError("offsets must be in 0 .. 2^30")
+    return _host_i32(a)
+
+
+def _count(v, name, lowest=0):
+    """A whole number, at most 2^30 (no sequence is longer)."""
+    if int(v) != v or v < lowest:
+        raise ValueError(f"{name} must be a whole number, at least {lowest}")
+    return min(int(v), 1 << 30)
+
+
+def window_attention(q, k, v, cu, window=None, sinks=0, causal=True, size=None, out=None):
+    """Attention of packed rows: row i of a sample sees its rows j <= i with
+    i - j < window or j < sinks; with causal=False those with |i - j| < window
+    or j < sinks.  window None: no limit.  q [M, heads, dh], k and v
+    [M, kv_heads, dh], bfloat16 or float32, dh a multiple of 8 up to 128, any
+    row and head strides in whole 16-byte pieces (views of one product's
+    output, say); cu: host offsets [batch + 1] (samples may be empty), rows
+    from cu[-1] on take no part; size: float32 [M], scores += ln(size), a size
+    of 0 hides the row.  Returns out [M, heads, dh]: rows that see nothing are
+    zero, rows from cu[-1] on are left as they were (zero if out is None)."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 3 or q.dtype not in _PREC:
+        raise ValueError("q must be a bfloat16 or float32 tensor [rows, heads, dh]")
+    M, heads, dh = q.shape
+    kv_heads = k.shape[1] if isinstance(k, torch.Tensor) and k.dim() == 3 else 0
+    strides = (ctypes.c_int64 * 6)(*_heads(q, "q", q.dtype, heads, dh),
+                                   *_heads(k, "k", q.dtype, kv_heads, dh),
+                                   *_heads(v, "v", q.dtype, kv_heads, dh))
+    if k.shape[0] != M or v.shape[0] != M:
+        raise ValueError("q, k and v must have the same rows")
+    if size is not None:
+        _need(size, "size", torch.float32)
+        if tuple(size.shape) != (M,):
+            raise ValueError("one size per row")
+    _here(q, k, v, size)
+    cu_h, cu_p = _offsets(cu)
+    if cu_h[-1] > M:
+        raise ValueError("offsets must end within the rows")
+    window = 0 if window is None else _count(window, "window", 1)
+    rows = int(cu_h[-1])
+    fresh = out is None
+    out = _out(out, M, heads, dh, q)
+    if fresh and rows < M:
+        out[max(rows, 0):].zero_()
+    check(_native.lib().fusion_window_attention(
+        _PREC[q.dtype], q.data_ptr(), k.data_ptr(), v.data_ptr(), strides, _ptr(size), cu_p,
+        len(cu_h) - 1, heads, kv_heads, dh, window, _count(sinks, "sinks"), int(bool(causal)),
+        out.data_ptr(), _stream(q, k, v, size, out)))
+    return out
+
+
+class TokenCache:
+    """A paged cache of keys and values with the attention weight that each
+    cached token has drawn; holds the caller's tensors and their checks.
+
+    k, v [pages, page_size, kv_heads, dh], bfloat16 or float32, contiguous
+    heads, other strides free in whole 16-byte pieces; table int32 [batch,
+    max_pages], the pages of each sequence (numbers outside the pages: none);
+    length, seen int32 [batch]: slots in use, tokens appended so far; weight
+    float32 and pos int32 [batch, max_pages * page_size]: attention weight and
+    position of the token in each slot.  length = seen = 0 is an empty
+    sequence; while they are equal, pos of slot x must be x.  The calls below
+    update k, v, length, seen, weight and pos in place, and the caller may
+    too, in stream order.  Pages that a call writes must not be shared."""
+
+    def __init__(self, k, v, table, length, seen, weight, pos):
+        if not isinstance(k, torch.Tensor) or k.dim() != 4 or k.dtype not in _PREC:
+            raise ValueError("k must be a bfloat16 or float32 tensor [pages, page_size, "
+                             "kv_heads, dh]")
+        for t, name in ((k, "k"), (v, "v")):
+            if not isinstance(t, torch.Tensor) or t.shape != k.shape or t.dtype != k.dtype:
+                raise ValueError("k and v must have the same shape and type")
+            if not t.is_cuda:
+                raise ValueError(f"{name} must be on a GPU")
+            extent = t.shape[3]
+            for st, n in sorted(zip(t.stride()[:3], t.shape[:3])):
+                if n > 1 and st < extent:
+                    raise ValueError(f"{name} must not overlap itself")
+                extent = st * (n - 1) + extent if n > 1 else extent
+            if t.stride(3) != 1 or t.data_ptr() % 16 or \
+                    any(st * t.element_size() % 16 for st in t.stride()[:3]):
+                raise ValueError(f"{name} must have contiguous heads, and strides and a base in "
+                                 "whole 16-byte pieces")
+        pages, page_size, kv_heads, dh = k.shape
+        for t, name in ((table, "table"), (length, "length"), (seen, "seen"), (pos, "pos")):
+            _need(t, name, torch.int32)
+        _need(weight, "weight", torch.float32)
+        if table.dim() != 2:
+            raise ValueError("table must be [batch, max_pages]")
+        batch, max_pages = table.shape
+        if tuple(length.shape) != (batch,) or tuple(seen.shape) != (batch,):
+            raise ValueError("length and seen must be [batch]")
+        if tuple(weight.shape) != (batch, max_pages * page_size) or pos.shape != weight.shape:
+            raise ValueError("weight and pos must be [batch, max_pages * page_size]")
+        self._tensors = (k, v, table, length, seen, weight, pos)
+        if any(t.device != k.device for t in self._tensors):
+            raise ValueError("the cache's tensors must be on one GPU")
+        self._c = FusionCache(k.data_ptr(), v.data_ptr(), k.stride()[:3], v.stride()[:3],
+                              table.data_ptr(), length.data_ptr(), seen.data_ptr(),
+                              weight.data_ptr(), pos.data_ptr(), _PREC[k.dtype], batch, pages,
+                              page_size, max_pages, kv_heads, dh)
+        self._ref = byref(self._c)
+        self._space, self._streams = {}, set()
+        self.batch, self.kv_heads, self.dh, self.dtype = batch, kv_heads, dh, k.dtype
+        self.capacity, self.device = max_pages * page_size, k.device
+        self._index = k.get_device()
+        self._bytes("fusion_cache_evict_workspace_bytes", 1)  # the library's checks
+
+    @classmethod
+    def empty(cls, batch, capacity, kv_heads, dh, page_size=64, dtype=torch.bfloat16):
+        """An empty cache on the current GPU with pages for `capacity` tokens
+        of every sequence."""
+        n = -(-capacity // page_size)
+        dev = torch.device("cuda", torch.cuda.current_device())
+        kv = [torch.empty((batch * n, page_size, kv_heads, dh), dtype=dtype, device=dev)
+              for _ in range(2)]
+        i32 = [torch.zeros(shape, dtype=torch.int32, device=dev)
+               for shape in ((batch,), (batch,), (batch, n * page_size))]
+        return cls(*kv, torch.arange(batch * n, dtype=torch.int32, device=dev).view(batch, n),
+                   i32[0], i32[1], torch.zeros((batch, n * page_size), device=dev), i32[2])
+
+    k, v, table, length, seen, weight, pos = (
+        property(lambda self, i=i: self._tensors[i]) for i in range(7))
+
+    def _bytes(self, entry, *args):
+        """Workspace of a call, asked once."""
+        key = (entry, *args)
+        if key not in self._space:
+            n = getattr(_native.lib(), entry)(self._ref, *args)
+            if n == 0:
+                check(-1)
+            self._space[key] = n
+        return self._space[key]
+
+    def _ready(self, entry=None, *args):
+        """(stream, workspace, its bytes) of a call; the cache's tensors are
+        recorded on each stream once, which holds until they are freed."""
+        if torch.cuda.current_device() != self._index:
+            raise ValueError(f"the cache is on {self.device}, not on the current GPU")
+        s = torch.cuda.current_stream()
+        if s.cuda_stream not in self._streams:
+            for t in self._tensors:
+                t.record_stream(s)
+            self._streams.add(s.cuda_stream)
+        if entry is None:
+            return s, None, 0
+        n = self._bytes(entry, *args)
+        return s, torch.empty(n, dtype=torch.uint8, device=self.device), n
+
+
+def cache_append(cache, k, v, cu=None):
+    """Append key and value rows [rows, kv_heads, dh]: one per sequence, or
+    rows cu[i] .. cu[i+1]-1 to sequence i (cu: host offsets).  Their weight
+    starts at 0; rows past a sequence's capacity are dropped."""
+    strides = (ctypes.c_int64 * 4)(*_heads(k, "k", cache.dtype, cache.kv_heads, cache.dh),
+                                   *_heads(v, "v", cache.dtype, cache.kv_heads, cache.dh))
+    _here(k, v)
+    cu_p = None
+    if cu is not None:
+        cu_h, cu_p = _offsets(cu)
+        if len(cu_h) != cache.batch + 1:
+            raise ValueError("offsets must be [batch + 1]")
+    rows = cache.batch if cu is None else int(cu_h[-1])
+    if k.shape[0] != rows or v.shape[0] != rows:
+        raise ValueError("rows do not match the sequences")
+    s, _, _ = cache._ready()
+    k.record_stream(s)
+    v.record_stream(s)
+    check(_native.lib().fusion_cache_append(cache._ref, k.data_ptr(), v.data_ptr(), strides, cu_p,
+                                            s.cuda_stream))
+
+
+def paged_attention(q, cache, window=None, sinks=0, accumulate=True, out=None):
+    """Attention of each sequence's newest token (appended before) over its
+    cached tokens; with a window, over those among the last `window` positions
+    or the first `sinks`.  q [batch, heads, dh]; returns out like q,
+    contiguous.  accumulate: cache.weight grows by the mean over the heads of
+    the attention probabilities."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 3 or q.shape[0] != cache.batch:
+        raise ValueError("q must be a tensor [batch, heads, dh]")
+    heads = q.shape[1]
+    strides = (ctypes.c_int64 * 2)(*_heads(q, "q", cache.dtype, heads, cache.dh))
+    window = 0 if window is None else _count(window, "window", 1)
+    _here(q)
+    out = _out(out, cache.batch, heads, cache.dh, q)
+    acc = int(bool(accumulate))
+    s, ws, n = cache._ready("fusion_paged_attention_workspace_bytes", heads, acc)
+    q.record_stream(s)
+    out.record_stream(s)
+    check(_native.lib().fusion_paged_attention(
+        cache._ref, q.data_ptr(), strides, heads, window, _count(sinks, "sinks"), acc,
+        out.data_ptr(), ws.data_ptr(), n, s.cuda_stream))
+    return out
+
+
+def cache_evict(cache, budget, sinks=0, recent=0):
+    """Bring every sequence down to `budget` tokens: the first `sinks` and
+    last `recent` positions stay, and the others by accumulated weight.
+    Returns src int32 [batch, budget]: the slot from which each slot's token
+    came, -1 past the sequence's length."""
+    budget, sinks = _count(budget, "budget", 1), _count(sinks, "sinks")
+    recent = _count(recent, "recent")
+    if sinks + recent > budget:
+        raise ValueError("sinks and recent do not fit the budget")
+    s, ws, n = cache._ready("fusion_cache_evict_workspace_bytes", budget)
+    src = torch.empty((cache.batch, budget), dtype=torch.int32, device=cache.device)
+    check(_native.lib().fusion_cache_evict(cache._ref, budget, sinks, recent, src.data_ptr(),
+                                           ws.data_ptr(), n, s.cuda_stream))
+    return src
