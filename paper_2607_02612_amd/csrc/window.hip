@@ -78,11 +78,341 @@ __global__ __launch_bounds__(256) void window_attention_valu(WindowArgs a, Windo
   if (64 + lane < dh) out[64 + lane] = St<T>::put(o1 * r);
 }
 
-}  // namespace
+// ------------------------------------------------------------ bf16 MFMA --
+// A workgroup of 4 waves takes 32 query rows per wave: of the heads that
+// share a key head as many as divide 4 at the same rows, else consecutive
+// rows of one head (waves of one workgroup then read the same key tiles, and
+// with shared key heads they also see the same ones).  Key tiles of 64 rows
+// stream through two LDS stages by asynchronous copies, the next tile's in
+// flight while the current one is computed, one barrier per tile; two
+// workgroups share a CU (128-wide heads), so that one's softmax runs beside
+// the other's matrix products.
+//
+// Scores are taken transposed, S^T = K Q^T, with v_mfma_f32_32x32x16_bf16:
+// lane (hl, c) = (lane / 32, lane % 32) holds query c against keys
+// 8 (i / 4) + 4 hl + i % 4, i < 16, of each 32-key half, so the row maximum
+// and sum are reductions over registers and one lane swap, and the registers
+// i = 8t .. 8t + 7, rounded to bf16, are the operand of the t-th step of
+// O^T = V^T P^T as they stand.  V^T comes from the row-major tile by the
+// transposing LDS read, with the same key order.  The running maximum moves
+// only when a row's maximum grows by more than 8 in the base-2 exponent (P
+// stays below 2^8, whose relative precision is that of 1), per row, so that
+// no row's result depends on another's; rows whose maximum stays multiply by 1.
+//
+// LDS rows are 2 DP bytes.  K's 16-byte pieces are XOR-permuted by the row
+// (mod 16 or 8), V's 32-byte segments by the row mod 4: the 16-byte reads of
+// consecutive rows and the 8-byte transposing reads of 4 rows spread over all
+// banks.  The copies write LDS in lane order, so the permutation is made in
+// the source address.
+//
+// A probability of 0 does not take a value out of P V when that value is
+// infinite or NaN.  A tile that some query of the workgroup sees and another
+// does not is therefore searched for such values; if there are any, they are
+// cleared in LDS and added by hand to the rows that see them (their weight is
+// positive, so an infinity stays one).
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
 
-template <typename T>
-hipError_t launch_window_attention(const WindowArgs& a, const int32_t* cu_host, int batch,
-                                   hipStream_t s) {
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int WKT = 64;  // keys per tile
+constexpr int WNW = 4;   // waves per workgroup
+
+// global -> LDS copy of 16 bytes per lane (lane l's land at the wave-uniform
+// LDS address + 16 l), awaited by wait_copies
+__device__ __forceinline__ void copy16(const void* sbase, unsigned voff, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+               :: "v"(voff), "s"(sbase), "s"(__builtin_amdgcn_readfirstlane(lds))
+               : "memory", "m0");
+}
+__device__ __forceinline__ void copy16(const void* p, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+               :: "v"(p), "s"(__builtin_amdgcn_readfirstlane(lds))
+               : "memory", "m0");
+}
+__device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// What the dimensions past dh are read from when the head is not DP wide.
+__device__ const uint4 kZeros = {0, 0, 0, 0};
+
+// Whether row i of a sample sees its row j (both in the sample).
+__device__ __forceinline__ bool sees(const WindowArgs& a, int i, int j) {
+  if (a.causal) return j <= i && (i - j < a.window || j < a.sinks);
+  return (i - j < a.window && j - i < a.window) || j < a.sinks;
+}
+// Whether all of rows i0 .. i1 see all of j0 .. j1.
+__device__ __forceinline__ bool all_see(const WindowArgs& a, int i0, int i1, int j0, int j1) {
+  if (a.causal) return j1 <= i0 && (i1 - j0 < a.window || j1 < a.sinks);
+  return (i1 - j0 < a.window && j1 - i0 < a.window) || j1 < a.sinks;
+}
+// Whether none of rows i0 .. i1 sees any of j0 .. j1.
+__device__ __forceinline__ bool none_see(const WindowArgs& a, int i0, int i1, int j0, int j1) {
+  if (a.causal) return j0 > i1 || (i0 - j1 >= a.window && j0 >= a.sinks);
+  return (i0 - j1 >= a.window || j0 - i1 >= a.window) && j0 >= a.sinks;
+}
+
+// The query rows of a workgroup and the key tiles that any of them sees: the
+// first `ns` tiles of the sample (sinks), then tiles lo .. hi.
+struct WindowPlan {
+  int base, n;   // the sample's first row and rows
+  int q0, q1;    // first and last query row
+  int ns, lo, nt;
+  __device__ __forceinline__ int tile(int it) const { return it < ns ? it : lo + it - ns; }
+};
+__device__ __forceinline__ WindowPlan window_plan(const WindowArgs& a, const WindowSeqs& sq, int tile,
+                                                  int rows, int keys) {
+  int lo = 0, hi = sq.n - 1;  // the last sample whose first tile is not after this one
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (sq.tile[mid] <= tile) lo = mid; else hi = mid - 1;
+  }
+  WindowPlan p;
+  p.base = sq.cu[lo];
+  p.n = sq.cu[lo + 1] - p.base;
+  p.q0 = (tile - sq.tile[lo]) * rows;
+  p.q1 = min(p.q0 + rows, p.n) - 1;
+  p.lo = max(0, p.q0 - a.window + 1) / keys;
+  const int last = a.causal ? p.q1 : min(p.n - 1, p.q1 + a.window - 1);
+  p.ns = min((min(a.sinks, p.n) + keys - 1) / keys, p.lo);
+  p.nt = p.ns + last / keys - p.lo + 1;
+  // sinks past the window's end (two-sided)
+  if (!a.causal) p.nt = max(p.nt, p.ns + (min(a.sinks, p.n) + keys - 1) / keys - p.lo);
+  return p;
+}
+
+template <int DP, bool PAD, bool SIZES>
+__global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma(WindowArgs a, WindowSeqs sq,
+                                                                     int tiles, int hshift) {
+  constexpr int PPR = DP / 8;             // 16-byte pieces per row
+  constexpr int RPC = 64 / PPR;           // rows per copy
+  constexpr int NC = WKT / RPC / WNW;     // copies of K (and of V) per wave and tile
+  constexpr int ROWB = DP * 2, TILEB = WKT * ROWB;
+  constexpr int KS = DP / 16, ND = DP / 32;
+  __shared__ __attribute__((aligned(16))) char smem[4 * TILEB];  // [stage][K, V]
+  __shared__ float lnS[2][WKT];
+  __shared__ int s_bad;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int hl = lane >> 5, c = lane & 31;
+  const int per_group = a.group >> hshift, units = a.H >> hshift;
+  const int unit = blockIdx.x % units, kh = unit / per_group;
+  const int h = unit % per_group * (1 << hshift) + kh * a.group + (wave & ((1 << hshift) - 1));
+  const WindowPlan pl = window_plan(a, sq, tiles - 1 - blockIdx.x / units,
+                                    32 * (WNW >> hshift), WKT);
+  const int n = pl.n, dh = a.dh;
+  const int w0 = pl.q0 + 32 * (wave >> hshift), w1 = min(w0 + 31, n - 1);
+  const bf16_t* kg = (const bf16_t*)a.k + (int64_t)pl.base * a.k_row + (int64_t)kh * a.k_head;
+  const bf16_t* vg = (const bf16_t*)a.v + (int64_t)pl.base * a.v_row + (int64_t)kh * a.v_head;
+  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
+  if (tid == 0) s_bad = -1;
+
+  // copy of one tile: the wave's rows r = (wave NC + u) RPC + lane / PPR
+  auto copy_tile = [&](int t, int st) {
+    const int k0 = t * WKT, lim = n - 1 - k0;
+    const bf16_t* kt = kg + (int64_t)k0 * a.k_row;
+    const bf16_t* vt = vg + (int64_t)k0 * a.v_row;
+#pragma unroll
+    for (int u = 0; u < NC; u++) {
+      const int r = (wave * NC + u) * RPC + lane / PPR, rr = min(r, lim), p = lane % PPR;
+      const int pk = p ^ (r & (PPR - 1)), pv = p ^ ((r & 3) << 1);
+      const unsigned dst = lds0 + st * 2 * TILEB + (wave * NC + u) * 1024;
+      const unsigned ko = (unsigned)rr * (unsigned)a.k_row * 2 + pk * 16;
+      const unsigned vo = (unsigned)rr * (unsigned)a.v_row * 2 + pv * 16;
+      if (PAD) {
+        copy16(pk * 8 < dh ? (const void*)((const char*)kt + ko) : (const void*)&kZeros, dst);
+        copy16(pv * 8 < dh ? (const void*)((const char*)vt + vo) : (const void*)&kZeros,
+               dst + TILEB);
+      } else {
+        copy16(kt, ko, dst);
+        copy16(vt, vo, dst + TILEB);
+      }
+    }
+  };
+  float size_next = 0.f;
+  auto load_size = [&](int t) {
+    if (SIZES && tid < WKT) size_next = a.size[pl.base + min(t * WKT + tid, n - 1)];
+  };
+  auto put_size = [&](int st) {
+    if (SIZES && tid < WKT) lnS[st][tid] = size_next > 0.f ? logf(size_next) * kLog2e : -INFINITY;
+  };
+  copy_tile(pl.tile(0), 0);
+  load_size(pl.tile(0));
+
+  // Q^T operand: lane holds Q[w0 + c][16 s + 8 hl .. + 7]
+  bf16x8_t qf[KS];
+  {
+    const bf16_t* qr = (const bf16_t*)a.q + (int64_t)(pl.base + min(w0 + c, n - 1)) * a.q_row +
+                       (int64_t)h * a.q_head;
+#pragma unroll
+    for (int s = 0; s < KS; s++) {
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (!PAD || 16 * s + 8 * hl < dh) v = *(const uint4*)(qr + 16 * s + 8 * hl);
+      qf[s] = __builtin_bit_cast(bf16x8_t, v);
+    }
+  }
+  put_size(0);
+  const float sc2 = a.scale * kLog2e;
+  float m = -INFINITY, l = 0.f;
+  f32x16_t O[ND];
+#pragma unroll
+  for (int d = 0; d < ND; d++)
+#pragma unroll
+    for (int i = 0; i < 16; i++) O[d][i] = 0.f;
+
+  // LDS addresses of the operands: K row c of a half, V rows of a 16-lane group
+  const int krow = c * ROWB, kx = c & (PPR - 1);
+  const int vkey = (lane & 15) >> 2;
+  const int vcol = ((lane >> 4) & 1) * 32 + (lane & 3) * 8;  // bytes within a 64-byte dim tile
+  for (int it = 0; it < pl.nt; it++) {
+    const int st = it & 1, t = pl.tile(it), k0 = t * WKT;
+    wait_copies();
+    __syncthreads();
+    if (it + 1 < pl.nt) {
+      copy_tile(pl.tile(it + 1), st ^ 1);
+      load_size(pl.tile(it + 1));
+    }
+    const char* Ks = smem + st * 2 * TILEB;
+    char* Vs = smem + st * 2 * TILEB + TILEB;
+    bool bad = false;
+    if (SIZES || k0 + WKT > n || !all_see(a, pl.q0, pl.q1, k0, k0 + WKT - 1)) {
+      uint32_t any = 0;
+#pragma unroll
+      for (int u = 0; u < TILEB / (64 * WNW * 16); u++) {
+        const uint4 v = *(const uint4*)(Vs + (tid + u * 64 * WNW) * 16);
+        any |= ((v.x & 0x7F807F80u) + 0x00800080u) | ((v.y & 0x7F807F80u) + 0x00800080u) |
+               ((v.z & 0x7F807F80u) + 0x00800080u) | ((v.w & 0x7F807F80u) + 0x00800080u);
+      }
+      if (any & 0x80008000u) s_bad = it;
+      __syncthreads();
+      bad = s_bad == it;
+    }
+    const bool active = w0 < n && !none_see(a, w0, w1, k0, k0 + WKT - 1);
+    if (bad) {
+      for (int u = tid; u < TILEB / 2; u += 64 * WNW) {
+        bf16_t* v = (bf16_t*)Vs + u;
+        if ((*v & 0x7F80) == 0x7F80) *v = 0;
+      }
+      __syncthreads();
+      for (int j = k0; active && j < min(n, k0 + WKT); j++) {
+        const bool see = w0 + c < n && sees(a, w0 + c, j) && !(SIZES && !(a.size[pl.base + j] > 0.f));
+        if (!see) continue;
+        const bf16_t* v = vg + (int64_t)j * a.v_row + 4 * hl;
+#pragma unroll
+        for (int d = 0; d < ND; d++)
+#pragma unroll
+          for (int i4 = 0; i4 < 4; i4++) {
+            if (PAD && 32 * d + 8 * i4 >= dh) break;
+            const uint2 x = *(const uint2*)(v + 32 * d + 8 * i4);
+            const float e[4] = {__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xFFFF0000u),
+                                __uint_as_float(x.y << 16), __uint_as_float(x.y & 0xFFFF0000u)};
+#pragma unroll
+            for (int q = 0; q < 4; q++) O[d][4 * i4 + q] += fabsf(e[q]) < INFINITY ? 0.f : e[q];
+          }
+      }
+    }
+    if (active) {
+      f32x16_t S[2];
+#pragma unroll
+      for (int x = 0; x < 2; x++) {
+#pragma unroll
+        for (int i = 0; i < 16; i++) S[x][i] = 0.f;
+#pragma unroll
+        for (int s = 0; s < KS; s++) {
+          const bf16x8_t kf = *(const bf16x8_t*)(Ks + x * 32 * ROWB + krow + (((2 * s + hl) ^ kx) << 4));
+          S[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], S[x], 0, 0, 0);
+        }
+      }
+      const bool edge = k0 + WKT > n || !all_see(a, w0, w1, k0, k0 + WKT - 1);
+      // -inf for keys that the query does not see; with sizes already in base 2
+      if (SIZES || edge) {
+#pragma unroll
+        for (int x = 0; x < 2; x++)
+#pragma unroll
+          for (int i4 = 0; i4 < 4; i4++) {
+            f32x4_t ln = {0.f, 0.f, 0.f, 0.f};
+            if (SIZES) ln = *(const f32x4_t*)(&lnS[st][x * 32 + 8 * i4 + 4 * hl]);
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+              const int key = k0 + x * 32 + 8 * i4 + 4 * hl + j;
+              const bool see = (!edge || (key < n && sees(a, w0 + c, key))) &&
+                               !(SIZES && ln[j] == -INFINITY);
+              const float t = SIZES ? fmaf(S[x][4 * i4 + j], sc2, ln[j]) : S[x][4 * i4 + j];
+              S[x][4 * i4 + j] = see ? t : -INFINITY;
+            }
+          }
+      }
+      float mt = -INFINITY;
+#pragma unroll
+      for (int x = 0; x < 2; x++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) mt = fmaxf(mt, S[x][i]);
+      mt = max_xor32(mt);
+      if (!SIZES) mt *= sc2;
+      const bool grow = mt > m + 8.f;
+      if (__any(grow)) {
+        const float f = grow ? __builtin_amdgcn_exp2f(m - mt) : 1.f;
+        if (grow) m = mt;
+        l *= f;
+#pragma unroll
+        for (int d = 0; d < ND; d++)
+#pragma unroll
+          for (int i = 0; i < 16; i++) O[d][i] *= f;
+      }
+      const float mu = m == -INFINITY ? 0.f : m;
+      bf16x8_t pf[4];
+      float lt[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < 2; x++)
+#pragma unroll
+        for (int y = 0; y < 2; y++) {
+          union { uint32_t u[4]; bf16x8_t v; } p;
+#pragma unroll
+          for (int w = 0; w < 4; w++) {
+            const float s0 = S[x][8 * y + 2 * w], s1 = S[x][8 * y + 2 * w + 1];
+            const float e0 = __builtin_amdgcn_exp2f(SIZES ? s0 - mu : fmaf(s0, sc2, -mu));
+            const float e1 = __builtin_amdgcn_exp2f(SIZES ? s1 - mu : fmaf(s1, sc2, -mu));
+            lt[w] += e0 + e1;
+            p.u[w] = pack_bf16x2(e0, e1);
+          }
+          pf[2 * x + y] = p.v;
+        }
+      l += (lt[0] + lt[1]) + (lt[2] + lt[3]);
+#pragma unroll
+      for (int y = 0; y < 4; y++)
+#pragma unroll
+        for (int d = 0; d < ND; d++) {
+          union { s16x4_t h[2]; bf16x8_t v; } vf;
+#pragma unroll
+          for (int z = 0; z < 2; z++) {
+            const int key = 16 * y + 8 * z + 4 * hl + vkey;  // key % 4 == vkey
+            const int seg = (d * 2 + (vcol >> 5)) ^ vkey;
+            vf.h[z] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) s16x4_t*)(Vs + key * ROWB + seg * 32 + (vcol & 31)));
+          }
+          O[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, pf[y], O[d], 0, 0, 0);
+        }
+    }
+    if (it + 1 < pl.nt) put_size(st ^ 1);
+  }
+  l = sum_xor32(l);
+  if (w0 + c < n) {
+    const float r = l == 0.f ? 0.f : 1.f / l;
+    bf16_t* out = (bf16_t*)a.out + ((int64_t)(pl.base + w0 + c) * a.H + h) * dh + 4 * hl;
+#pragma unroll
+    for (int d = 0; d < ND; d++)
+#pragma unroll
+      for (int i4 = 0; i4 < 4; i4++)
+        if (!PAD || 32 * d + 8 * i4 < dh)
+          *(uint2*)(out + 32 * d + 8 * i4) =
+              make_uint2(pack_bf16x2(O[d][4 * i4] * r, O[d][4 * i4 + 1] * r),
+                         pack_bf16x2(O[d][4 * i4 + 2] * r, O[d][4 * i4 + 3] * r));
+  }
+}
+
+// Runs `launch(samples, tiles)` for all samples, as many at once as the
+// arguments of a launch hold, with tiles of `rows` rows.
+template <typename F>
+hipError_t for_samples(const int32_t* cu_host, int batch, int rows, F launch) {
   for (int f = 0; f < batch; f += WIN_SEQS) {
     WindowSeqs sq;
     sq.n = std::min(batch - f, WIN_SEQS);
@@ -90,13 +420,42 @@ hipError_t launch_window_attention(const WindowArgs& a, const int32_t* cu_host, 
     for (int i = 0; i <= sq.n; i++) {
       sq.cu[i] = cu_host[f + i];
       sq.tile[i] = tiles;
-      if (i < sq.n) tiles += (cu_host[f + i + 1] - cu_host[f + i] + WIN_ROWS - 1) / WIN_ROWS;
+      if (i < sq.n) tiles += (cu_host[f + i + 1] - cu_host[f + i] + rows - 1) / rows;
     }
     if (tiles == 0) continue;
-    window_attention_valu<T><<<dim3(tiles, a.H), 256, 0, s>>>(a, sq);
+    launch(sq, tiles);
     if (hipError_t e = hipGetLastError()) return e;
   }
   return hipSuccess;
+}
+
+template <int DP, bool PAD>
+hipError_t launch_mfma(const WindowArgs& a, const int32_t* cu_host, int batch, hipStream_t s) {
+  // heads of a group per workgroup, 1 << hshift
+  const int hshift = a.group % 4 == 0 ? 2 : a.group % 2 == 0 ? 1 : 0;
+  return for_samples(cu_host, batch, 32 * (WNW >> hshift), [&](const WindowSeqs& sq, int tiles) {
+    const dim3 grid((unsigned)tiles * (a.H >> hshift));
+    if (a.size)
+      window_attention_mfma<DP, PAD, true><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
+    else
+      window_attention_mfma<DP, PAD, false><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
+  });
+}
+
+}  // namespace
+
+template <typename T>
+hipError_t launch_window_attention(const WindowArgs& a, const int32_t* cu_host, int batch,
+                                   hipStream_t s) {
+  if (sizeof(T) == 2) {
+    if (a.dh == 64) return launch_mfma<64, false>(a, cu_host, batch, s);
+    if (a.dh < 64) return launch_mfma<64, true>(a, cu_host, batch, s);
+    if (a.dh == 128) return launch_mfma<128, false>(a, cu_host, batch, s);
+    return launch_mfma<128, true>(a, cu_host, batch, s);
+  }
+  return for_samples(cu_host, batch, WIN_ROWS, [&](const WindowSeqs& sq, int tiles) {
+    window_attention_valu<T><<<dim3(tiles, a.H), 256, 0, s>>>(a, sq);
+  });
 }
 template hipError_t launch_window_attention<float>(const WindowArgs&, const int32_t*, int,
                                                    hipStream_t);
