@@ -328,6 +328,8 @@ int check_cache(const fusion_cache* c, CacheArgs* a) {
   if (c->pages < 1 || c->page_size < 1 || c->max_pages < 1)
     return bad("pages, page_size and max_pages must be positive");
   if ((int64_t)c->max_pages * c->page_size > (1 << 30)) return bad("capacity above 2^30 slots");
+  if ((int64_t)c->batch * c->max_pages * c->page_size > (int64_t)1 << 34)
+    return bad("more than 2^34 slots");
   if (!c->k || !c->v || !c->table || !c->len || !c->seen || !c->weight || !c->pos)
     return bad("null cache buffer");
   if (((uintptr_t)c->k | (uintptr_t)c->v) % 16) return bad("buffers must be 16-byte aligned");

@@ -254,12 +254,12 @@ def _cache(torch, rng, dtype, lengths, hkv, dh, page, cap, evicted=False, heads_
 def _rows(cache, b, n):
     """Keys, values and `stored` marks of slots 0 .. n-1 in 64 bits."""
     page = cache.k.shape[1]
-    t = cache.table[b].cpu().numpy()
     x = np.arange(n)
-    pg = t[x // page]
-    ok = (pg >= 0) & (pg < cache.k.shape[0])
-    at = np.where(ok, pg, 0)
-    return _np(cache.k)[at, x % page], _np(cache.v)[at, x % page], ok
+    t = cache.table[b].long()
+    ok = (t >= 0) & (t < cache.k.shape[0])
+    t = t.clamp(0, cache.k.shape[0] - 1)[:-(-n // page)]
+    k, v = (_np(a[t]).reshape(-1, *a.shape[2:])[:n] for a in (cache.k, cache.v))
+    return k, v, ok.cpu().numpy()[x // page]
 
 
 def _paged_ref(q, cache, window, sinks, dtype):
@@ -359,6 +359,22 @@ def test_paged_attention_hidden_and_odd_contents(torch_cuda, dtype):
             _close(_np(_kern().paged_attention(q, d, window, sinks)), out, tol, (window, value))
             err = np.abs(_np(w) - _np(c.weight) - add)
             assert (err <= add_tol + U32 * (_np(c.weight) + add)).all()
+
+
+@pytest.mark.parametrize("B", [63, 64, 65, 200, 1024, 1025, 2100])
+def test_paged_attention_many_sequences(torch_cuda, B):
+    """Around the sequences that a wave looks at together and those up to
+    which the work is split over lengths, empty ones among them."""
+    torch = torch_cuda
+    rng = np.random.default_rng(B)
+    lengths = [int(v) for v in rng.integers(0, 90, size=B)]
+    lengths[-1] = 0
+    c = _cache(torch, rng, "bf16", lengths, 1, 64, 16, 96, evicted=True)
+    q = _normal(torch, rng, "bf16", B, 2, 64)
+    before = _np(c.weight)
+    out, tol, add, add_tol = _paged_ref(_np(q), c, 60, 2, "bf16")
+    _close(_np(_kern().paged_attention(q, c, 60, 2)), out, tol)
+    assert (np.abs(_np(c.weight) - before - add) <= add_tol + U32 * (before + add)).all()
 
 
 def test_paged_attention_offsets_past_32_bits(torch_cuda):
