@@ -19,6 +19,22 @@ __device__ __forceinline__ int held(const CacheArgs& c, int b) {
   return max(0, min(c.len[b], c.cap));
 }
 
+// 16-byte pieces of the rows of a token's key heads (or value heads).
+struct RowPieces {
+  int per_head, all;
+};
+template <typename T>
+__device__ __forceinline__ RowPieces row_pieces(const CacheArgs& c) {
+  const int p = c.dh * (int)sizeof(T) / 16;
+  return {p, p * c.Hkv};
+}
+// Address of a piece of a cached row.
+template <typename T>
+__device__ __forceinline__ uint4* piece(void* base, int64_t page_stride, int64_t row_stride,
+                                        int64_t head_stride, int page, int place, int h, int d) {
+  return (uint4*)((T*)base + page * page_stride + place * row_stride + h * head_stride) + d;
+}
+
 // Offsets of a batch as kernel arguments.
 constexpr int APPEND_SEQS = 896;
 struct AppendSeqs {
@@ -27,49 +43,71 @@ struct AppendSeqs {
 };
 
 // --------------------------------------------------------------- append --
-// One workgroup per new row; row r of sample i goes to slot len + r - cu[i].
+// Row r of sample i goes to slot len + r - cu[i]: a copy, bound by its bytes.
+// A wave copies whole rows in 16-byte pieces.  With few rows a sample, one
+// workgroup takes a sample's rows and moves its lengths on; else the lengths
+// move in a launch of their own, after all rows have read them.
+constexpr int APPEND_FEW = 8;  // rows of a sample up to which one workgroup takes them
+
 template <typename T>
-__global__ __launch_bounds__(256) void append_kernel(CacheArgs c, AppendArgs a, AppendSeqs sq) {
-  int b, r, nth;
-  if (sq.n == 0) {  // one row per sample
-    b = r = blockIdx.x;
-    nth = 0;
-  } else {
-    r = sq.cu[0] + blockIdx.x;
-    int lo = 0, hi = sq.n - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (sq.cu[mid] <= r) lo = mid; else hi = mid - 1;
-    }
-    b = sq.first + lo;
-    nth = r - sq.cu[lo];
-  }
-  const int64_t slot = (int64_t)held(c, b) + nth;
+__device__ __forceinline__ void append_row(const CacheArgs& c, const AppendArgs& a, int b, int r,
+                                           int64_t slot, int pos, int lane, int step) {
   if (slot >= c.cap) return;
-  if (threadIdx.x == 0) {
+  if (lane == 0) {
     c.weight[(int64_t)b * c.cap + slot] = 0.f;
-    c.pos[(int64_t)b * c.cap + slot] = c.seen[b] + nth;
+    c.pos[(int64_t)b * c.cap + slot] = pos;
   }
   const uint32_t pg = quot((uint32_t)slot, c.page);
-  const int p = page_of(c, b, pg);
-  if (p < 0) return;
-  const int64_t in_page = slot - (int64_t)pg * c.page.d;
-  T* kd = (T*)c.k + p * c.k_page + in_page * c.k_row;
-  T* vd = (T*)c.v + p * c.v_page + in_page * c.v_row;
-  const T* ks = (const T*)a.k + r * a.k_row;
-  const T* vs = (const T*)a.v + r * a.v_row;
-  for (int t = threadIdx.x; t < c.Hkv * c.dh; t += 256) {
-    const int h = t / c.dh, d = t - h * c.dh;
-    kd[h * c.k_head + d] = ks[h * a.k_head + d];
-    vd[h * c.v_head + d] = vs[h * a.v_head + d];
+  const int page = page_of(c, b, pg), place = (int)(slot - (int64_t)pg * c.page.d);
+  if (page < 0) return;
+  const RowPieces rp = row_pieces<T>(c);
+  for (int t = lane; t < rp.all; t += step) {
+    const int h = t / rp.per_head, d = t - h * rp.per_head;
+    const uint4 k = ((const uint4*)((const T*)a.k + r * a.k_row + h * a.k_head))[d];
+    const uint4 v = ((const uint4*)((const T*)a.v + r * a.v_row + h * a.v_head))[d];
+    *piece<T>(c.k, c.k_page, c.k_row, c.k_head, page, place, h, d) = k;
+    *piece<T>(c.v, c.v_page, c.v_row, c.v_head, page, place, h, d) = v;
   }
+}
+
+// One workgroup per sample; first[b] .. its rows, one each without offsets.
+template <typename T, bool OFFSETS>
+__global__ __launch_bounds__(256) void append_few(CacheArgs c, AppendArgs a, AppendSeqs sq) {
+  const int b = OFFSETS ? sq.first + blockIdx.x : blockIdx.x;
+  const int r0 = OFFSETS ? sq.cu[blockIdx.x] : b, n = OFFSETS ? sq.cu[blockIdx.x + 1] - r0 : 1;
+  const int have = held(c, b), seen = c.seen[b];
+  __syncthreads();  // all waves have the lengths
+  if (threadIdx.x == 0 && n > 0) {
+    const int fit = min(n, c.cap - have);
+    c.len[b] = have + fit;
+    c.seen[b] = seen + fit;
+  }
+  if (n == 1) {
+    append_row<T>(c, a, b, r0, have, seen, threadIdx.x, 256);
+  } else {
+    for (int i = threadIdx.x >> 6; i < n; i += 4)
+      append_row<T>(c, a, b, r0 + i, (int64_t)have + i, seen + i, threadIdx.x & 63, 64);
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void append_many(CacheArgs c, AppendArgs a, AppendSeqs sq) {
+  const int r = sq.cu[0] + blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (r >= sq.cu[sq.n]) return;
+  int lo = 0, hi = sq.n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (sq.cu[mid] <= r) lo = mid; else hi = mid - 1;
+  }
+  const int b = sq.first + lo, nth = r - sq.cu[lo];
+  append_row<T>(c, a, b, r, (int64_t)held(c, b) + nth, c.seen[b] + nth, threadIdx.x & 63, 64);
 }
 
 __global__ __launch_bounds__(256) void append_lengths(CacheArgs c, AppendSeqs sq) {
   const int t = blockIdx.x * 256 + threadIdx.x;
-  if (t >= (sq.n ? sq.n : c.B)) return;
-  const int b = sq.n ? sq.first + t : t, n = sq.n ? sq.cu[t + 1] - sq.cu[t] : 1;
-  const int have = held(c, b), fit = min(n, c.cap - have);
+  if (t >= sq.n) return;
+  const int b = sq.first + t, have = held(c, b), fit = min(sq.cu[t + 1] - sq.cu[t], c.cap - have);
+  if (sq.cu[t + 1] == sq.cu[t]) return;
   c.len[b] = have + fit;
   c.seen[b] += fit;
 }
@@ -367,6 +405,7 @@ __global__ __launch_bounds__(256) void paged_attention(CacheArgs c, PagedArgs a,
 // The parts of every sequence joined: workgroups 0 .. B H - 1 write an output
 // row each, the others add the weights of 1024 visible tokens of a sequence.
 constexpr int JOIN_HEADS = 128;
+constexpr int JOIN_AHEAD = 8;  // loads under way per thread
 template <typename T>
 __global__ __launch_bounds__(256) void paged_join(CacheArgs c, PagedArgs a, PagedSpace ws, int DP,
                                                   int chunks) {
@@ -415,11 +454,21 @@ __global__ __launch_bounds__(256) void paged_join(CacheArgs c, PagedArgs a, Page
       // maximum and 1 / (sum H) of the heads, 16 lanes a head
       for (int h = tid >> 4; h < nh; h += 16) {
         float m = -INFINITY, l = 0.f;
-        for (int i = tid & 15; i < plan.y; i += 16) {
-          const float2 ml = ws.ml[(int64_t)(plan.x + i) * a.H + hc + h];
-          const float m2 = fmaxf(m, ml.x);
-          if (m2 != -INFINITY)
-            l = l * __builtin_amdgcn_exp2f(m - m2) + ml.y * __builtin_amdgcn_exp2f(ml.x - m2);
+        for (int i = tid & 15; i < plan.y; i += 16 * JOIN_AHEAD) {
+          float2 ml[JOIN_AHEAD];
+          float m2 = m;
+#pragma unroll
+          for (int u = 0; u < JOIN_AHEAD; u++) {
+            ml[u] = ws.ml[(int64_t)(plan.x + min(i + 16 * u, plan.y - 1)) * a.H + hc + h];
+            if (i + 16 * u >= plan.y) ml[u].x = -INFINITY;
+          }
+#pragma unroll
+          for (int u = 0; u < JOIN_AHEAD; u++) m2 = fmaxf(m2, ml[u].x);
+          if (m2 != -INFINITY) {
+            l *= __builtin_amdgcn_exp2f(m - m2);
+#pragma unroll
+            for (int u = 0; u < JOIN_AHEAD; u++) l += ml[u].y * __builtin_amdgcn_exp2f(ml[u].x - m2);
+          }
           m = m2;
         }
         for (int o = 8; o; o >>= 1) {
@@ -434,11 +483,18 @@ __global__ __launch_bounds__(256) void paged_join(CacheArgs c, PagedArgs a, Page
       __syncthreads();
       if (x < vis.nv) {
         const float* sp = ws.score + ((int64_t)b * a.H + hc) * ws.capv + x;
-        for (int h = 0; h < nh; h++) {
-          const f32x4_t s = *(const f32x4_t*)(sp + (int64_t)h * ws.capv);
-          const float2 ml = s_ml[h];
+        for (int h = 0; h < nh; h += JOIN_AHEAD) {
+          f32x4_t s[JOIN_AHEAD];
 #pragma unroll
-          for (int j = 0; j < 4; j++) w[j] = fmaf(__builtin_amdgcn_exp2f(s[j] - ml.x), ml.y, w[j]);
+          for (int u = 0; u < JOIN_AHEAD; u++)
+            s[u] = *(const f32x4_t*)(sp + (int64_t)min(h + u, nh - 1) * ws.capv);
+#pragma unroll
+          for (int u = 0; u < JOIN_AHEAD; u++) {
+            const float2 ml = s_ml[min(h + u, nh - 1)];
+            const float r = h + u < nh ? ml.y : 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; j++) w[j] = fmaf(__builtin_amdgcn_exp2f(s[u][j] - ml.x), r, w[j]);
+          }
         }
       }
     }
@@ -464,16 +520,45 @@ struct EvictSpace {
   int room;     // most moves of a sequence
 };
 
-// One workgroup of 1024 per sequence: the budget-th largest key by four
-// rounds of 256 bins, then one pass in slot order that lists free slots below
-// the budget and hands them to the kept ones beyond it.
-__global__ __launch_bounds__(1024) void evict_select(CacheArgs c, EvictArgs a, EvictSpace ws) {
+template <typename T>
+__device__ __forceinline__ void move_row(const CacheArgs& c, int b, int2 m, int lane, int step) {
+  const uint32_t pd = quot(m.x, c.page), ps = quot(m.y, c.page);
+  const int to = page_of(c, b, pd), from = page_of(c, b, ps);
+  if (to < 0 || from < 0) return;
+  const int rd = m.x - (int)(pd * c.page.d), rs = m.y - (int)(ps * c.page.d);
+  const RowPieces rp = row_pieces<T>(c);
+  for (int t = lane; t < rp.all; t += step) {
+    const int h = t / rp.per_head, d = t - h * rp.per_head;
+    const uint4 k = *piece<T>(c.k, c.k_page, c.k_row, c.k_head, from, rs, h, d);
+    const uint4 v = *piece<T>(c.v, c.v_page, c.v_row, c.v_head, from, rs, h, d);
+    *piece<T>(c.k, c.k_page, c.k_row, c.k_head, to, rd, h, d) = k;
+    *piece<T>(c.v, c.v_page, c.v_row, c.v_head, to, rd, h, d) = v;
+  }
+}
+
+// The choice, one workgroup of NT threads per sequence.  The budget-th largest
+// key is found from the top by digits of 12, 10 and 10 bits: counts of the
+// keys that share the digits found so far in bins, a sum over the bins from
+// the highest, the bin where it reaches the rank.  (The first digit holds the
+// sign, the exponent and three bits of the weight, so that weights of similar
+// size meet in few bins: the counts are LDS atomics, and lanes that hit one
+// address wait for each other.)  Each thread holds E neighbouring slots' keys
+// in registers, of longer sequences one chunk of NT E slots after the other,
+// read again in every round.  Then one pass in slot order lists the free
+// slots below the budget and hands them to the kept ones beyond it.  Bound by
+// the rounds' latency (barriers, bins); 64 sequences of 4,097 slots are read
+// in 0.5 us.
+constexpr int EVICT_BINS = 4096;
+constexpr int EVICT_FEW = 32;  // moves that the choosing workgroup makes itself
+template <typename T, int NT, int E>
+__global__ __launch_bounds__(NT) void evict_select(CacheArgs c, EvictArgs a, EvictSpace ws) {
+  constexpr int NW = NT / 64;
   const int b = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int n = held(c, b), seen = c.seen[b];
   float* weight = c.weight + (int64_t)b * c.cap;
   int* pos = c.pos + (int64_t)b * c.cap;
   int* src = a.src + (int64_t)b * a.budget;
-  for (int x = tid; x < a.budget; x += 1024) src[x] = x < n ? x : -1;
+  for (int x = tid; x < a.budget; x += NT) src[x] = x < n ? x : -1;
   if (n <= a.budget) {
     if (tid == 0) {
       ws.moves[b] = 0;
@@ -481,98 +566,134 @@ __global__ __launch_bounds__(1024) void evict_select(CacheArgs c, EvictArgs a, E
     }
     return;
   }
-  auto key_of = [&](int x) {
-    const int p = pos[x];
-    return keep_key(weight[x], p < a.sinks || seen - p <= a.recent);
+  __shared__ int bins[EVICT_BINS];
+  __shared__ int s_found[2], s_wave[2][NW];
+  // exclusive sum over the workgroup's threads (two values at once)
+  auto scan = [&](int u, int v, int* before_u, int* before_v, int* total_u, int* total_v) {
+    int iu = u, iv = v;
+    for (int o = 1; o < 64; o <<= 1) {
+      const int tu = __shfl_up(iu, o, 64), tv = __shfl_up(iv, o, 64);
+      if (lane >= o) {
+        iu += tu;
+        iv += tv;
+      }
+    }
+    __syncthreads();
+    if (lane == 63) {
+      s_wave[0][wave] = iu;
+      s_wave[1][wave] = iv;
+    }
+    __syncthreads();
+    int bu = 0, bv = 0, au = 0, av = 0;
+    for (int w = 0; w < NW; w++) {
+      const int tu = s_wave[0][w], tv = s_wave[1][w];
+      if (w < wave) {
+        bu += tu;
+        bv += tv;
+      }
+      au += tu;
+      av += tv;
+    }
+    *before_u = bu + iu - u;
+    *before_v = bv + iv - v;
+    *total_u = au;
+    *total_v = av;
   };
-  __shared__ int bins[256];
-  __shared__ int s_digit, s_want, s_w[16];
+  uint32_t key[E];
+  const int chunks = (n + NT * E - 1) / (NT * E);
+  auto load = [&](int ch) {
+#pragma unroll
+    for (int e = 0; e < E; e++) {
+      const int x = min((ch * NT + tid) * E + e, n - 1), p = pos[x];
+      key[e] = keep_key(weight[x], p < a.sinks || seen - p <= a.recent);
+    }
+  };
+  load(0);
   uint32_t prefix = 0;
   int want = a.budget;  // rank of the key searched, among those with the prefix
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    if (tid < 256) bins[tid] = 0;
+  constexpr int SHIFT[3] = {20, 10, 0};
+#pragma unroll
+  for (int round = 0; round < 3; round++) {
+    const int shift = SHIFT[round], nb = round ? 1024 : 4096;
+    const int per = nb / NT;  // bins per thread
+    for (int i = tid; i < nb; i += NT) bins[i] = 0;
     __syncthreads();
-    for (int x = tid; x < n; x += 1024) {
-      const uint32_t k = key_of(x);
-      if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8)))
-        atomicAdd(&bins[(k >> shift) & 255], 1);
+    for (int ch = 0; ch < chunks; ch++) {
+      if (chunks > 1 && (ch || round)) load(ch);
+#pragma unroll
+      for (int e = 0; e < E; e++)
+        if ((ch * NT + tid) * E + e < n &&
+            (round == 0 || key[e] >> (shift + 10) == prefix >> (shift + 10)))
+          atomicAdd(&bins[key[e] >> shift & (nb - 1)], 1);
     }
     __syncthreads();
-    if (tid == 0) {
-      int left = want, d = 255;
-      for (; d > 0 && left > bins[d]; d--) left -= bins[d];
-      s_digit = d;
-      s_want = left;
+    // thread t sums bins nb - 1 - t per .. down
+    int mine = 0;
+    for (int i = 0; i < per; i++) mine += bins[nb - 1 - tid * per - i];
+    int above, unused0, unused1, unused2;
+    scan(mine, 0, &above, &unused0, &unused1, &unused2);
+    if (above < want && above + mine >= want) {
+      int i = nb - 1 - tid * per, left = want - above;
+      for (; left > bins[i]; i--) left -= bins[i];
+      s_found[0] = i;
+      s_found[1] = left;
     }
     __syncthreads();
-    prefix |= (uint32_t)s_digit << shift;
-    want = s_want;
+    prefix |= (uint32_t)s_found[0] << shift;
+    want = s_found[1];
     __syncthreads();
   }
   // keys above `prefix` stay, and the first `want` equal to it
-  auto scan = [&](bool v, int& total) {  // count of set flags before this thread's
-    const uint64_t m = __ballot(v);
-    __syncthreads();
-    if (lane == 0) s_w[wave] = __popcll(m);
-    __syncthreads();
-    int before = 0;
-    total = 0;
-    for (int w = 0; w < 16; w++) {
-      if (w < wave) before += s_w[w];
-      total += s_w[w];
-    }
-    return before + (int)__popcll(m & ((1ull << lane) - 1));
-  };
   int ties = 0, holes = 0, late = 0;
   int2* mv = ws.move + (int64_t)b * ws.room;
-  for (int x0 = 0; x0 < n; x0 += 1024) {
-    const int x = x0 + tid;
-    const uint32_t k = x < n ? key_of(x) : 0u;
-    const bool tie = x < n && k == prefix;
-    int total;
-    const int rank = ties + scan(tie, total);
-    ties += total;
-    const bool keep = x < n && (k > prefix || (tie && rank < want));
-    const bool hole = x < n && x < a.budget && !keep, over = keep && x >= a.budget;
-    const int hi = holes + scan(hole, total);
-    holes += total;
-    if (hole) mv[hi].x = x;
-    const int li = late + scan(over, total);
-    late += total;
-    if (over) mv[li].y = x;
+  for (int ch = 0; ch < chunks; ch++) {
+    if (chunks > 1) load(ch);
+    const int x0 = (ch * NT + tid) * E;
+    int tie = 0;
+#pragma unroll
+    for (int e = 0; e < E; e++) tie += x0 + e < n && key[e] == prefix;
+    int rank, unused, more, unused2;
+    scan(tie, 0, &rank, &unused, &more, &unused2);
+    rank += ties;
+    ties += more;
+    uint64_t free = 0, over = 0;  // the thread's free slots, kept slots beyond the budget
+    static_assert(E <= 64, "one bit per slot");
+#pragma unroll
+    for (int e = 0; e < E; e++) {
+      if (x0 + e >= n) continue;
+      const bool eq = key[e] == prefix, keep = key[e] > prefix || (eq && rank < want);
+      rank += eq;
+      if (x0 + e < a.budget && !keep) free |= 1ull << e;
+      if (x0 + e >= a.budget && keep) over |= 1ull << e;
+    }
+    int hi, li, nh, nl;
+    scan(__popcll(free), __popcll(over), &hi, &li, &nh, &nl);
+    for (hi += holes; free; free &= free - 1) mv[hi++].x = x0 + __builtin_ctzll(free);
+    for (li += late; over; over &= over - 1) mv[li++].y = x0 + __builtin_ctzll(over);
+    holes += nh;
+    late += nl;
   }
   __syncthreads();
-  for (int i = tid; i < holes; i += 1024) {
+  for (int i = tid; i < holes; i += NT) {
     const int2 m = mv[i];
     weight[m.x] = weight[m.y];
     pos[m.x] = pos[m.y];
     src[m.x] = m.y;
   }
+  if (ws.room <= EVICT_FEW)
+    for (int i = wave; i < holes; i += NW) move_row<T>(c, b, mv[i], lane, 64);
   if (tid == 0) {
     ws.moves[b] = holes;
     c.len[b] = a.budget;
   }
 }
 
+// One wave per move.
 template <typename T>
 __global__ __launch_bounds__(256) void evict_move(CacheArgs c, EvictSpace ws) {
   const int b = blockIdx.x, n = ws.moves[b];
-  for (int i = blockIdx.y; i < n; i += gridDim.y) {
-    const int2 m = ws.move[(int64_t)b * ws.room + i];
-    const uint32_t pd = quot(m.x, c.page), ps = quot(m.y, c.page);
-    const int pgd = page_of(c, b, pd), pgs = page_of(c, b, ps);
-    if (pgd < 0 || pgs < 0) continue;
-    const int64_t rd = m.x - (int64_t)pd * c.page.d, rs = m.y - (int64_t)ps * c.page.d;
-    T* k = (T*)c.k;
-    T* v = (T*)c.v;
-    for (int t = threadIdx.x; t < c.Hkv * c.dh; t += 256) {
-      const int h = t / c.dh, d = t - h * c.dh;
-      k[pgd * c.k_page + rd * c.k_row + h * c.k_head + d] =
-          k[pgs * c.k_page + rs * c.k_row + h * c.k_head + d];
-      v[pgd * c.v_page + rd * c.v_row + h * c.v_head + d] =
-          v[pgs * c.v_page + rs * c.v_row + h * c.v_head + d];
-    }
-  }
+  for (int i = blockIdx.y * 4 + (threadIdx.x >> 6); i < n; i += gridDim.y * 4)
+    move_row<T>(c, b, ws.move[(int64_t)b * ws.room + i], threadIdx.x & 63, 64);
 }
 
 }  // namespace
@@ -583,8 +704,7 @@ hipError_t launch_cache_append(const CacheArgs& c, const AppendArgs& a, const in
   AppendSeqs sq;
   if (!cu_host) {
     sq.n = 0;
-    append_kernel<T><<<c.B, 256, 0, s>>>(c, a, sq);
-    append_lengths<<<(c.B + 255) / 256, 256, 0, s>>>(c, sq);
+    append_few<T, false><<<c.B, 256, 0, s>>>(c, a, sq);
     return hipGetLastError();
   }
   for (int f = 0; f < c.B; f += APPEND_SEQS) {
@@ -592,9 +712,15 @@ hipError_t launch_cache_append(const CacheArgs& c, const AppendArgs& a, const in
     sq.n = std::min(c.B - f, APPEND_SEQS);
     std::copy(cu_host + f, cu_host + f + sq.n + 1, sq.cu);
     const int rows = sq.cu[sq.n] - sq.cu[0];
+    int most = 0;
+    for (int i = 0; i < sq.n; i++) most = std::max(most, sq.cu[i + 1] - sq.cu[i]);
     if (rows == 0) continue;
-    append_kernel<T><<<rows, 256, 0, s>>>(c, a, sq);
-    append_lengths<<<(sq.n + 255) / 256, 256, 0, s>>>(c, sq);
+    if (most <= APPEND_FEW) {
+      append_few<T, true><<<sq.n, 256, 0, s>>>(c, a, sq);
+    } else {
+      append_many<T><<<(rows + 3) / 4, 256, 0, s>>>(c, a, sq);
+      append_lengths<<<(sq.n + 255) / 256, 256, 0, s>>>(c, sq);
+    }
     if (hipError_t e = hipGetLastError()) return e;
   }
   return hipSuccess;
@@ -673,10 +799,18 @@ template <typename T>
 hipError_t launch_cache_evict(const CacheArgs& c, const EvictArgs& a, hipStream_t s) {
   const EvictSpace ws{(int*)a.ws, (int2*)((char*)a.ws + round256((size_t)c.B * 4)),
                       evict_room(c, a.budget)};
-  evict_select<<<c.B, 1024, 0, s>>>(c, a, ws);
-  if (ws.room > 0) {
-    const int x = std::min(ws.room, std::max(1, 4096 / c.B));
-    evict_move<T><<<dim3(c.B, x), 256, 0, s>>>(c, ws);
+  if (c.cap <= 1024)
+    evict_select<T, 256, 4><<<c.B, 256, 0, s>>>(c, a, ws);
+  else if (c.cap <= 4096)
+    evict_select<T, 1024, 4><<<c.B, 1024, 0, s>>>(c, a, ws);
+  else if (c.cap <= 8192)
+    evict_select<T, 1024, 8><<<c.B, 1024, 0, s>>>(c, a, ws);
+  else
+    evict_select<T, 1024, 16><<<c.B, 1024, 0, s>>>(c, a, ws);
+  if (hipError_t e = hipGetLastError()) return e;
+  if (ws.room > EVICT_FEW) {
+    const int y = std::min((ws.room + 3) / 4, std::max(1, 4096 / c.B));
+    evict_move<T><<<dim3(c.B, y), 256, 0, s>>>(c, ws);
   }
   return hipGetLastError();
 }
