@@ -4,6 +4,7 @@
 #include "kernels.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace fusion {
 namespace {
@@ -139,6 +140,7 @@ __global__ __launch_bounds__(256) void append_lengths(CacheArgs c, AppendSeqs sq
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int PAGED_SPLIT = 1024;  // sequences up to which the work is split over their lengths
@@ -148,9 +150,9 @@ struct PagedSpace {
   int2* plan;    // [B]: first part, number of parts
   float2* ml;    // [parts][H]: maximum (base 2), sum
   float* o;      // [parts][H][DP]
-  float* score;  // [B][H][capv], base 2, by visible token
+  float* score;  // [B][tiles][H][KT], base 2, by visible token
   int ranges;    // parts per unit
-  int units, qtiles, capv;
+  int units, qtiles, tiles;
 };
 
 // The visible tokens of a sequence: x-th visible token -> slot.  In a cache
@@ -179,7 +181,7 @@ __device__ __forceinline__ Visible visible(const CacheArgs& c, const PagedArgs& 
   return v;
 }
 
-template <typename T, int DP, bool PAD, bool SPLIT>
+template <typename T, int DP, bool PAD, bool ACC>
 __global__ __launch_bounds__(256) void paged_attention(CacheArgs c, PagedArgs a, PagedSpace ws) {
   constexpr bool BF = sizeof(T) == 2;
   constexpr int KT = BF ? 32 : 16, NSUB = KT / 16;
@@ -199,7 +201,11 @@ __global__ __launch_bounds__(256) void paged_attention(CacheArgs c, PagedArgs a,
   const float sc2 = a.scale * kLog2e;
 
   auto segment = [&](int b, int ta, int tb, int part) {
-    const Visible vis = visible(c, a, b);
+    Visible vis = visible(c, a, b);
+    vis.nv = __builtin_amdgcn_readfirstlane(vis.nv);
+    vis.head = __builtin_amdgcn_readfirstlane(vis.head);
+    vis.gap = __builtin_amdgcn_readfirstlane(vis.gap);
+    vis.oldest = __builtin_amdgcn_readfirstlane(vis.by_pos ? vis.oldest : INT32_MIN);
     // Q^T operand
     uint4 q[NL];
 #pragma unroll
@@ -210,8 +216,10 @@ __global__ __launch_bounds__(256) void paged_attention(CacheArgs c, PagedArgs a,
         q[s] = *(const uint4*)((const T*)a.q + (int64_t)b * a.q_row + (int64_t)(h0 + cl) * a.q_head + d);
     }
     const int* table = c.table + (int64_t)b * c.max_pages;
-    const int* pos = c.pos + (int64_t)b * c.cap;
-    // page, place and visibility of the lane's tokens of a tile
+    // (positions that decide nothing are read from the table's line)
+    const int* pos = vis.oldest == INT32_MIN ? table : c.pos + (int64_t)b * c.cap;
+    const bool by_pos = vis.oldest != INT32_MIN;
+    // page, place and position of the lane's tokens of a tile
     int page[NSUB], place[NSUB], at[NSUB];
     auto look_up = [&](int t) {
 #pragma unroll
@@ -220,34 +228,42 @@ __global__ __launch_bounds__(256) void paged_attention(CacheArgs c, PagedArgs a,
         const uint32_t pg = quot((uint32_t)x, c.page);
         page[u] = table[pg];
         place[u] = x - (int)(pg * c.page.d);
-        at[u] = vis.by_pos ? pos[x] : 0;
+        at[u] = pos[by_pos ? (uint32_t)x : pg];
       }
     };
+    // keys and values of the lane's tokens; hidden ones read the cache's first row
     uint4 kr[NSUB][NL], vr[NSUB][NL];
-    uint32_t mask = 0, mask_next;  // visible tokens of the tile, one bit each
+    uint32_t mask_next;  // visible tokens of the tile, one bit each
     bool see[NSUB];
     auto load_kv = [&](int t) {
       mask_next = 0;
+      int64_t p[NSUB], r[NSUB];
 #pragma unroll
       for (int u = 0; u < NSUB; u++) {
-        see[u] = t * KT + 16 * u + cl < vis.nv && (unsigned)page[u] < (unsigned)c.pages &&
-                 (!vis.by_pos || at[u] >= vis.oldest || at[u] < a.sinks);
+        see[u] = (t * KT + 16 * u + cl < vis.nv) & ((unsigned)page[u] < (unsigned)c.pages) &
+                 ((at[u] >= vis.oldest) | (at[u] < a.sinks));
         mask_next |= (uint32_t)(__ballot(see[u]) & 0xFFFF) << (16 * u);
+        p[u] = see[u] ? page[u] : 0;
+        r[u] = see[u] ? place[u] : 0;
       }
-      if (mask_next == 0) return;
 #pragma unroll
       for (int u = 0; u < NSUB; u++) {
-        const int64_t p = see[u] ? page[u] : 0, r = see[u] ? place[u] : 0;
-        const T* k = (const T*)c.k + p * c.k_page + r * c.k_row + kh * c.k_head;
-        const T* v = (const T*)c.v + p * c.v_page + r * c.v_row + kh * c.v_head;
+        const T* k = (const T*)c.k + p[u] * c.k_page + r[u] * c.k_row + kh * c.k_head;
 #pragma unroll
         for (int s = 0; s < NL; s++) {
           const int d = (4 * s + g) * EPP;
-          kr[u][s] = vr[u][s] = make_uint4(0, 0, 0, 0);
-          if (!PAD || d < dh) {
-            kr[u][s] = *(const uint4*)(k + d);
-            vr[u][s] = *(const uint4*)(v + d);
-          }
+          kr[u][s] = make_uint4(0, 0, 0, 0);
+          if (!PAD || d < dh) kr[u][s] = *(const uint4*)(k + d);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < NSUB; u++) {
+        const T* v = (const T*)c.v + p[u] * c.v_page + r[u] * c.v_row + kh * c.v_head;
+#pragma unroll
+        for (int s = 0; s < NL; s++) {
+          const int d = (4 * s + g) * EPP;
+          vr[u][s] = make_uint4(0, 0, 0, 0);
+          if (!PAD || d < dh) vr[u][s] = *(const uint4*)(v + d);
         }
       }
     };
@@ -255,58 +271,65 @@ __global__ __launch_bounds__(256) void paged_attention(CacheArgs c, PagedArgs a,
     f32x4_t O[ND];
 #pragma unroll
     for (int d = 0; d < ND; d++) O[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    look_up(ta);
-    load_kv(ta);
-    if (ta + 1 < tb) look_up(ta + 1);
-    for (int t = ta; t < tb; t++) {
-      mask = mask_next;
+    // one tile, in straight line but for the rescaling, so that the waits for
+    // loads can be counted; LAST: no tile follows
+    auto tile = [&](int t, auto last_c) {
+      constexpr bool LAST = decltype(last_c)::value;
+      const uint32_t mask = mask_next;
       f32x4_t S[NSUB];
 #pragma unroll
-      for (int u = 0; u < NSUB; u++) S[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-      if (mask) {
+      for (int u = 0; u < NSUB; u++) {
+        S[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int u = 0; u < NSUB; u++) {
+        for (int s = 0; s < NL; s++) {
+          if constexpr (BF) {
+            S[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kr[u][s]),
+                                                           __builtin_bit_cast(bf16x8_t, q[s]),
+                                                           S[u], 0, 0, 0);
+          } else {
+            const f32x4_t kf = __builtin_bit_cast(f32x4_t, kr[u][s]);
+            const f32x4_t qf = __builtin_bit_cast(f32x4_t, q[s]);
 #pragma unroll
-          for (int s = 0; s < NL; s++) {
-            if constexpr (BF) {
-              S[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kr[u][s]),
-                                                             __builtin_bit_cast(bf16x8_t, q[s]),
-                                                             S[u], 0, 0, 0);
-            } else {
-              const f32x4_t kf = __builtin_bit_cast(f32x4_t, kr[u][s]);
-              const f32x4_t qf = __builtin_bit_cast(f32x4_t, q[s]);
-#pragma unroll
-              for (int i = 0; i < 4; i++)
-                S[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[i], qf[i], S[u], 0, 0, 0);
-            }
-          }
-#pragma unroll
-          for (int s = 0; s < NL; s++) {
-            const uint4 v = see[u] ? vr[u][s] : make_uint4(0, 0, 0, 0);
-            const int r = 16 * u + cl, p = 4 * s + g;
-            if constexpr (BF)
-              *(uint4*)(Vs + r * VROW + (((p >> 1) ^ (r & (DP / 16 - 1))) << 5) + ((p & 1) << 4)) = v;
-            else
-              *(uint4*)(Vs + r * VROW + p * 16) = v;
+            for (int i = 0; i < 4; i++)
+              S[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[i], qf[i], S[u], 0, 0, 0);
           }
         }
       }
+#pragma unroll
+      for (int u = 0; u < NSUB; u++)
+#pragma unroll
+        for (int s = 0; s < NL; s++) {
+          const uint4 x = vr[u][s];
+          const uint4 v = make_uint4(see[u] ? x.x : 0, see[u] ? x.y : 0, see[u] ? x.z : 0,
+                                     see[u] ? x.w : 0);
+          const int r = 16 * u + cl, p = 4 * s + g;
+          if constexpr (BF)
+            *(uint4*)(Vs + r * VROW + (((p >> 1) ^ (r & (DP / 16 - 1))) << 5) + ((p & 1) << 4)) = v;
+          else
+            *(uint4*)(Vs + r * VROW + p * 16) = v;
+        }
       __builtin_amdgcn_sched_barrier(0);
-      if (t + 1 < tb) load_kv(t + 1);
-      if (t + 2 < tb) look_up(t + 2);
+      if constexpr (!LAST) {
+        load_kv(t + 1);
+        look_up(min(t + 2, tb - 1));
+      }
       __builtin_amdgcn_sched_barrier(0);
-      if (mask == 0 && !a.accumulate) continue;
 #pragma unroll
       for (int u = 0; u < NSUB; u++)
 #pragma unroll
         for (int j = 0; j < 4; j++)
           S[u][j] = mask >> (16 * u + 4 * g + j) & 1 ? S[u][j] * sc2 : -INFINITY;
-      if (a.accumulate && cl < nq) {
-        float* sp = ws.score + ((int64_t)b * a.H + h0 + cl) * ws.capv + t * KT + 4 * g;
+      if constexpr (ACC) {
+        // rows past the unit's heads are past the buffer's end and dropped
+        // (a branch around the store would have the next tile's loads waited
+        // for together with it)
+        const auto rows = __builtin_amdgcn_make_buffer_rsrc(
+            ws.score + (((int64_t)b * ws.tiles + t) * a.H + h0) * KT, 0, nq * KT * 4, 0x00027000);
 #pragma unroll
-        for (int u = 0; u < NSUB; u++) *(f32x4_t*)(sp + 16 * u) = S[u];
+        for (int u = 0; u < NSUB; u++)
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, S[u]), rows,
+                                                 (cl * KT + 16 * u + 4 * g) * 4, 0, 0);
       }
-      if (mask == 0) continue;
       float mt = fmaxf(fmaxf(S[0][0], S[0][1]), fmaxf(S[0][2], S[0][3]));
       if (NSUB > 1)
         mt = fmaxf(mt, fmaxf(fmaxf(S[NSUB - 1][0], S[NSUB - 1][1]), fmaxf(S[NSUB - 1][2], S[NSUB - 1][3])));
@@ -355,7 +378,12 @@ __global__ __launch_bounds__(256) void paged_attention(CacheArgs c, PagedArgs a,
             O[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(
                 *(const float*)(Vs + (4 * g + j) * VROW + (16 * d + cl) * 4), S[0][j], O[d], 0, 0, 0);
       }
-    }
+    };
+    look_up(ta);
+    load_kv(ta);
+    look_up(min(ta + 1, tb - 1));
+    for (int t = ta; t < tb - 1; t++) tile(t, std::false_type{});
+    tile(tb - 1, std::true_type{});
     l = sum_xor32(sum_xor16(l));
     if (cl < nq) {
       const int64_t o = (int64_t)part * a.H + h0 + cl;
@@ -365,55 +393,57 @@ __global__ __launch_bounds__(256) void paged_attention(CacheArgs c, PagedArgs a,
     }
   };
 
-  auto tiles_of = [&](int b) {
-    if (b >= c.B) return 0;
-    return (visible(c, a, b).nv + KT - 1) / KT;
-  };
-  if constexpr (!SPLIT) {
-    const int t = __builtin_amdgcn_readfirstlane(tiles_of(range));
-    if (unit == 0 && lane == 0) ws.plan[range] = make_int2(range, t > 0);
-    if (t > 0) segment(range, 0, t, range);
-    return;
-  }
+  // the sequences whose tiles form the line: all, or the part's own
+  const bool split = c.B <= PAGED_SPLIT;
+  const int b0 = split ? 0 : range, b1 = split ? c.B : range + 1;
+  auto tiles_of = [&](int b) { return b < b1 ? (visible(c, a, b).nv + KT - 1) / KT : 0; };
   int total = 0;
-  for (int b = 0; b < c.B; b += 64) total += wave_sum_i(tiles_of(b + lane));
-  const int per = max(1, (total + ws.ranges - 1) / ws.ranges);
-  const int first = range * per, last = min(first + per, total);
-  const bool planner = unit == 0 && range == 0;
+  for (int b = b0; b < b1; b += 64)
+    total += __builtin_amdgcn_readfirstlane(wave_sum_i(tiles_of(b + lane)));
+  const int per = max(1, split ? (total + ws.ranges - 1) / ws.ranges : total);
+  const int first = split ? range * per : 0, last = min(first + per, total);
+  const bool planner = unit == 0 && (range == 0 || !split);
   if (first >= total && !planner) return;
   int before = 0;  // tiles of the sequences before b
-  for (int b = 0; b < c.B && (before < last || planner); b += 64) {
+  for (int b = b0; b < b1 && (before < last || planner); b += 64) {
     const int t = tiles_of(b + lane);
     int p = t;  // inclusive, then exclusive sum over the lanes
     for (int o = 1; o < 64; o <<= 1) {
       const int v = __shfl_up(p, o, 64);
       if (lane >= o) p += v;
     }
-    const int sum = __shfl(p, 63, 64);
+    const int sum = __builtin_amdgcn_readlane(p, 63);
     p += before - t;
     before += sum;
-    if (planner && b + lane < c.B)
+    if (planner && b + lane < b1)
       ws.plan[b + lane] = make_int2(p / per + b + lane, t > 0 ? (p + t - 1) / per - p / per + 1 : 0);
     for (uint64_t mine = __ballot(t > 0 && p < last && p + t > first); mine; mine &= mine - 1) {
       const int i = __builtin_ctzll(mine);
       const int tp = __builtin_amdgcn_readlane(p, i), tn = __builtin_amdgcn_readlane(t, i);
-      segment(b + i, max(first - tp, 0), min(last - tp, tn), range + b + i);
+      segment(b + i, max(first - tp, 0), min(last - tp, tn), split ? range + b + i : range);
     }
   }
 }
 
-// The parts of every sequence joined: workgroups 0 .. B H - 1 write an output
-// row each, the others add the weights of 1024 visible tokens of a sequence.
+// The parts of every sequence joined: the first workgroups write the output
+// rows, four each (4 waves a row), the others add the weights of 1024 visible
+// tokens of a sequence: 4 tokens a lane, a fourth of the heads a wave, summed
+// over the waves in order.  Loads go out JOIN_AHEAD at a time, since a
+// sequence of the chip alone has hundreds of parts (two of 131,072 tokens took
+// 37 us with one row of parts after the other).
 constexpr int JOIN_HEADS = 128;
-constexpr int JOIN_AHEAD = 8;  // loads under way per thread
-template <typename T>
-__global__ __launch_bounds__(256) void paged_join(CacheArgs c, PagedArgs a, PagedSpace ws, int DP,
-                                                  int chunks) {
+constexpr int JOIN_AHEAD = 8;
+template <typename T, int DP>
+__global__ __launch_bounds__(1024) void paged_join(CacheArgs c, PagedArgs a, PagedSpace ws,
+                                                   int rows, int chunks) {
+  constexpr int KT = sizeof(T) == 2 ? 32 : 16;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  __shared__ float part[4][128];
+  __shared__ __attribute__((aligned(16))) float part[16][256];
   __shared__ float2 s_ml[JOIN_HEADS];
-  if ((int64_t)blockIdx.x < (int64_t)c.B * a.H) {
-    const int b = blockIdx.x / a.H, h = blockIdx.x % a.H;
+  if (blockIdx.x < rows) {
+    const int64_t row = (int64_t)blockIdx.x * 4 + (wave >> 2);
+    const bool real = row < (int64_t)c.B * a.H;
+    const int b = real ? (int)(row / a.H) : 0, h = real ? (int)(row % a.H) : 0, w4 = wave & 3;
     const int2 plan = ws.plan[b];
     float m = -INFINITY;
     for (int i = lane; i < plan.y; i += 64)
@@ -421,86 +451,102 @@ __global__ __launch_bounds__(256) void paged_join(CacheArgs c, PagedArgs a, Page
     m = wave_max(m);
     const float mu = m == -INFINITY ? 0.f : m;
     float o0 = 0.f, o1 = 0.f, l = 0.f;
-    for (int i = wave; i < plan.y; i += 4) {
-      const int64_t p = (int64_t)(plan.x + i) * a.H + h;
-      const float2 ml = ws.ml[p];
-      const float f = __builtin_amdgcn_exp2f(ml.x - mu);
-      l += ml.y * f;
-      if (ml.x == -INFINITY) continue;
-      if (lane < DP) o0 = fmaf(ws.o[p * DP + lane], f, o0);
-      if (64 + lane < DP) o1 = fmaf(ws.o[p * DP + 64 + lane], f, o1);
+    for (int i = w4; i < plan.y; i += 4 * JOIN_AHEAD) {
+      float2 ml[JOIN_AHEAD];
+      float x0[JOIN_AHEAD], x1[JOIN_AHEAD];
+#pragma unroll
+      for (int u = 0; u < JOIN_AHEAD; u++) {
+        const int64_t p = (int64_t)(plan.x + min(i + 4 * u, plan.y - 1)) * a.H + h;
+        ml[u] = ws.ml[p];
+        x0[u] = ws.o[p * DP + lane];
+        x1[u] = DP > 64 ? ws.o[p * DP + 64 + lane] : 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < JOIN_AHEAD; u++) {
+        const float f = i + 4 * u < plan.y ? __builtin_amdgcn_exp2f(ml[u].x - mu) : 0.f;
+        l = fmaf(ml[u].y, f, l);
+        o0 = fmaf(x0[u], f, o0);
+        o1 = fmaf(x1[u], f, o1);
+      }
     }
     part[wave][lane] = o0;
-    part[wave][64 + lane] = o1;
+    if (DP > 64) part[wave][64 + lane] = o1;
     if (lane == 0) s_ml[wave].y = l;
     __syncthreads();
-    l = (s_ml[0].y + s_ml[1].y) + (s_ml[2].y + s_ml[3].y);
-    if (tid < c.dh) {
-      const float o = (part[0][tid] + part[1][tid]) + (part[2][tid] + part[3][tid]);
-      ((T*)a.out)[((int64_t)b * a.H + h) * c.dh + tid] = St<T>::put(l == 0.f ? 0.f : o / l);
+    const int d = tid & 255, w = wave & ~3;  // a row's first wave
+    l = (s_ml[w].y + s_ml[w + 1].y) + (s_ml[w + 2].y + s_ml[w + 3].y);
+    if (real && d < c.dh) {
+      const float o = (part[w][d] + part[w + 1][d]) + (part[w + 2][d] + part[w + 3][d]);
+      ((T*)a.out)[row * c.dh + d] = St<T>::put(l == 0.f ? 0.f : o / l);
     }
     return;
   }
-  const int64_t id = blockIdx.x - (int64_t)c.B * a.H;
+  const int64_t id = (int64_t)blockIdx.x - rows;
   const int b = (int)(id / chunks), first = (int)(id % chunks) * 1024;
   const Visible vis = visible(c, a, b);
+  if (first >= vis.nv) return;
   const int2 plan = ws.plan[b];
-  for (int x0 = first; x0 < vis.nv; x0 += chunks * 1024) {
-    const int x = x0 + tid * 4;
-    f32x4_t w = {0.f, 0.f, 0.f, 0.f};
-    for (int hc = 0; hc < a.H; hc += JOIN_HEADS) {
-      const int nh = min(JOIN_HEADS, a.H - hc);
-      __syncthreads();
-      // maximum and 1 / (sum H) of the heads, 16 lanes a head
-      for (int h = tid >> 4; h < nh; h += 16) {
-        float m = -INFINITY, l = 0.f;
-        for (int i = tid & 15; i < plan.y; i += 16 * JOIN_AHEAD) {
-          float2 ml[JOIN_AHEAD];
-          float m2 = m;
+  for (int hc = 0; hc < a.H; hc += JOIN_HEADS) {
+    const int nh = min(JOIN_HEADS, a.H - hc);
+    __syncthreads();
+    // maximum and 1 / (sum H) of the heads, 32 lanes a head
+    for (int h = tid >> 5; h < nh; h += 32) {
+      float m = -INFINITY, l = 0.f;
+      for (int i = tid & 31; i < plan.y; i += 32 * JOIN_AHEAD) {
+        float2 ml[JOIN_AHEAD];
+        float m2 = m;
 #pragma unroll
-          for (int u = 0; u < JOIN_AHEAD; u++) {
-            ml[u] = ws.ml[(int64_t)(plan.x + min(i + 16 * u, plan.y - 1)) * a.H + hc + h];
-            if (i + 16 * u >= plan.y) ml[u].x = -INFINITY;
-          }
-#pragma unroll
-          for (int u = 0; u < JOIN_AHEAD; u++) m2 = fmaxf(m2, ml[u].x);
-          if (m2 != -INFINITY) {
-            l *= __builtin_amdgcn_exp2f(m - m2);
-#pragma unroll
-            for (int u = 0; u < JOIN_AHEAD; u++) l += ml[u].y * __builtin_amdgcn_exp2f(ml[u].x - m2);
-          }
-          m = m2;
+        for (int u = 0; u < JOIN_AHEAD; u++) {
+          ml[u] = ws.ml[(int64_t)(plan.x + min(i + 32 * u, plan.y - 1)) * a.H + hc + h];
+          if (i + 32 * u >= plan.y) ml[u].x = -INFINITY;
         }
-        for (int o = 8; o; o >>= 1) {
-          const float mo = __shfl_xor(m, o, 16), lo = __shfl_xor(l, o, 16), m2 = fmaxf(m, mo);
-          if (m2 != -INFINITY)
-            l = l * __builtin_amdgcn_exp2f(m - m2) + lo * __builtin_amdgcn_exp2f(mo - m2);
-          m = m2;
+#pragma unroll
+        for (int u = 0; u < JOIN_AHEAD; u++) m2 = fmaxf(m2, ml[u].x);
+        if (m2 != -INFINITY) {
+          l *= __builtin_amdgcn_exp2f(m - m2);
+#pragma unroll
+          for (int u = 0; u < JOIN_AHEAD; u++) l = fmaf(ml[u].y, __builtin_amdgcn_exp2f(ml[u].x - m2), l);
         }
-        if ((tid & 15) == 0)
-          s_ml[h] = make_float2(m == -INFINITY ? 0.f : m, l == 0.f ? 0.f : 1.f / (l * (float)a.H));
+        m = m2;
       }
-      __syncthreads();
+      for (int o = 16; o; o >>= 1) {
+        const float mo = __shfl_xor(m, o, 32), lo = __shfl_xor(l, o, 32), m2 = fmaxf(m, mo);
+        if (m2 != -INFINITY)
+          l = l * __builtin_amdgcn_exp2f(m - m2) + lo * __builtin_amdgcn_exp2f(mo - m2);
+        m = m2;
+      }
+      if ((tid & 31) == 0)
+        s_ml[h] = make_float2(m == -INFINITY ? 0.f : m, l == 0.f ? 0.f : 1.f / (l * (float)a.H));
+    }
+    __syncthreads();
+    for (int x0 = first; x0 < vis.nv; x0 += chunks * 1024) {
+      const int x = x0 + (wave & 3) * 256 + lane * 4, h0 = wave >> 2;
+      f32x4_t w = {0.f, 0.f, 0.f, 0.f};
       if (x < vis.nv) {
-        const float* sp = ws.score + ((int64_t)b * a.H + hc) * ws.capv + x;
-        for (int h = 0; h < nh; h += JOIN_AHEAD) {
+        const float* sp = ws.score + (((int64_t)b * ws.tiles + x / KT) * a.H + hc) * KT + x % KT;
+        for (int h = h0; h < nh; h += 4 * JOIN_AHEAD) {
           f32x4_t s[JOIN_AHEAD];
 #pragma unroll
-          for (int u = 0; u < JOIN_AHEAD; u++)
-            s[u] = *(const f32x4_t*)(sp + (int64_t)min(h + u, nh - 1) * ws.capv);
+          for (int u = 0; u < JOIN_AHEAD; u++) s[u] = *(const f32x4_t*)(sp + min(h + 4 * u, nh - 1) * KT);
 #pragma unroll
           for (int u = 0; u < JOIN_AHEAD; u++) {
-            const float2 ml = s_ml[min(h + u, nh - 1)];
-            const float r = h + u < nh ? ml.y : 0.f;
+            const float2 ml = s_ml[min(h + 4 * u, nh - 1)];
+            const float r = h + 4 * u < nh ? ml.y : 0.f;
 #pragma unroll
             for (int j = 0; j < 4; j++) w[j] = fmaf(__builtin_amdgcn_exp2f(s[u][j] - ml.x), r, w[j]);
           }
         }
       }
+      *(f32x4_t*)&part[wave][lane * 4] = w;
+      __syncthreads();
+      const int xt = x0 + tid;
+      if (xt < vis.nv) {
+        const int t = tid >> 8, i = tid & 255;
+        c.weight[(int64_t)b * c.cap + vis.slot(xt)] +=
+            (part[t][i] + part[4 + t][i]) + (part[8 + t][i] + part[12 + t][i]);
+      }
+      __syncthreads();
     }
-#pragma unroll
-    for (int j = 0; j < 4; j++)
-      if (x + j < vis.nv) c.weight[(int64_t)b * c.cap + vis.slot(x + j)] += w[j];
   }
 }
 
@@ -732,14 +778,15 @@ template hipError_t launch_cache_append<bf16_t>(const CacheArgs&, const AppendAr
 
 namespace {
 // Layout of the workspace; `space` null: its size alone.
-size_t paged_space(const CacheArgs& c, int H, int accumulate, char* ws, PagedSpace* space) {
+size_t paged_space(const CacheArgs& c, int KT, int H, int accumulate, char* ws,
+                   PagedSpace* space) {
   PagedSpace p;
   const int group = H / c.Hkv, DP = c.dh <= 64 ? 64 : 128;
   p.qtiles = (group + 15) / 16;
   p.units = c.Hkv * p.qtiles;
   const bool split = c.B <= PAGED_SPLIT;
   p.ranges = split ? std::max(1, PAGED_WAVES / p.units) : c.B;
-  p.capv = (c.cap + 31) / 32 * 32;
+  p.tiles = (c.cap + KT - 1) / KT;
   const size_t parts = (size_t)p.ranges + (split ? c.B : 0);
   size_t n = 0;
   auto take = [&](size_t bytes) {
@@ -750,7 +797,7 @@ size_t paged_space(const CacheArgs& c, int H, int accumulate, char* ws, PagedSpa
   p.plan = (int2*)take((size_t)c.B * 8);
   p.ml = (float2*)take(parts * H * 8);
   p.o = (float*)take(parts * H * DP * 4);
-  p.score = (float*)take(accumulate ? (size_t)c.B * H * p.capv * 4 : 0);
+  p.score = (float*)take(accumulate ? (size_t)c.B * p.tiles * H * KT * 4 : 0);
   if (space) *space = p;
   return n;
 }
@@ -759,27 +806,28 @@ template <typename T, int DP, bool PAD>
 hipError_t launch_paged(const CacheArgs& c, const PagedArgs& a, const PagedSpace& ws,
                         hipStream_t s) {
   const unsigned grid = (unsigned)(((int64_t)ws.units * ws.ranges + 3) / 4);
-  if (c.B <= PAGED_SPLIT)
+  if (a.accumulate)
     paged_attention<T, DP, PAD, true><<<grid, 256, 0, s>>>(c, a, ws);
   else
     paged_attention<T, DP, PAD, false><<<grid, 256, 0, s>>>(c, a, ws);
   if (hipError_t e = hipGetLastError()) return e;
   // (workgroups past a sequence's tokens leave at once)
+  const int rows = (int)(((int64_t)c.B * a.H + 3) / 4);
   const int chunks = a.accumulate ? std::max(1, std::min((c.cap + 1023) / 1024, 16384 / c.B)) : 0;
-  const unsigned join = (unsigned)((int64_t)c.B * a.H + (int64_t)c.B * chunks);
-  paged_join<T><<<join, 256, 0, s>>>(c, a, ws, DP, chunks);
+  paged_join<T, DP><<<(unsigned)(rows + (int64_t)c.B * chunks), 1024, 0, s>>>(c, a, ws, rows, chunks);
   return hipGetLastError();
 }
+constexpr int tile_tokens(size_t size) { return size == 2 ? 32 : 16; }
 }  // namespace
 
-size_t paged_workspace_bytes(const CacheArgs& c, int H, int accumulate) {
-  return paged_space(c, H, accumulate, nullptr, nullptr);
+size_t paged_workspace_bytes(const CacheArgs& c, size_t elem, int H, int accumulate) {
+  return paged_space(c, tile_tokens(elem), H, accumulate, nullptr, nullptr);
 }
 
 template <typename T>
 hipError_t launch_paged_attention(const CacheArgs& c, const PagedArgs& a, hipStream_t s) {
   PagedSpace ws;
-  paged_space(c, a.H, a.accumulate, (char*)a.ws, &ws);
+  paged_space(c, tile_tokens(sizeof(T)), a.H, a.accumulate, (char*)a.ws, &ws);
   if (c.dh == 64) return launch_paged<T, 64, false>(c, a, ws, s);
   if (c.dh < 64) return launch_paged<T, 64, true>(c, a, ws, s);
   if (c.dh == 128) return launch_paged<T, 128, false>(c, a, ws, s);

@@ -321,6 +321,8 @@ int check_strides(int precision, const int64_t* strides, int n) {
   return FUSION_OK;
 }
 
+size_t elem_bytes(int precision) { return precision == 1 ? 2 : 4; }
+
 int check_cache(const fusion_cache* c, CacheArgs* a) {
   if (!c) return bad("cache is null");
   if (int rc = check_heads(c->precision, c->kv_heads, c->kv_heads, c->dh)) return rc;
@@ -574,7 +576,7 @@ FUSION_API size_t fusion_paged_attention_workspace_bytes(const fusion_cache* c, 
                                                          int accumulate) {
   CacheArgs ca;
   if (check_cache(c, &ca) || check_heads(c->precision, heads, c->kv_heads, c->dh)) return 0;
-  return paged_workspace_bytes(ca, heads, accumulate);
+  return paged_workspace_bytes(ca, elem_bytes(c->precision), heads, accumulate);
 }
 
 FUSION_API int fusion_paged_attention(const fusion_cache* c, const void* q, const int64_t* strides,
@@ -588,7 +590,9 @@ FUSION_API int fusion_paged_attention(const fusion_cache* c, const void* q, cons
   if (!q || !strides || !out) return bad("null buffer");
   if (int rc = check_strides(c->precision, strides, 2)) return rc;
   if (((uintptr_t)q | (uintptr_t)out) % 16) return bad("buffers must be 16-byte aligned");
-  if (int rc = check_space(ws, ws_bytes, paged_workspace_bytes(ca, heads, accumulate))) return rc;
+  if (int rc = check_space(ws, ws_bytes, paged_workspace_bytes(ca, elem_bytes(c->precision), heads,
+                                                               accumulate)))
+    return rc;
   PagedArgs a{};
   a.q = q; a.q_row = strides[0]; a.q_head = strides[1]; a.out = out;
   a.H = heads; a.group = heads / c->kv_heads;

@@ -241,7 +241,7 @@ struct PagedArgs {
   float scale;
   void* ws;
 };
-size_t paged_workspace_bytes(const CacheArgs& c, int H, int accumulate);
+size_t paged_workspace_bytes(const CacheArgs& c, size_t elem, int H, int accumulate);
 template <typename T>
 hipError_t launch_paged_attention(const CacheArgs& c, const PagedArgs& a, hipStream_t s);
 
