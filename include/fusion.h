@@ -404,8 +404,8 @@ FUSION_API int fusion_test_topk_compact_ws(const fusion_ragged* in, const float*
  * A row that sees nothing gets zeros; a value of a row that a query does not
  * see has no influence on its output, whatever it is.
  * q: device [M][heads][dh], k, v: device [M][kv_heads][dh]; strides: HOST
- * int64 [6], row and head strides of q, k and v (row strides of k and v
- * below 2^24); out: device
+ * int64 [6], row and head strides of q, k and v (row strides of k and v at
+ * most 2^23); out: device
  * [M][heads][dh], contiguous, apart from the inputs.  M = cu[batch].
  * Errors: FUSION_E_INVALID_ARG, FUSION_E_HIP. */
 FUSION_API int fusion_window_attention(int precision, const void* q, const void* k, const void* v,

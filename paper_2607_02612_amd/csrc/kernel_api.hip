@@ -538,8 +538,8 @@ FUSION_API int fusion_window_attention(int precision, const void* q, const void*
   if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)out) % 16)
     return bad("buffers must be 16-byte aligned");
   // (a tile's rows are addressed by 32-bit byte offsets from its first)
-  if (strides[2] >= (1 << 24) || strides[4] >= (1 << 24))
-    return bad("row strides of k and v must be below 2^24");
+  if (strides[2] > (1 << 23) || strides[4] > (1 << 23))
+    return bad("row strides of k and v must be at most 2^23");
   WindowArgs a{};
   a.q = q; a.k = k; a.v = v; a.size = size; a.out = out;
   a.q_row = strides[0]; a.q_head = strides[1]; a.k_row = strides[2]; a.k_head = strides[3];

@@ -19,65 +19,6 @@ struct WindowSeqs {
   int tile[WIN_SEQS + 1];
 };
 
-// One wave per query row and head, one key per lane.
-constexpr int WIN_ROWS = 4;  // rows per workgroup
-template <typename T>
-__global__ __launch_bounds__(256) void window_attention_valu(WindowArgs a, WindowSeqs sq) {
-  const int tile = blockIdx.x, h = blockIdx.y;
-  int lo = 0, hi = sq.n - 1;  // the last sample whose first tile is not after this one
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (sq.tile[mid] <= tile) lo = mid; else hi = mid - 1;
-  }
-  const int base = sq.cu[lo], n = sq.cu[lo + 1] - base;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int i = (tile - sq.tile[lo]) * WIN_ROWS + wave;
-  if (i >= n) return;
-  const int dh = a.dh, kh = h / a.group;
-  __shared__ float qs[WIN_ROWS][128];
-  const T* q = (const T*)a.q + (base + i) * a.q_row + h * a.q_head;
-  for (int d = lane; d < dh; d += 64) qs[wave][d] = St<T>::get(q[d]) * a.scale;
-  const T* kg = (const T*)a.k + base * a.k_row + kh * a.k_head;
-  const T* vg = (const T*)a.v + base * a.v_row + kh * a.v_head;
-  float m = -INFINITY, l = 0.f, o0 = 0.f, o1 = 0.f;
-  for (int j0 = 0; j0 < n; j0 += 64) {
-    const int j = j0 + lane;
-    float s = -INFINITY;
-    bool see = j < n && (i - j < a.window && j - i < a.window || j < a.sinks);
-    if (a.causal && j > i) see = false;
-    float lnsize = 0.f;
-    if (see && a.size) {
-      const float sz = a.size[base + j];
-      see = sz > 0.f;
-      lnsize = logf(sz);
-    }
-    if (see) {
-      float dot = 0.f;
-      for (int d = 0; d < dh; d++) dot = fmaf(qs[wave][d], St<T>::get(kg[j * a.k_row + d]), dot);
-      s = dot + lnsize;
-    }
-    const uint64_t seen = __ballot(see);
-    if (!seen) continue;
-    const float m2 = fmaxf(m, wave_max(s));
-    const float e = see ? expf(s - m2) : 0.f, f = m == -INFINITY ? 0.f : expf(m - m2);
-    l = l * f + wave_sum(e);
-    o0 *= f;
-    o1 *= f;
-    m = m2;
-    for (uint64_t left = seen; left; left &= left - 1) {
-      const int t = __builtin_ctzll(left);
-      const float p = __shfl(e, t, 64);
-      const T* v = vg + (j0 + t) * a.v_row;
-      if (lane < dh) o0 = fmaf(p, St<T>::get(v[lane]), o0);
-      if (64 + lane < dh) o1 = fmaf(p, St<T>::get(v[64 + lane]), o1);
-    }
-  }
-  T* out = (T*)a.out + ((int64_t)(base + i) * a.H + h) * dh;
-  const float r = l == 0.f ? 0.f : 1.f / l;
-  if (lane < dh) out[lane] = St<T>::put(o0 * r);
-  if (64 + lane < dh) out[64 + lane] = St<T>::put(o1 * r);
-}
-
 // ------------------------------------------------------------ bf16 MFMA --
 // A workgroup of 4 waves takes 32 query rows per wave: of the heads that
 // share a key head as many as divide 4 at the same rows, else consecutive
@@ -409,6 +350,200 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma(WindowArgs 
   }
 }
 
+// ------------------------------------------------------------ fp32 MFMA --
+// The same plan with v_mfma_f32_16x16x4_f32, 16 query rows per wave, bound by
+// the fp32 matrix rate.  Lane (g, c) = (lane / 16, lane % 16) holds query c
+// against keys 16 t + 4 g + j, and these registers are the operand of
+// O^T = V^T P^T as they stand (slot g of step j is key 16 t + 4 g + j).  A
+// 16-byte piece of a key feeds four steps (slot g of step i is dim
+// 16 u + 4 g + i).  Tiles are 16 KB of keys and as much of values; K's pieces
+// are XOR-permuted by the row mod 16, V's groups of four pieces by row / 4
+// mod 4, so that the 16-byte key reads of 16 rows and the 4-byte value reads
+// of 4 x 16 spread over all banks.
+template <int DP, bool PAD, bool SIZES>
+__global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowArgs a, WindowSeqs sq,
+                                                                         int tiles, int hshift) {
+  constexpr int PPR = DP / 4, RPC = 64 / PPR;  // pieces per row, rows per copy
+  constexpr int TILEB = 16384, ROWB = DP * 4, KT = TILEB / ROWB;
+  constexpr int NC = KT / RPC / WNW, NT = KT / 16, NU = DP / 16;
+  __shared__ __attribute__((aligned(16))) char smem[4 * TILEB];  // [stage][K, V]
+  __shared__ float lnS[2][KT];
+  __shared__ int s_bad;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int g = lane >> 4, c = lane & 15;
+  const int per_group = a.group >> hshift, units = a.H >> hshift;
+  const int unit = blockIdx.x % units, kh = unit / per_group;
+  const int h = unit % per_group * (1 << hshift) + kh * a.group + (wave & ((1 << hshift) - 1));
+  const WindowPlan pl = window_plan(a, sq, tiles - 1 - blockIdx.x / units, 16 * (WNW >> hshift), KT);
+  const int n = pl.n, dh = a.dh;
+  const int w0 = pl.q0 + 16 * (wave >> hshift), w1 = min(w0 + 15, n - 1);
+  const float* kg = (const float*)a.k + (int64_t)pl.base * a.k_row + (int64_t)kh * a.k_head;
+  const float* vg = (const float*)a.v + (int64_t)pl.base * a.v_row + (int64_t)kh * a.v_head;
+  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
+  if (tid == 0) s_bad = -1;
+
+  auto copy_tile = [&](int t, int st) {
+    const int k0 = t * KT, lim = n - 1 - k0;
+    const float* kt = kg + (int64_t)k0 * a.k_row;
+    const float* vt = vg + (int64_t)k0 * a.v_row;
+#pragma unroll
+    for (int u = 0; u < NC; u++) {
+      const int r = (wave * NC + u) * RPC + lane / PPR, rr = min(r, lim), p = lane % PPR;
+      const int pk = p ^ (r & 15), pv = p ^ ((r >> 2 & 3) << 2);
+      const unsigned dst = lds0 + st * 2 * TILEB + (wave * NC + u) * 1024;
+      const unsigned ko = (unsigned)rr * (unsigned)a.k_row * 4 + pk * 16;
+      const unsigned vo = (unsigned)rr * (unsigned)a.v_row * 4 + pv * 16;
+      if (PAD) {
+        copy16(pk * 4 < dh ? (const void*)((const char*)kt + ko) : (const void*)&kZeros, dst);
+        copy16(pv * 4 < dh ? (const void*)((const char*)vt + vo) : (const void*)&kZeros,
+               dst + TILEB);
+      } else {
+        copy16(kt, ko, dst);
+        copy16(vt, vo, dst + TILEB);
+      }
+    }
+  };
+  float size_next = 0.f;
+  auto load_size = [&](int t) {
+    if (SIZES && tid < KT) size_next = a.size[pl.base + min(t * KT + tid, n - 1)];
+  };
+  auto put_size = [&](int st) {
+    if (SIZES && tid < KT) lnS[st][tid] = size_next > 0.f ? logf(size_next) * kLog2e : -INFINITY;
+  };
+  copy_tile(pl.tile(0), 0);
+  load_size(pl.tile(0));
+
+  f32x4_t qf[NU];
+  {
+    const float* qr = (const float*)a.q + (int64_t)(pl.base + min(w0 + c, n - 1)) * a.q_row +
+                      (int64_t)h * a.q_head;
+#pragma unroll
+    for (int u = 0; u < NU; u++) {
+      qf[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      if (!PAD || 16 * u + 4 * g < dh) qf[u] = *(const f32x4_t*)(qr + 16 * u + 4 * g);
+    }
+  }
+  put_size(0);
+  const float sc2 = a.scale * kLog2e;
+  float m = -INFINITY, l = 0.f;
+  f32x4_t O[NU];
+#pragma unroll
+  for (int d = 0; d < NU; d++) O[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
+  for (int it = 0; it < pl.nt; it++) {
+    const int st = it & 1, t = pl.tile(it), k0 = t * KT;
+    wait_copies();
+    __syncthreads();
+    if (it + 1 < pl.nt) {
+      copy_tile(pl.tile(it + 1), st ^ 1);
+      load_size(pl.tile(it + 1));
+    }
+    const char* Ks = smem + st * 2 * TILEB;
+    char* Vs = smem + st * 2 * TILEB + TILEB;
+    bool bad = false;
+    if (SIZES || k0 + KT > n || !all_see(a, pl.q0, pl.q1, k0, k0 + KT - 1)) {
+      bool any = false;
+#pragma unroll
+      for (int u = 0; u < TILEB / (64 * WNW * 16); u++) {
+        const f32x4_t v = *(const f32x4_t*)(Vs + (tid + u * 64 * WNW) * 16);
+        any |= !(fabsf(v[0]) < INFINITY) | !(fabsf(v[1]) < INFINITY) | !(fabsf(v[2]) < INFINITY) |
+               !(fabsf(v[3]) < INFINITY);
+      }
+      if (any) s_bad = it;
+      __syncthreads();
+      bad = s_bad == it;
+    }
+    const bool active = w0 < n && !none_see(a, w0, w1, k0, k0 + KT - 1);
+    if (bad) {
+      for (int u = tid; u < TILEB / 4; u += 64 * WNW) {
+        float* v = (float*)Vs + u;
+        if (!(fabsf(*v) < INFINITY)) *v = 0.f;
+      }
+      __syncthreads();
+      for (int j = k0; active && j < min(n, k0 + KT); j++) {
+        const bool see = w0 + c < n && sees(a, w0 + c, j) && !(SIZES && !(a.size[pl.base + j] > 0.f));
+        if (!see) continue;
+        const float* v = vg + (int64_t)j * a.v_row + 4 * g;
+#pragma unroll
+        for (int d = 0; d < NU; d++) {
+          if (PAD && 16 * d + 4 * g >= dh) break;
+          const f32x4_t x = *(const f32x4_t*)(v + 16 * d);
+#pragma unroll
+          for (int q = 0; q < 4; q++) O[d][q] += fabsf(x[q]) < INFINITY ? 0.f : x[q];
+        }
+      }
+    }
+    if (active) {
+      f32x4_t S[NT];
+#pragma unroll
+      for (int x = 0; x < NT; x++) S[x] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int u = 0; u < NU; u++) {
+        f32x4_t kf[NT];
+#pragma unroll
+        for (int x = 0; x < NT; x++)
+          kf[x] = *(const f32x4_t*)(Ks + (16 * x + c) * ROWB + (((4 * u + g) ^ c) << 4));
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+#pragma unroll
+          for (int x = 0; x < NT; x++)
+            S[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[x][i], qf[u][i], S[x], 0, 0, 0);
+      }
+      const bool edge = k0 + KT > n || !all_see(a, w0, w1, k0, k0 + KT - 1);
+      float mt = -INFINITY;
+#pragma unroll
+      for (int x = 0; x < NT; x++) {
+        f32x4_t ln = {0.f, 0.f, 0.f, 0.f};
+        if (SIZES) ln = *(const f32x4_t*)(&lnS[st][16 * x + 4 * g]);
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+          const int key = k0 + 16 * x + 4 * g + j;
+          const bool see = (!edge || (key < n && sees(a, w0 + c, key))) && !(SIZES && ln[j] == -INFINITY);
+          S[x][j] = see ? fmaf(S[x][j], sc2, ln[j]) : -INFINITY;
+          mt = fmaxf(mt, S[x][j]);
+        }
+      }
+      mt = max_xor32(max_xor16(mt));
+      const bool grow = mt > m + 8.f;
+      if (__any(grow)) {
+        const float f = grow ? __builtin_amdgcn_exp2f(m - mt) : 1.f;
+        if (grow) m = mt;
+        l *= f;
+#pragma unroll
+        for (int d = 0; d < NU; d++)
+#pragma unroll
+          for (int j = 0; j < 4; j++) O[d][j] *= f;
+      }
+      const float mu = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int x = 0; x < NT; x++) {
+#pragma unroll
+        for (int j = 0; j < 4; j++) S[x][j] = __builtin_amdgcn_exp2f(S[x][j] - mu);
+        l += (S[x][0] + S[x][1]) + (S[x][2] + S[x][3]);
+      }
+#pragma unroll
+      for (int x = 0; x < NT; x++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+          const char* vr = Vs + (16 * x + 4 * g + j) * ROWB + (c & 3) * 4;
+#pragma unroll
+          for (int d = 0; d < NU; d++)
+            O[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                *(const float*)(vr + (((4 * d + (c >> 2)) ^ (g << 2)) << 4)), S[x][j], O[d], 0, 0, 0);
+        }
+    }
+    if (it + 1 < pl.nt) put_size(st ^ 1);
+  }
+  l = sum_xor32(sum_xor16(l));
+  if (w0 + c < n) {
+    const float r = l == 0.f ? 0.f : 1.f / l;
+    float* out = (float*)a.out + ((int64_t)(pl.base + w0 + c) * a.H + h) * dh + 4 * g;
+#pragma unroll
+    for (int d = 0; d < NU; d++)
+      if (!PAD || 16 * d + 4 * g < dh) *(f32x4_t*)(out + 16 * d) = O[d] * r;
+  }
+}
+
 // Runs `launch(samples, tiles)` for all samples, as many at once as the
 // arguments of a launch hold, with tiles of `rows` rows.
 template <typename F>
@@ -429,16 +564,24 @@ hipError_t for_samples(const int32_t* cu_host, int batch, int rows, F launch) {
   return hipSuccess;
 }
 
-template <int DP, bool PAD>
+template <typename T, int DP, bool PAD>
 hipError_t launch_mfma(const WindowArgs& a, const int32_t* cu_host, int batch, hipStream_t s) {
   // heads of a group per workgroup, 1 << hshift
   const int hshift = a.group % 4 == 0 ? 2 : a.group % 2 == 0 ? 1 : 0;
-  return for_samples(cu_host, batch, 32 * (WNW >> hshift), [&](const WindowSeqs& sq, int tiles) {
+  const int rows = (sizeof(T) == 2 ? 32 : 16) * (WNW >> hshift);
+  return for_samples(cu_host, batch, rows, [&](const WindowSeqs& sq, int tiles) {
     const dim3 grid((unsigned)tiles * (a.H >> hshift));
-    if (a.size)
-      window_attention_mfma<DP, PAD, true><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
-    else
-      window_attention_mfma<DP, PAD, false><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
+    if constexpr (sizeof(T) == 2) {
+      if (a.size)
+        window_attention_mfma<DP, PAD, true><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
+      else
+        window_attention_mfma<DP, PAD, false><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
+    } else {
+      if (a.size)
+        window_attention_mfma_f32<DP, PAD, true><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
+      else
+        window_attention_mfma_f32<DP, PAD, false><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
+    }
   });
 }
 
@@ -447,15 +590,10 @@ hipError_t launch_mfma(const WindowArgs& a, const int32_t* cu_host, int batch, h
 template <typename T>
 hipError_t launch_window_attention(const WindowArgs& a, const int32_t* cu_host, int batch,
                                    hipStream_t s) {
-  if (sizeof(T) == 2) {
-    if (a.dh == 64) return launch_mfma<64, false>(a, cu_host, batch, s);
-    if (a.dh < 64) return launch_mfma<64, true>(a, cu_host, batch, s);
-    if (a.dh == 128) return launch_mfma<128, false>(a, cu_host, batch, s);
-    return launch_mfma<128, true>(a, cu_host, batch, s);
-  }
-  return for_samples(cu_host, batch, WIN_ROWS, [&](const WindowSeqs& sq, int tiles) {
-    window_attention_valu<T><<<dim3(tiles, a.H), 256, 0, s>>>(a, sq);
-  });
+  if (a.dh == 64) return launch_mfma<T, 64, false>(a, cu_host, batch, s);
+  if (a.dh < 64) return launch_mfma<T, 64, true>(a, cu_host, batch, s);
+  if (a.dh == 128) return launch_mfma<T, 128, false>(a, cu_host, batch, s);
+  return launch_mfma<T, 128, true>(a, cu_host, batch, s);
 }
 template hipError_t launch_window_attention<float>(const WindowArgs&, const int32_t*, int,
                                                    hipStream_t);
