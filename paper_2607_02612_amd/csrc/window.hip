@@ -93,6 +93,19 @@ __device__ __forceinline__ bool none_see(const WindowArgs& a, int i0, int i1, in
   return (i0 - j1 >= a.window || j0 - i1 >= a.window) && j0 >= a.sinks;
 }
 
+// The rows that a row sees: lo .. lo + span, and those below first.
+struct RowSpan {
+  int lo, first;
+  unsigned span;
+};
+__device__ __forceinline__ RowSpan row_span(const WindowArgs& a, int i, int n) {
+  RowSpan r;
+  r.lo = max(0, i - a.window + 1);
+  r.span = (unsigned)((a.causal ? min(i, n - 1) : min(n - 1, i + a.window - 1)) - r.lo);
+  r.first = min(a.sinks, a.causal ? i + 1 : n);
+  return r;
+}
+
 // The query rows of a workgroup and the key tiles that any of them sees: the
 // first `ns` tiles of the sample (sinks), then tiles lo .. hi.
 struct WindowPlan {
@@ -131,8 +144,8 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma(WindowArgs 
   constexpr int ROWB = DP * 2, TILEB = WKT * ROWB;
   constexpr int KS = DP / 16, ND = DP / 32;
   __shared__ __attribute__((aligned(16))) char smem[4 * TILEB];  // [stage][K, V]
-  __shared__ float lnS[2][WKT];
-  __shared__ int s_bad;
+  __shared__ __attribute__((aligned(16))) float lnS[2][WKT];
+  __shared__ int s_bad, s_hidden[2];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int hl = lane >> 5, c = lane & 31;
   const int per_group = a.group >> hshift, units = a.H >> hshift;
@@ -174,7 +187,11 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma(WindowArgs 
     if (SIZES && tid < WKT) size_next = a.size[pl.base + min(t * WKT + tid, n - 1)];
   };
   auto put_size = [&](int st) {
-    if (SIZES && tid < WKT) lnS[st][tid] = size_next > 0.f ? logf(size_next) * kLog2e : -INFINITY;
+    if (SIZES && tid < WKT) {
+      lnS[st][tid] = size_next > 0.f ? logf(size_next) * kLog2e : -INFINITY;
+      const bool hidden = __any(!(size_next > 0.f));
+      if (tid == 0) s_hidden[st] = hidden;
+    }
   };
   copy_tile(pl.tile(0), 0);
   load_size(pl.tile(0));
@@ -194,6 +211,7 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma(WindowArgs 
   put_size(0);
   const float sc2 = a.scale * kLog2e;
   float m = -INFINITY, l = 0.f;
+  const RowSpan sp = row_span(a, w0 + c, n);
   f32x16_t O[ND];
 #pragma unroll
   for (int d = 0; d < ND; d++)
@@ -215,7 +233,8 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma(WindowArgs 
     const char* Ks = smem + st * 2 * TILEB;
     char* Vs = smem + st * 2 * TILEB + TILEB;
     bool bad = false;
-    if (SIZES || k0 + WKT > n || !all_see(a, pl.q0, pl.q1, k0, k0 + WKT - 1)) {
+    const bool hidden = SIZES && s_hidden[st];  // some key of the tile has no size
+    if (hidden || k0 + WKT > n || !all_see(a, pl.q0, pl.q1, k0, k0 + WKT - 1)) {
       uint32_t any = 0;
 #pragma unroll
       for (int u = 0; u < TILEB / (64 * WNW * 16); u++) {
@@ -264,23 +283,41 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma(WindowArgs 
         }
       }
       const bool edge = k0 + WKT > n || !all_see(a, w0, w1, k0, k0 + WKT - 1);
-      // -inf for keys that the query does not see; with sizes already in base 2
-      if (SIZES || edge) {
+      // with sizes the scores of base 2; -inf for keys that the query does not see
+      if (SIZES) {
 #pragma unroll
         for (int x = 0; x < 2; x++)
 #pragma unroll
           for (int i4 = 0; i4 < 4; i4++) {
-            f32x4_t ln = {0.f, 0.f, 0.f, 0.f};
-            if (SIZES) ln = *(const f32x4_t*)(&lnS[st][x * 32 + 8 * i4 + 4 * hl]);
+            const f32x4_t ln = *(const f32x4_t*)(&lnS[st][x * 32 + 8 * i4 + 4 * hl]);
 #pragma unroll
-            for (int j = 0; j < 4; j++) {
-              const int key = k0 + x * 32 + 8 * i4 + 4 * hl + j;
-              const bool see = (!edge || (key < n && sees(a, w0 + c, key))) &&
-                               !(SIZES && ln[j] == -INFINITY);
-              const float t = SIZES ? fmaf(S[x][4 * i4 + j], sc2, ln[j]) : S[x][4 * i4 + j];
-              S[x][4 * i4 + j] = see ? t : -INFINITY;
-            }
+            for (int j = 0; j < 4; j++) S[x][4 * i4 + j] = fmaf(S[x][4 * i4 + j], sc2, ln[j]);
           }
+        if (hidden)
+#pragma unroll
+          for (int x = 0; x < 2; x++)
+#pragma unroll
+            for (int i = 0; i < 16; i++)
+              if (lnS[st][x * 32 + 8 * (i / 4) + 4 * hl + i % 4] == -INFINITY) S[x][i] = -INFINITY;
+      }
+      if (edge) {
+        const unsigned at = (unsigned)(k0 + 4 * hl - sp.lo);
+        if (k0 < a.sinks) {
+          const int first = sp.first - k0 - 4 * hl;
+#pragma unroll
+          for (int x = 0; x < 2; x++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+              const int key = x * 32 + 8 * (i / 4) + i % 4;
+              S[x][i] = (at + key <= sp.span) | (key < first) ? S[x][i] : -INFINITY;
+            }
+        } else {
+#pragma unroll
+          for (int x = 0; x < 2; x++)
+#pragma unroll
+            for (int i = 0; i < 16; i++)
+              S[x][i] = at + (x * 32 + 8 * (i / 4) + i % 4) <= sp.span ? S[x][i] : -INFINITY;
+        }
       }
       float mt = -INFINITY;
 #pragma unroll
@@ -367,8 +404,8 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowA
   constexpr int TILEB = 16384, ROWB = DP * 4, KT = TILEB / ROWB;
   constexpr int NC = KT / RPC / WNW, NT = KT / 16, NU = DP / 16;
   __shared__ __attribute__((aligned(16))) char smem[4 * TILEB];  // [stage][K, V]
-  __shared__ float lnS[2][KT];
-  __shared__ int s_bad;
+  __shared__ __attribute__((aligned(16))) float lnS[2][KT];
+  __shared__ int s_bad, s_hidden[2];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int g = lane >> 4, c = lane & 15;
   const int per_group = a.group >> hshift, units = a.H >> hshift;
@@ -408,7 +445,11 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowA
     if (SIZES && tid < KT) size_next = a.size[pl.base + min(t * KT + tid, n - 1)];
   };
   auto put_size = [&](int st) {
-    if (SIZES && tid < KT) lnS[st][tid] = size_next > 0.f ? logf(size_next) * kLog2e : -INFINITY;
+    if (SIZES && tid < KT) {
+      lnS[st][tid] = size_next > 0.f ? logf(size_next) * kLog2e : -INFINITY;
+      const bool hidden = __any(!(size_next > 0.f));
+      if (tid == 0) s_hidden[st] = hidden;
+    }
   };
   copy_tile(pl.tile(0), 0);
   load_size(pl.tile(0));
@@ -426,6 +467,7 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowA
   put_size(0);
   const float sc2 = a.scale * kLog2e;
   float m = -INFINITY, l = 0.f;
+  const RowSpan sp = row_span(a, w0 + c, n);
   f32x4_t O[NU];
 #pragma unroll
   for (int d = 0; d < NU; d++) O[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -441,7 +483,8 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowA
     const char* Ks = smem + st * 2 * TILEB;
     char* Vs = smem + st * 2 * TILEB + TILEB;
     bool bad = false;
-    if (SIZES || k0 + KT > n || !all_see(a, pl.q0, pl.q1, k0, k0 + KT - 1)) {
+    const bool hidden = SIZES && s_hidden[st];  // some key of the tile has no size
+    if (hidden || k0 + KT > n || !all_see(a, pl.q0, pl.q1, k0, k0 + KT - 1)) {
       bool any = false;
 #pragma unroll
       for (int u = 0; u < TILEB / (64 * WNW * 16); u++) {
@@ -490,19 +533,30 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowA
             S[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[x][i], qf[u][i], S[x], 0, 0, 0);
       }
       const bool edge = k0 + KT > n || !all_see(a, w0, w1, k0, k0 + KT - 1);
-      float mt = -INFINITY;
 #pragma unroll
       for (int x = 0; x < NT; x++) {
         f32x4_t ln = {0.f, 0.f, 0.f, 0.f};
         if (SIZES) ln = *(const f32x4_t*)(&lnS[st][16 * x + 4 * g]);
 #pragma unroll
         for (int j = 0; j < 4; j++) {
-          const int key = k0 + 16 * x + 4 * g + j;
-          const bool see = (!edge || (key < n && sees(a, w0 + c, key))) && !(SIZES && ln[j] == -INFINITY);
-          S[x][j] = see ? fmaf(S[x][j], sc2, ln[j]) : -INFINITY;
-          mt = fmaxf(mt, S[x][j]);
+          S[x][j] = fmaf(S[x][j], sc2, ln[j]);
+          if (hidden && ln[j] == -INFINITY) S[x][j] = -INFINITY;
         }
       }
+      if (edge) {
+        const unsigned at = (unsigned)(k0 + 4 * g - sp.lo);
+        const int first = sp.first - k0 - 4 * g;
+#pragma unroll
+        for (int x = 0; x < NT; x++)
+#pragma unroll
+          for (int j = 0; j < 4; j++)
+            S[x][j] = (at + (16 * x + j) <= sp.span) | (16 * x + j < first) ? S[x][j] : -INFINITY;
+      }
+      float mt = -INFINITY;
+#pragma unroll
+      for (int x = 0; x < NT; x++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) mt = fmaxf(mt, S[x][j]);
       mt = max_xor32(max_xor16(mt));
       const bool grow = mt > m + 8.f;
       if (__any(grow)) {
