@@ -6,6 +6,7 @@
 #include "kernels.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace fusion {
 namespace {
@@ -49,8 +50,8 @@ struct WindowSeqs {
 // A probability of 0 does not take a value out of P V when that value is
 // infinite or NaN.  A tile that some query of the workgroup sees and another
 // does not is therefore searched for such values; if there are any, they are
-// cleared in LDS and added by hand to the rows that see them (their weight is
-// positive, so an infinity stays one).
+// cleared in LDS and, after the last tile, added to the rows that see them
+// (their weight is positive, so an infinity stays one).
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
@@ -82,15 +83,25 @@ __device__ __forceinline__ bool sees(const WindowArgs& a, int i, int j) {
   if (a.causal) return j <= i && (i - j < a.window || j < a.sinks);
   return (i - j < a.window && j - i < a.window) || j < a.sinks;
 }
-// Whether all of rows i0 .. i1 see all of j0 .. j1.
+// Whether all of rows i0 .. i1 see all of j0 .. j1, and whether none sees any.
+// (Without short cuts: each is one scalar condition, and the tile loop keeps
+// its branches simple.)
 __device__ __forceinline__ bool all_see(const WindowArgs& a, int i0, int i1, int j0, int j1) {
-  if (a.causal) return j1 <= i0 && (i1 - j0 < a.window || j1 < a.sinks);
-  return (i1 - j0 < a.window && j1 - i0 < a.window) || j1 < a.sinks;
+  const bool near = (i1 - j0 < a.window) & ((a.causal != 0) | (j1 - i0 < a.window));
+  return (near | (j1 < a.sinks)) & ((a.causal == 0) | (j1 <= i0));
 }
-// Whether none of rows i0 .. i1 sees any of j0 .. j1.
 __device__ __forceinline__ bool none_see(const WindowArgs& a, int i0, int i1, int j0, int j1) {
-  if (a.causal) return j0 > i1 || (i0 - j1 >= a.window && j0 >= a.sinks);
-  return (i0 - j1 >= a.window || j0 - i1 >= a.window) && j0 >= a.sinks;
+  const bool far = (i0 - j1 >= a.window) | ((a.causal == 0) & (j0 - i1 >= a.window));
+  return (far & (j0 >= a.sinks)) | ((a.causal != 0) & (j0 > i1));
+}
+// How a wave takes a tile of keys j0 .. j0 + keys - 1: not at all, or with or
+// without looking at each pair.
+enum { TILE_SKIP, TILE_WHOLE, TILE_EDGE };
+__device__ __forceinline__ int tile_mode(const WindowArgs& a, int n, int i0, int i1, int j0, int keys,
+                                         bool hidden) {
+  const bool edge = hidden | (j0 + keys > n) | !all_see(a, i0, i1, j0, j0 + keys - 1);
+  const bool skip = (i0 >= n) | none_see(a, i0, i1, j0, j0 + keys - 1);
+  return __builtin_amdgcn_readfirstlane(skip ? TILE_SKIP : edge ? TILE_EDGE : TILE_WHOLE);
 }
 
 // The rows that a row sees: lo .. lo + span, and those below first.
@@ -114,6 +125,7 @@ struct WindowPlan {
   int ns, lo, nt;
   __device__ __forceinline__ int tile(int it) const { return it < ns ? it : lo + it - ns; }
 };
+// (every member is the same in all lanes, and the compiler has to know it)
 __device__ __forceinline__ WindowPlan window_plan(const WindowArgs& a, const WindowSeqs& sq, int tile,
                                                   int rows, int keys) {
   int lo = 0, hi = sq.n - 1;  // the last sample whose first tile is not after this one
@@ -136,7 +148,7 @@ __device__ __forceinline__ WindowPlan window_plan(const WindowArgs& a, const Win
 }
 
 template <int DP, bool PAD, bool SIZES>
-__global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma(WindowArgs a, WindowSeqs sq,
+__global__ __launch_bounds__(64 * WNW, DP == 64 ? 3 : 2) void window_attention_mfma(WindowArgs a, WindowSeqs sq,
                                                                      int tiles, int hshift) {
   constexpr int PPR = DP / 8;             // 16-byte pieces per row
   constexpr int RPC = 64 / PPR;           // rows per copy
@@ -212,6 +224,7 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma(WindowArgs 
   const float sc2 = a.scale * kLog2e;
   float m = -INFINITY, l = 0.f;
   const RowSpan sp = row_span(a, w0 + c, n);
+  bool any_bad = false;
   f32x16_t O[ND];
 #pragma unroll
   for (int d = 0; d < ND; d++)
@@ -222,19 +235,22 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma(WindowArgs 
   const int krow = c * ROWB, kx = c & (PPR - 1);
   const int vkey = (lane & 15) >> 2;
   const int vcol = ((lane >> 4) & 1) * 32 + (lane & 3) * 8;  // bytes within a 64-byte dim tile
-  for (int it = 0; it < pl.nt; it++) {
-    const int st = it & 1, t = pl.tile(it), k0 = t * WKT;
+  int it = 0, st = 0, k0 = 0;  // the tile in hand: its number, LDS stage and first key
+  bool hidden = false;         // some key of it has no size
+  // waits for tile `it`, starts the next one's copies, clears what no product
+  // may meet; returns how the wave takes it
+  auto begin = [&]() {
+    st = it & 1;
+    k0 = pl.tile(it) * WKT;
     wait_copies();
     __syncthreads();
     if (it + 1 < pl.nt) {
       copy_tile(pl.tile(it + 1), st ^ 1);
       load_size(pl.tile(it + 1));
     }
-    const char* Ks = smem + st * 2 * TILEB;
-    char* Vs = smem + st * 2 * TILEB + TILEB;
-    bool bad = false;
-    const bool hidden = SIZES && s_hidden[st];  // some key of the tile has no size
-    if (hidden || k0 + WKT > n || !all_see(a, pl.q0, pl.q1, k0, k0 + WKT - 1)) {
+    hidden = SIZES && __builtin_amdgcn_readfirstlane(s_hidden[st]);
+    if (tile_mode(a, n, pl.q0, pl.q1, k0, WKT, hidden) == TILE_EDGE) {
+      char* Vs = smem + st * 2 * TILEB + TILEB;
       uint32_t any = 0;
 #pragma unroll
       for (int u = 0; u < TILEB / (64 * WNW * 16); u++) {
@@ -244,18 +260,134 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma(WindowArgs 
       }
       if (any & 0x80008000u) s_bad = it;
       __syncthreads();
-      bad = s_bad == it;
-    }
-    const bool active = w0 < n && !none_see(a, w0, w1, k0, k0 + WKT - 1);
-    if (bad) {
-      for (int u = tid; u < TILEB / 2; u += 64 * WNW) {
-        bf16_t* v = (bf16_t*)Vs + u;
-        if ((*v & 0x7F80) == 0x7F80) *v = 0;
+      if (__builtin_amdgcn_readfirstlane(s_bad) == it) {
+        for (int u = tid; u < TILEB / 2; u += 64 * WNW) {
+          bf16_t* v = (bf16_t*)Vs + u;
+          if ((*v & 0x7F80) == 0x7F80) *v = 0;
+        }
+        any_bad = true;
+        __syncthreads();
       }
-      __syncthreads();
-      for (int j = k0; active && j < min(n, k0 + WKT); j++) {
-        const bool see = w0 + c < n && sees(a, w0 + c, j) && !(SIZES && !(a.size[pl.base + j] > 0.f));
-        if (!see) continue;
+    }
+    return tile_mode(a, n, w0, w1, k0, WKT, hidden);
+  };
+  // the next tile's mode, or -1 after the last
+  auto next = [&]() {
+    if (it + 1 < pl.nt) put_size(st ^ 1);
+    return ++it < pl.nt ? begin() : -1;
+  };
+  auto compute = [&](auto edge_c) {
+    constexpr bool EDGE = decltype(edge_c)::value;
+    const char* Ks = smem + st * 2 * TILEB;
+    const char* Vs = Ks + TILEB;
+    f32x16_t S[2];
+#pragma unroll
+    for (int x = 0; x < 2; x++) {
+#pragma unroll
+      for (int i = 0; i < 16; i++) S[x][i] = 0.f;
+#pragma unroll
+      for (int s = 0; s < KS; s++) {
+        const bf16x8_t kf = *(const bf16x8_t*)(Ks + x * 32 * ROWB + krow + (((2 * s + hl) ^ kx) << 4));
+        S[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], S[x], 0, 0, 0);
+      }
+    }
+    // with sizes the scores of base 2; -inf for keys that the query does not see
+    if (SIZES) {
+#pragma unroll
+      for (int x = 0; x < 2; x++)
+#pragma unroll
+        for (int i4 = 0; i4 < 4; i4++) {
+          const f32x4_t ln = *(const f32x4_t*)(&lnS[st][x * 32 + 8 * i4 + 4 * hl]);
+#pragma unroll
+          for (int j = 0; j < 4; j++) S[x][4 * i4 + j] = fmaf(S[x][4 * i4 + j], sc2, ln[j]);
+        }
+      if (EDGE && hidden)
+#pragma unroll
+        for (int x = 0; x < 2; x++)
+#pragma unroll
+          for (int i = 0; i < 16; i++)
+            if (lnS[st][x * 32 + 8 * (i / 4) + 4 * hl + i % 4] == -INFINITY) S[x][i] = -INFINITY;
+    }
+    if (EDGE) {
+      const unsigned at = (unsigned)(k0 + 4 * hl - sp.lo);
+      const int first = sp.first - k0 - 4 * hl;
+#pragma unroll
+      for (int x = 0; x < 2; x++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+          const int key = x * 32 + 8 * (i / 4) + i % 4;
+          S[x][i] = (at + key <= sp.span) | (key < first) ? S[x][i] : -INFINITY;
+        }
+    }
+    float mt = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < 2; x++)
+#pragma unroll
+      for (int i = 0; i < 16; i++) mt = fmaxf(mt, S[x][i]);
+    mt = max_xor32(mt);
+    if (!SIZES) mt *= sc2;
+    const bool grow = mt > m + 8.f;
+    if (__any(grow)) {
+      const float f = grow ? __builtin_amdgcn_exp2f(m - mt) : 1.f;
+      if (grow) m = mt;
+      l *= f;
+#pragma unroll
+      for (int d = 0; d < ND; d++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) O[d][i] *= f;
+    }
+    const float mu = m == -INFINITY ? 0.f : m;
+    bf16x8_t pf[4];
+    float lt[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < 2; x++)
+#pragma unroll
+      for (int y = 0; y < 2; y++) {
+        union { uint32_t u[4]; bf16x8_t v; } p;
+#pragma unroll
+        for (int w = 0; w < 4; w++) {
+          const float s0 = S[x][8 * y + 2 * w], s1 = S[x][8 * y + 2 * w + 1];
+          const float e0 = __builtin_amdgcn_exp2f(SIZES ? s0 - mu : fmaf(s0, sc2, -mu));
+          const float e1 = __builtin_amdgcn_exp2f(SIZES ? s1 - mu : fmaf(s1, sc2, -mu));
+          lt[w] += e0 + e1;
+          p.u[w] = pack_bf16x2(e0, e1);
+        }
+        pf[2 * x + y] = p.v;
+      }
+    l += (lt[0] + lt[1]) + (lt[2] + lt[3]);
+#pragma unroll
+    for (int y = 0; y < 4; y++)
+#pragma unroll
+      for (int d = 0; d < ND; d++) {
+        union { s16x4_t h[2]; bf16x8_t v; } vf;
+#pragma unroll
+        for (int z = 0; z < 2; z++) {
+          const int key = 16 * y + 8 * z + 4 * hl + vkey;  // key % 4 == vkey
+          const int seg = (d * 2 + (vcol >> 5)) ^ vkey;
+          vf.h[z] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (__attribute__((address_space(3))) s16x4_t*)(Vs + key * ROWB + seg * 32 + (vcol & 31)));
+        }
+        O[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, pf[y], O[d], 0, 0, 0);
+      }
+  };
+  // (a loop for each mode, since tiles of one come in runs: with one loop over
+  // both copies of the code the output moved between registers in every tile)
+  int mode = begin();
+  while (mode >= 0) {
+    while (mode == TILE_WHOLE) {
+      compute(std::false_type{});
+      mode = next();
+    }
+    while (mode == TILE_EDGE) {
+      compute(std::true_type{});
+      mode = next();
+    }
+    while (mode == TILE_SKIP) mode = next();
+  }
+  if (any_bad && w0 + c < n) {  // the values that were cleared, for the rows that see them
+    for (int it = 0; it < pl.nt; it++)
+      for (int j = pl.tile(it) * WKT; j < min(n, pl.tile(it) * WKT + WKT); j++) {
+        if (!sees(a, w0 + c, j) || (SIZES && !(a.size[pl.base + j] > 0.f))) continue;
         const bf16_t* v = vg + (int64_t)j * a.v_row + 4 * hl;
 #pragma unroll
         for (int d = 0; d < ND; d++)
@@ -269,108 +401,6 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma(WindowArgs 
             for (int q = 0; q < 4; q++) O[d][4 * i4 + q] += fabsf(e[q]) < INFINITY ? 0.f : e[q];
           }
       }
-    }
-    if (active) {
-      f32x16_t S[2];
-#pragma unroll
-      for (int x = 0; x < 2; x++) {
-#pragma unroll
-        for (int i = 0; i < 16; i++) S[x][i] = 0.f;
-#pragma unroll
-        for (int s = 0; s < KS; s++) {
-          const bf16x8_t kf = *(const bf16x8_t*)(Ks + x * 32 * ROWB + krow + (((2 * s + hl) ^ kx) << 4));
-          S[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], S[x], 0, 0, 0);
-        }
-      }
-      const bool edge = k0 + WKT > n || !all_see(a, w0, w1, k0, k0 + WKT - 1);
-      // with sizes the scores of base 2; -inf for keys that the query does not see
-      if (SIZES) {
-#pragma unroll
-        for (int x = 0; x < 2; x++)
-#pragma unroll
-          for (int i4 = 0; i4 < 4; i4++) {
-            const f32x4_t ln = *(const f32x4_t*)(&lnS[st][x * 32 + 8 * i4 + 4 * hl]);
-#pragma unroll
-            for (int j = 0; j < 4; j++) S[x][4 * i4 + j] = fmaf(S[x][4 * i4 + j], sc2, ln[j]);
-          }
-        if (hidden)
-#pragma unroll
-          for (int x = 0; x < 2; x++)
-#pragma unroll
-            for (int i = 0; i < 16; i++)
-              if (lnS[st][x * 32 + 8 * (i / 4) + 4 * hl + i % 4] == -INFINITY) S[x][i] = -INFINITY;
-      }
-      if (edge) {
-        const unsigned at = (unsigned)(k0 + 4 * hl - sp.lo);
-        if (k0 < a.sinks) {
-          const int first = sp.first - k0 - 4 * hl;
-#pragma unroll
-          for (int x = 0; x < 2; x++)
-#pragma unroll
-            for (int i = 0; i < 16; i++) {
-              const int key = x * 32 + 8 * (i / 4) + i % 4;
-              S[x][i] = (at + key <= sp.span) | (key < first) ? S[x][i] : -INFINITY;
-            }
-        } else {
-#pragma unroll
-          for (int x = 0; x < 2; x++)
-#pragma unroll
-            for (int i = 0; i < 16; i++)
-              S[x][i] = at + (x * 32 + 8 * (i / 4) + i % 4) <= sp.span ? S[x][i] : -INFINITY;
-        }
-      }
-      float mt = -INFINITY;
-#pragma unroll
-      for (int x = 0; x < 2; x++)
-#pragma unroll
-        for (int i = 0; i < 16; i++) mt = fmaxf(mt, S[x][i]);
-      mt = max_xor32(mt);
-      if (!SIZES) mt *= sc2;
-      const bool grow = mt > m + 8.f;
-      if (__any(grow)) {
-        const float f = grow ? __builtin_amdgcn_exp2f(m - mt) : 1.f;
-        if (grow) m = mt;
-        l *= f;
-#pragma unroll
-        for (int d = 0; d < ND; d++)
-#pragma unroll
-          for (int i = 0; i < 16; i++) O[d][i] *= f;
-      }
-      const float mu = m == -INFINITY ? 0.f : m;
-      bf16x8_t pf[4];
-      float lt[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int x = 0; x < 2; x++)
-#pragma unroll
-        for (int y = 0; y < 2; y++) {
-          union { uint32_t u[4]; bf16x8_t v; } p;
-#pragma unroll
-          for (int w = 0; w < 4; w++) {
-            const float s0 = S[x][8 * y + 2 * w], s1 = S[x][8 * y + 2 * w + 1];
-            const float e0 = __builtin_amdgcn_exp2f(SIZES ? s0 - mu : fmaf(s0, sc2, -mu));
-            const float e1 = __builtin_amdgcn_exp2f(SIZES ? s1 - mu : fmaf(s1, sc2, -mu));
-            lt[w] += e0 + e1;
-            p.u[w] = pack_bf16x2(e0, e1);
-          }
-          pf[2 * x + y] = p.v;
-        }
-      l += (lt[0] + lt[1]) + (lt[2] + lt[3]);
-#pragma unroll
-      for (int y = 0; y < 4; y++)
-#pragma unroll
-        for (int d = 0; d < ND; d++) {
-          union { s16x4_t h[2]; bf16x8_t v; } vf;
-#pragma unroll
-          for (int z = 0; z < 2; z++) {
-            const int key = 16 * y + 8 * z + 4 * hl + vkey;  // key % 4 == vkey
-            const int seg = (d * 2 + (vcol >> 5)) ^ vkey;
-            vf.h[z] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (__attribute__((address_space(3))) s16x4_t*)(Vs + key * ROWB + seg * 32 + (vcol & 31)));
-          }
-          O[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, pf[y], O[d], 0, 0, 0);
-        }
-    }
-    if (it + 1 < pl.nt) put_size(st ^ 1);
   }
   l = sum_xor32(l);
   if (w0 + c < n) {
@@ -468,6 +498,7 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowA
   const float sc2 = a.scale * kLog2e;
   float m = -INFINITY, l = 0.f;
   const RowSpan sp = row_span(a, w0 + c, n);
+  bool any_bad = false;
   f32x4_t O[NU];
 #pragma unroll
   for (int d = 0; d < NU; d++) O[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -483,8 +514,8 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowA
     const char* Ks = smem + st * 2 * TILEB;
     char* Vs = smem + st * 2 * TILEB + TILEB;
     bool bad = false;
-    const bool hidden = SIZES && s_hidden[st];  // some key of the tile has no size
-    if (hidden || k0 + KT > n || !all_see(a, pl.q0, pl.q1, k0, k0 + KT - 1)) {
+    const bool hidden = SIZES && __builtin_amdgcn_readfirstlane(s_hidden[st]);  // some key of the tile has no size
+    if (tile_mode(a, n, pl.q0, pl.q1, k0, KT, hidden) == TILE_EDGE) {
       bool any = false;
 #pragma unroll
       for (int u = 0; u < TILEB / (64 * WNW * 16); u++) {
@@ -494,29 +525,18 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowA
       }
       if (any) s_bad = it;
       __syncthreads();
-      bad = s_bad == it;
+      bad = __builtin_amdgcn_readfirstlane(s_bad) == it;
     }
-    const bool active = w0 < n && !none_see(a, w0, w1, k0, k0 + KT - 1);
     if (bad) {
       for (int u = tid; u < TILEB / 4; u += 64 * WNW) {
         float* v = (float*)Vs + u;
         if (!(fabsf(*v) < INFINITY)) *v = 0.f;
       }
+      any_bad = true;
       __syncthreads();
-      for (int j = k0; active && j < min(n, k0 + KT); j++) {
-        const bool see = w0 + c < n && sees(a, w0 + c, j) && !(SIZES && !(a.size[pl.base + j] > 0.f));
-        if (!see) continue;
-        const float* v = vg + (int64_t)j * a.v_row + 4 * g;
-#pragma unroll
-        for (int d = 0; d < NU; d++) {
-          if (PAD && 16 * d + 4 * g >= dh) break;
-          const f32x4_t x = *(const f32x4_t*)(v + 16 * d);
-#pragma unroll
-          for (int q = 0; q < 4; q++) O[d][q] += fabsf(x[q]) < INFINITY ? 0.f : x[q];
-        }
-      }
     }
-    if (active) {
+    const int mode = tile_mode(a, n, w0, w1, k0, KT, hidden);
+    if (mode != TILE_SKIP) {
       f32x4_t S[NT];
 #pragma unroll
       for (int x = 0; x < NT; x++) S[x] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -532,7 +552,6 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowA
           for (int x = 0; x < NT; x++)
             S[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[x][i], qf[u][i], S[x], 0, 0, 0);
       }
-      const bool edge = k0 + KT > n || !all_see(a, w0, w1, k0, k0 + KT - 1);
 #pragma unroll
       for (int x = 0; x < NT; x++) {
         f32x4_t ln = {0.f, 0.f, 0.f, 0.f};
@@ -543,7 +562,7 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowA
           if (hidden && ln[j] == -INFINITY) S[x][j] = -INFINITY;
         }
       }
-      if (edge) {
+      if (mode == TILE_EDGE) {
         const unsigned at = (unsigned)(k0 + 4 * g - sp.lo);
         const int first = sp.first - k0 - 4 * g;
 #pragma unroll
@@ -587,6 +606,20 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowA
         }
     }
     if (it + 1 < pl.nt) put_size(st ^ 1);
+  }
+  if (any_bad && w0 + c < n) {  // the values that were cleared, for the rows that see them
+    for (int it = 0; it < pl.nt; it++)
+      for (int j = pl.tile(it) * KT; j < min(n, pl.tile(it) * KT + KT); j++) {
+        if (!sees(a, w0 + c, j) || (SIZES && !(a.size[pl.base + j] > 0.f))) continue;
+        const float* v = vg + (int64_t)j * a.v_row + 4 * g;
+#pragma unroll
+        for (int d = 0; d < NU; d++) {
+          if (PAD && 16 * d + 4 * g >= dh) break;
+          const f32x4_t x = *(const f32x4_t*)(v + 16 * d);
+#pragma unroll
+          for (int q = 0; q < 4; q++) O[d][q] += fabsf(x[q]) < INFINITY ? 0.f : x[q];
+        }
+      }
   }
   l = sum_xor32(sum_xor16(l));
   if (w0 + c < n) {
