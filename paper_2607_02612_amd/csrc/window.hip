@@ -147,14 +147,15 @@ __device__ __forceinline__ WindowPlan window_plan(const WindowArgs& a, const Win
   return p;
 }
 
-template <int DP, bool PAD, bool SIZES>
-__global__ __launch_bounds__(64 * WNW, DP == 64 ? 3 : 2) void window_attention_mfma(WindowArgs a, WindowSeqs sq,
+template <int DC, bool PAD, bool SIZES>
+__global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_mfma(WindowArgs a, WindowSeqs sq,
                                                                      int tiles, int hshift) {
+  constexpr int DP = DC <= 64 ? 64 : 128;  // dims of an LDS row; DC of them take part
   constexpr int PPR = DP / 8;             // 16-byte pieces per row
   constexpr int RPC = 64 / PPR;           // rows per copy
   constexpr int NC = WKT / RPC / WNW;     // copies of K (and of V) per wave and tile
   constexpr int ROWB = DP * 2, TILEB = WKT * ROWB;
-  constexpr int KS = DP / 16, ND = DP / 32;
+  constexpr int KS = DC / 16, ND = DC / 32;
   __shared__ __attribute__((aligned(16))) char smem[4 * TILEB];  // [stage][K, V]
   __shared__ __attribute__((aligned(16))) float lnS[2][WKT];
   __shared__ int s_bad, s_hidden[2];
@@ -423,16 +424,18 @@ __global__ __launch_bounds__(64 * WNW, DP == 64 ? 3 : 2) void window_attention_m
 // against keys 16 t + 4 g + j, and these registers are the operand of
 // O^T = V^T P^T as they stand (slot g of step j is key 16 t + 4 g + j).  A
 // 16-byte piece of a key feeds four steps (slot g of step i is dim
-// 16 u + 4 g + i).  Tiles are 16 KB of keys and as much of values; K's pieces
-// are XOR-permuted by the row mod 16, V's groups of four pieces by row / 4
+// 16 u + 4 g + i).  Tiles are 8 KB of keys and as much of values (with 16 KB a
+// window of 130 took 51 us instead of 37, since more of a tile lies outside,
+// and one of 4,096 took 491 instead of 502); K's pieces are XOR-permuted by the row mod 16, V's groups of four pieces by row / 4
 // mod 4, so that the 16-byte key reads of 16 rows and the 4-byte value reads
 // of 4 x 16 spread over all banks.
-template <int DP, bool PAD, bool SIZES>
+template <int DC, bool PAD, bool SIZES>
 __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowArgs a, WindowSeqs sq,
                                                                          int tiles, int hshift) {
+  constexpr int DP = DC <= 64 ? 64 : 128;
   constexpr int PPR = DP / 4, RPC = 64 / PPR;  // pieces per row, rows per copy
-  constexpr int TILEB = 16384, ROWB = DP * 4, KT = TILEB / ROWB;
-  constexpr int NC = KT / RPC / WNW, NT = KT / 16, NU = DP / 16;
+  constexpr int TILEB = 8192, ROWB = DP * 4, KT = TILEB / ROWB;
+  constexpr int NC = KT / RPC / WNW, NT = KT / 16, NU = DC / 16;
   __shared__ __attribute__((aligned(16))) char smem[4 * TILEB];  // [stage][K, V]
   __shared__ __attribute__((aligned(16))) float lnS[2][KT];
   __shared__ int s_bad, s_hidden[2];
@@ -651,7 +654,7 @@ hipError_t for_samples(const int32_t* cu_host, int batch, int rows, F launch) {
   return hipSuccess;
 }
 
-template <typename T, int DP, bool PAD>
+template <typename T, int DC, bool PAD>
 hipError_t launch_mfma(const WindowArgs& a, const int32_t* cu_host, int batch, hipStream_t s) {
   // heads of a group per workgroup, 1 << hshift
   const int hshift = a.group % 4 == 0 ? 2 : a.group % 2 == 0 ? 1 : 0;
@@ -660,14 +663,14 @@ hipError_t launch_mfma(const WindowArgs& a, const int32_t* cu_host, int batch, h
     const dim3 grid((unsigned)tiles * (a.H >> hshift));
     if constexpr (sizeof(T) == 2) {
       if (a.size)
-        window_attention_mfma<DP, PAD, true><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
+        window_attention_mfma<DC, PAD, true><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
       else
-        window_attention_mfma<DP, PAD, false><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
+        window_attention_mfma<DC, PAD, false><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
     } else {
       if (a.size)
-        window_attention_mfma_f32<DP, PAD, true><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
+        window_attention_mfma_f32<DC, PAD, true><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
       else
-        window_attention_mfma_f32<DP, PAD, false><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
+        window_attention_mfma_f32<DC, PAD, false><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
     }
   });
 }
@@ -677,10 +680,12 @@ hipError_t launch_mfma(const WindowArgs& a, const int32_t* cu_host, int batch, h
 template <typename T>
 hipError_t launch_window_attention(const WindowArgs& a, const int32_t* cu_host, int batch,
                                    hipStream_t s) {
+  // (dims are taken in 64, 96 or 128, the rest of them zeros)
   if (a.dh == 64) return launch_mfma<T, 64, false>(a, cu_host, batch, s);
   if (a.dh < 64) return launch_mfma<T, 64, true>(a, cu_host, batch, s);
-  if (a.dh == 128) return launch_mfma<T, 128, false>(a, cu_host, batch, s);
-  return launch_mfma<T, 128, true>(a, cu_host, batch, s);
+  if (a.dh <= 96) return launch_mfma<T, 96, true>(a, cu_host, batch, s);
+  if (a.dh < 128) return launch_mfma<T, 128, true>(a, cu_host, batch, s);
+  return launch_mfma<T, 128, false>(a, cu_host, batch, s);
 }
 template hipError_t launch_window_attention<float>(const WindowArgs&, const int32_t*, int,
                                                    hipStream_t);
