@@ -36,12 +36,13 @@ __device__ __forceinline__ uint4* piece(void* base, int64_t page_stride, int64_t
   return (uint4*)((T*)base + page * page_stride + place * row_stride + h * head_stride) + d;
 }
 
-// Offsets of a batch as kernel arguments.
-constexpr int APPEND_SEQS = 896;
+// Offsets of the samples of one launch as kernel arguments.
+constexpr int APPEND_SEQS = 256;
 struct AppendSeqs {
-  int n, first;  // samples of this launch, the first one's index
+  int n, first;  // samples, the first one's index
   int cu[APPEND_SEQS + 1];
 };
+struct OneRowEach {};
 
 // --------------------------------------------------------------- append --
 // Row r of sample i goes to slot len + r - cu[i]: a copy, bound by its bytes.
@@ -71,11 +72,15 @@ __device__ __forceinline__ void append_row(const CacheArgs& c, const AppendArgs&
   }
 }
 
-// One workgroup per sample; first[b] .. its rows, one each without offsets.
-template <typename T, bool OFFSETS>
-__global__ __launch_bounds__(256) void append_few(CacheArgs c, AppendArgs a, AppendSeqs sq) {
-  const int b = OFFSETS ? sq.first + blockIdx.x : blockIdx.x;
-  const int r0 = OFFSETS ? sq.cu[blockIdx.x] : b, n = OFFSETS ? sq.cu[blockIdx.x + 1] - r0 : 1;
+// One workgroup per sample (Seqs: AppendSeqs, or OneRowEach).
+template <typename T, typename Seqs>
+__global__ __launch_bounds__(256) void append_few(CacheArgs c, AppendArgs a, Seqs sq) {
+  int b = blockIdx.x, r0 = b, n = 1;
+  if constexpr (std::is_same<Seqs, AppendSeqs>::value) {
+    b += sq.first;
+    r0 = sq.cu[blockIdx.x];
+    n = sq.cu[blockIdx.x + 1] - r0;
+  }
   const int have = held(c, b), seen = c.seen[b];
   __syncthreads();  // all waves have the lengths
   if (threadIdx.x == 0 && n > 0) {
@@ -747,12 +752,11 @@ __global__ __launch_bounds__(256) void evict_move(CacheArgs c, EvictSpace ws) {
 template <typename T>
 hipError_t launch_cache_append(const CacheArgs& c, const AppendArgs& a, const int32_t* cu_host,
                                hipStream_t s) {
-  AppendSeqs sq;
   if (!cu_host) {
-    sq.n = 0;
-    append_few<T, false><<<c.B, 256, 0, s>>>(c, a, sq);
+    append_few<T><<<c.B, 256, 0, s>>>(c, a, OneRowEach{});
     return hipGetLastError();
   }
+  AppendSeqs sq;
   for (int f = 0; f < c.B; f += APPEND_SEQS) {
     sq.first = f;
     sq.n = std::min(c.B - f, APPEND_SEQS);
@@ -762,7 +766,7 @@ hipError_t launch_cache_append(const CacheArgs& c, const AppendArgs& a, const in
     for (int i = 0; i < sq.n; i++) most = std::max(most, sq.cu[i + 1] - sq.cu[i]);
     if (rows == 0) continue;
     if (most <= APPEND_FEW) {
-      append_few<T, true><<<sq.n, 256, 0, s>>>(c, a, sq);
+      append_few<T><<<sq.n, 256, 0, s>>>(c, a, sq);
     } else {
       append_many<T><<<(rows + 3) / 4, 256, 0, s>>>(c, a, sq);
       append_lengths<<<(sq.n + 255) / 256, 256, 0, s>>>(c, sq);

@@ -193,36 +193,83 @@ def topk_compact(x, size, origin, cu, keep_ratio, scores=None, heads=1, prune_w=
 
 
 # ------------------------------------------- long sequences, token caches --
+# (the host's part of a small call is longer than the kernels': the helpers
+# below ask torch for as little as they can)
 _PREC = {torch.bfloat16: 1, torch.float32: 0}
+_PIECE = {torch.bfloat16: 7, torch.float32: 3}  # strides are multiples of one more
+_STREAMS = {}
+
+
+def _current(dev, *used):
+    """Handle of the current stream of GPU `dev`, with `used` recorded on it.
+    torch.cuda.current_stream makes an object, which takes 2.6 us; here each
+    stream's is made once."""
+    raw = torch._C._cuda_getCurrentRawStream(dev)
+    s = _STREAMS.get((dev, raw))
+    if s is None:
+        s = _STREAMS[dev, raw] = torch.cuda.current_stream(dev)
+    for t in used:
+        if t is not None:
+            t.record_stream(s)
+    return raw
 
 
 def _heads(t, name, dtype, heads, dh):
     """Checks a [rows, heads, dh] tensor of any row and head strides in whole
-    16-byte pieces; returns the two strides."""
-    if not isinstance(t, torch.Tensor) or t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dh:
+    16-byte pieces; returns its address and the two strides."""
+    shape = t.shape if isinstance(t, torch.Tensor) else ()
+    if len(shape) != 3 or shape[1] != heads or shape[2] != dh:
         raise ValueError(f"{name} must be a tensor [rows, {heads}, {dh}]")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype}")
     if t.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{name} requires a gradient, and none is computed: detach it")
     row, head, one = t.stride()
-    if one != 1 or (row | head) * t.element_size() % 16 or t.data_ptr() % 16:
+    p = t.data_ptr()
+    if one != 1 or (row | head) & _PIECE[dtype] or p & 15:
         raise ValueError(f"{name} must have contiguous heads, and strides and a base in whole "
                          "16-byte pieces")
-    return row, head
+    return p, row, head
 
 
 def _here(*tensors):
-    """All tensors on the current GPU, whose current stream the call uses."""
+    """The current GPU, whose current stream the call uses; all tensors are on
+    it."""
     dev = torch.cuda.current_device()
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise ValueError(f"tensors must be on the current GPU (cuda:{dev}), got {t.device}")
+    return dev
+
+
+def _offsets(cu):
+    """Host row offsets as int32 and their address (the library checks their
+    order)."""
+    a = cu if isinstance(cu, np.ndarray) else np.asarray(cu)
+    if a.ndim != 1 or len(a) < 2 or a.dtype.kind not in "iu":
+        raise ValueError("offsets must be [batch + 1] whole numbers")
+    if a.dtype != np.int32:
+        if a.min() < 0 or a.max() > 1 << 30:
+            raise ValueError("offsets must be in 0 .. 2^30")
+        a = a.astype(np.int32)
+    if not (a.flags.c_contiguous and a.flags.writeable):
+        a = a.copy()
+    return a, ctypes.addressof(ctypes.c_char.from_buffer(a))
+
+
+def _count(v, name, lowest=0):
+    """A whole number, at most 2^30 (no sequence is longer)."""
+    if int(v) != v or v < lowest:
+        raise ValueError(f"{name} must be a whole number, at least {lowest}")
+    return min(int(v), 1 << 30)
+
+
+_Strides2, _Strides4, _Strides6 = (ctypes.c_int64 * n for n in (2, 4, 6))
 
 
 def _out(out, rows, heads, dh, like):
     if out is None:
-        return torch.empty((rows, heads, dh), dtype=like.dtype, device=like.device)
+        return like.new_empty((rows, heads, dh))
     _need(out, "out", like.dtype)
     if tuple(out.shape) != (rows, heads, dh) or out.data_ptr() % 16:
         raise ValueError(f"out must be a 16-byte aligned tensor [{rows}, {heads}, {dh}]")
@@ -261,16 +308,16 @@ def window_attention(q, k, v, cu, window=None, sinks=0, causal=True, size=None, 
         raise ValueError("q must be a bfloat16 or float32 tensor [rows, heads, dh]")
     M, heads, dh = q.shape
     kv_heads = k.shape[1] if isinstance(k, torch.Tensor) and k.dim() == 3 else 0
-    strides = (ctypes.c_int64 * 6)(*_heads(q, "q", q.dtype, heads, dh),
-                                   *_heads(k, "k", q.dtype, kv_heads, dh),
-                                   *_heads(v, "v", q.dtype, kv_heads, dh))
+    qp, q_row, q_head = _heads(q, "q", q.dtype, heads, dh)
+    kp, k_row, k_head = _heads(k, "k", q.dtype, kv_heads, dh)
+    vp, v_row, v_head = _heads(v, "v", q.dtype, kv_heads, dh)
     if k.shape[0] != M or v.shape[0] != M:
         raise ValueError("q, k and v must have the same rows")
     if size is not None:
         _need(size, "size", torch.float32)
         if tuple(size.shape) != (M,):
             raise ValueError("one size per row")
-    _here(q, k, v, size)
+    dev = _here(q, k, v, size)
     cu_h, cu_p = _offsets(cu)
     if cu_h[-1] > M:
         raise ValueError("offsets must end within the rows")
@@ -281,9 +328,9 @@ def window_attention(q, k, v, cu, window=None, sinks=0, causal=True, size=None, 
     if fresh and rows < M:
         out[max(rows, 0):].zero_()
     check(_native.lib().fusion_window_attention(
-        _PREC[q.dtype], q.data_ptr(), k.data_ptr(), v.data_ptr(), strides, _ptr(size), cu_p,
-        len(cu_h) - 1, heads, kv_heads, dh, window, _count(sinks, "sinks"), int(bool(causal)),
-        out.data_ptr(), _stream(q, k, v, size, out)))
+        _PREC[q.dtype], qp, kp, vp, _Strides6(q_row, q_head, k_row, k_head, v_row, v_head),
+        _ptr(size), cu_p, len(cu_h) - 1, heads, kv_heads, dh, window, _count(sinks, "sinks"),
+        1 if causal else 0, out.data_ptr(), _current(dev, q, k, v, size, None if fresh else out)))
     return out
 
 
@@ -370,28 +417,29 @@ class TokenCache:
             self._space[key] = n
         return self._space[key]
 
-    def _ready(self, entry=None, *args):
-        """(stream, workspace, its bytes) of a call; the cache's tensors are
-        recorded on each stream once, which holds until they are freed."""
+    def _ready(self, *used):
+        """Handle of the current stream, with the caller's tensors recorded on
+        it; the cache's own are recorded on each stream once, which holds
+        until they are freed."""
         if torch.cuda.current_device() != self._index:
             raise ValueError(f"the cache is on {self.device}, not on the current GPU")
-        s = torch.cuda.current_stream()
-        if s.cuda_stream not in self._streams:
-            for t in self._tensors:
-                t.record_stream(s)
-            self._streams.add(s.cuda_stream)
-        if entry is None:
-            return s, None, 0
+        raw = _current(self._index, *used)
+        if raw not in self._streams:
+            _current(self._index, *self._tensors)
+            self._streams.add(raw)
+        return raw
+
+    def _workspace(self, entry, *args):
         n = self._bytes(entry, *args)
-        return s, torch.empty(n, dtype=torch.uint8, device=self.device), n
+        return torch.empty(n, dtype=torch.uint8, device=self.device), n
 
 
 def cache_append(cache, k, v, cu=None):
     """Append key and value rows [rows, kv_heads, dh]: one per sequence, or
     rows cu[i] .. cu[i+1]-1 to sequence i (cu: host offsets).  Their weight
     starts at 0; rows past a sequence's capacity are dropped."""
-    strides = (ctypes.c_int64 * 4)(*_heads(k, "k", cache.dtype, cache.kv_heads, cache.dh),
-                                   *_heads(v, "v", cache.dtype, cache.kv_heads, cache.dh))
+    kp, k_row, k_head = _heads(k, "k", cache.dtype, cache.kv_heads, cache.dh)
+    vp, v_row, v_head = _heads(v, "v", cache.dtype, cache.kv_heads, cache.dh)
     _here(k, v)
     cu_p = None
     if cu is not None:
@@ -401,11 +449,9 @@ def cache_append(cache, k, v, cu=None):
     rows = cache.batch if cu is None else int(cu_h[-1])
     if k.shape[0] != rows or v.shape[0] != rows:
         raise ValueError("rows do not match the sequences")
-    s, _, _ = cache._ready()
-    k.record_stream(s)
-    v.record_stream(s)
-    check(_native.lib().fusion_cache_append(cache._ref, k.data_ptr(), v.data_ptr(), strides, cu_p,
-                                            s.cuda_stream))
+    check(_native.lib().fusion_cache_append(cache._ref, kp, vp,
+                                            _Strides4(k_row, k_head, v_row, v_head), cu_p,
+                                            cache._ready(k, v)))
 
 
 def paged_attention(q, cache, window=None, sinks=0, accumulate=True, out=None):
@@ -417,17 +463,17 @@ def paged_attention(q, cache, window=None, sinks=0, accumulate=True, out=None):
     if not isinstance(q, torch.Tensor) or q.dim() != 3 or q.shape[0] != cache.batch:
         raise ValueError("q must be a tensor [batch, heads, dh]")
     heads = q.shape[1]
-    strides = (ctypes.c_int64 * 2)(*_heads(q, "q", cache.dtype, heads, cache.dh))
+    qp, q_row, q_head = _heads(q, "q", cache.dtype, heads, cache.dh)
     window = 0 if window is None else _count(window, "window", 1)
     _here(q)
+    fresh = out is None
     out = _out(out, cache.batch, heads, cache.dh, q)
-    acc = int(bool(accumulate))
-    s, ws, n = cache._ready("fusion_paged_attention_workspace_bytes", heads, acc)
-    q.record_stream(s)
-    out.record_stream(s)
+    acc = 1 if accumulate else 0
+    stream = cache._ready(q, None if fresh else out)
+    ws, n = cache._workspace("fusion_paged_attention_workspace_bytes", heads, acc)
     check(_native.lib().fusion_paged_attention(
-        cache._ref, q.data_ptr(), strides, heads, window, _count(sinks, "sinks"), acc,
-        out.data_ptr(), ws.data_ptr(), n, s.cuda_stream))
+        cache._ref, qp, _Strides2(q_row, q_head), heads, window, _count(sinks, "sinks"), acc,
+        out.data_ptr(), ws.data_ptr(), n, stream))
     return out
 
 
@@ -440,8 +486,9 @@ def cache_evict(cache, budget, sinks=0, recent=0):
     recent = _count(recent, "recent")
     if sinks + recent > budget:
         raise ValueError("sinks and recent do not fit the budget")
-    s, ws, n = cache._ready("fusion_cache_evict_workspace_bytes", budget)
+    stream = cache._ready()
+    ws, n = cache._workspace("fusion_cache_evict_workspace_bytes", budget)
     src = torch.empty((cache.batch, budget), dtype=torch.int32, device=cache.device)
     check(_native.lib().fusion_cache_evict(cache._ref, budget, sinks, recent, src.data_ptr(),
-                                           ws.data_ptr(), n, s.cuda_stream))
+                                           ws.data_ptr(), n, stream))
     return src

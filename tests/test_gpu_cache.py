@@ -198,7 +198,7 @@ def test_window_attention_strides_out_and_padding(torch_cuda):
     assert kern.window_attention(q[:0], k[:0], v[:0], [0, 0, 0]).shape == (0, 4, 64)
 
 
-@pytest.mark.parametrize("B", [447, 448, 449, 1000])
+@pytest.mark.parametrize("B", [127, 128, 129, 256, 448, 1000])
 def test_window_attention_many_samples(torch_cuda, B):
     """More samples than one launch describes."""
     torch = torch_cuda
@@ -432,6 +432,29 @@ def test_cache_append(torch_cuda, dtype, counts):
     _kern().cache_append(c, k, v, cu)
     for x in state:
         assert np.array_equal(_np(getattr(c, x)), state[x]), x
+
+
+@pytest.mark.parametrize("B,most", [(255, 8), (256, 9), (257, 8), (600, 20)])
+def test_cache_append_many_sequences(torch_cuda, B, most):
+    """More sequences than one launch describes, few rows each or more."""
+    torch = torch_cuda
+    rng = np.random.default_rng(B)
+    n = rng.integers(0, most + 1, size=B)
+    n[3] = most
+    lengths = rng.integers(0, 12, size=B)
+    c = _cache(torch, rng, "bf16", lengths, 1, 16, 16, 32, seen=lengths + 5)
+    k, v = (_normal(torch, rng, "bf16", int(n.sum()), 1, 16) for _ in range(2))
+    cu = np.concatenate([[0], np.cumsum(n)])
+    _kern().cache_append(c, k, v, cu)
+    assert np.array_equal(c.length.cpu().numpy(), lengths + n)
+    assert np.array_equal(c.seen.cpu().numpy(), lengths + 5 + n)
+    pos, w = c.pos.cpu().numpy(), c.weight.cpu().numpy()
+    for b in range(B):
+        new = slice(lengths[b], lengths[b] + n[b])
+        kc, vc, _ = _rows(c, b, int(lengths[b] + n[b]))
+        assert np.array_equal(kc[new], _np(k[cu[b]:cu[b + 1]]))
+        assert np.array_equal(vc[new], _np(v[cu[b]:cu[b + 1]]))
+        assert np.array_equal(pos[b, new], lengths[b] + 5 + np.arange(n[b])) and not w[b, new].any()
 
 
 def _evict_ref(length, seen, weight, pos, cap, budget, sinks, recent):
