@@ -140,8 +140,7 @@ __global__ __launch_bounds__(256) void append_lengths(CacheArgs c, AppendSeqs sq
 //
 // Each part of a sequence leaves its maximum, sum and unnormalised output;
 // paged_join adds the parts up and turns the scores, kept in fp32, into the
-// weight that every token drew.  P is rounded to bf16 before it multiplies V
-// (the matrix operand's type), nothing else is until the output.
+// weight that every token drew.
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
@@ -187,7 +186,7 @@ __device__ __forceinline__ Visible visible(const CacheArgs& c, const PagedArgs& 
 }
 
 template <typename T, int DP, bool PAD, bool ACC>
-__global__ __launch_bounds__(256) void paged_attention(CacheArgs c, PagedArgs a, PagedSpace ws) {
+__global__ __launch_bounds__(256, 2) void paged_attention(CacheArgs c, PagedArgs a, PagedSpace ws) {
   constexpr bool BF = sizeof(T) == 2;
   constexpr int KT = BF ? 32 : 16, NSUB = KT / 16;
   constexpr int EPP = 16 / sizeof(T);       // values per 16-byte piece
@@ -225,60 +224,77 @@ __global__ __launch_bounds__(256) void paged_attention(CacheArgs c, PagedArgs a,
     const int* pos = vis.oldest == INT32_MIN ? table : c.pos + (int64_t)b * c.cap;
     const bool by_pos = vis.oldest != INT32_MIN;
     // page, place and position of the lane's tokens of a tile
-    int page[NSUB], place[NSUB], at[NSUB];
+    struct Tokens {
+      int page[NSUB], place[NSUB], at[NSUB];
+    };
     auto look_up = [&](int t) {
+      Tokens k;
 #pragma unroll
       for (int u = 0; u < NSUB; u++) {
         const int x = vis.slot(min(t * KT + 16 * u + cl, vis.nv - 1));
         const uint32_t pg = quot((uint32_t)x, c.page);
-        page[u] = table[pg];
-        place[u] = x - (int)(pg * c.page.d);
-        at[u] = pos[by_pos ? (uint32_t)x : pg];
+        k.page[u] = table[pg];
+        k.place[u] = x - (int)(pg * c.page.d);
+        k.at[u] = pos[by_pos ? (uint32_t)x : pg];
       }
+      return k;
     };
     // keys and values of the lane's tokens; hidden ones read the cache's first row
     uint4 kr[NSUB][NL], vr[NSUB][NL];
     uint32_t mask_next;  // visible tokens of the tile, one bit each
     bool see[NSUB];
-    auto load_kv = [&](int t) {
+    const T* kp[NSUB];
+    const T* vp[NSUB];
+    auto point = [&](int t, const Tokens& tk) {
       mask_next = 0;
-      int64_t p[NSUB], r[NSUB];
 #pragma unroll
       for (int u = 0; u < NSUB; u++) {
-        see[u] = (t * KT + 16 * u + cl < vis.nv) & ((unsigned)page[u] < (unsigned)c.pages) &
-                 ((at[u] >= vis.oldest) | (at[u] < a.sinks));
+        see[u] = (t * KT + 16 * u + cl < vis.nv) & ((unsigned)tk.page[u] < (unsigned)c.pages) &
+                 ((tk.at[u] >= vis.oldest) | (tk.at[u] < a.sinks));
         mask_next |= (uint32_t)(__ballot(see[u]) & 0xFFFF) << (16 * u);
-        p[u] = see[u] ? page[u] : 0;
-        r[u] = see[u] ? place[u] : 0;
+        const int64_t p = see[u] ? tk.page[u] : 0, r = see[u] ? tk.place[u] : 0;
+        kp[u] = (const T*)c.k + p * c.k_page + r * c.k_row + kh * c.k_head;
+        vp[u] = (const T*)c.v + p * c.v_page + r * c.v_row + kh * c.v_head;
       }
+    };
+    auto load_kv = [&]() {
 #pragma unroll
-      for (int u = 0; u < NSUB; u++) {
-        const T* k = (const T*)c.k + p[u] * c.k_page + r[u] * c.k_row + kh * c.k_head;
+      for (int u = 0; u < NSUB; u++)
 #pragma unroll
         for (int s = 0; s < NL; s++) {
           const int d = (4 * s + g) * EPP;
           kr[u][s] = make_uint4(0, 0, 0, 0);
-          if (!PAD || d < dh) kr[u][s] = *(const uint4*)(k + d);
+          if (!PAD || d < dh) kr[u][s] = *(const uint4*)(kp[u] + d);
         }
-      }
 #pragma unroll
-      for (int u = 0; u < NSUB; u++) {
-        const T* v = (const T*)c.v + p[u] * c.v_page + r[u] * c.v_row + kh * c.v_head;
+      for (int u = 0; u < NSUB; u++)
 #pragma unroll
         for (int s = 0; s < NL; s++) {
           const int d = (4 * s + g) * EPP;
           vr[u][s] = make_uint4(0, 0, 0, 0);
-          if (!PAD || d < dh) vr[u][s] = *(const uint4*)(v + d);
+          if (!PAD || d < dh) vr[u][s] = *(const uint4*)(vp[u] + d);
         }
-      }
     };
     float m = -INFINITY, l = 0.f;
     f32x4_t O[ND];
 #pragma unroll
     for (int d = 0; d < ND; d++) O[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    // one tile, in straight line but for the rescaling, so that the waits for
-    // loads can be counted; LAST: no tile follows
-    auto tile = [&](int t, auto last_c) {
+    // Scores of a tile to the workspace, `n` of the unit's heads (rows past
+    // them are past the buffer's end and dropped).
+    auto store_scores = [&](int t, const f32x4_t* S, int n) {
+      const auto rows = __builtin_amdgcn_make_buffer_rsrc(
+          ws.score + (((int64_t)b * ws.tiles + t) * a.H + h0) * KT, 0, n * KT * 4, 0x00027000);
+#pragma unroll
+      for (int u = 0; u < NSUB; u++)
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, S[u]), rows,
+                                               (cl * KT + 16 * u + 4 * g) * 4, 0, 0);
+    };
+    // One tile in straight line, with its memory operations in a fixed order
+    // (look-ups two tiles ahead, the next tile's keys, its values, this tile's
+    // scores), so that each wait counts exactly the operations after the one
+    // it needs: with a branch or another order every tile waited for its
+    // stores too (2 x 131,072 tokens, 32 heads: XXX us).  LAST: no tile follows.
+    auto tile = [&](int t, Tokens& ahead, auto last_c) {
       constexpr bool LAST = decltype(last_c)::value;
       const uint32_t mask = mask_next;
       f32x4_t S[NSUB];
@@ -315,8 +331,11 @@ __global__ __launch_bounds__(256) void paged_attention(CacheArgs c, PagedArgs a,
         }
       __builtin_amdgcn_sched_barrier(0);
       if constexpr (!LAST) {
-        load_kv(t + 1);
-        look_up(min(t + 2, tb - 1));
+        point(t + 1, ahead);
+        __builtin_amdgcn_sched_barrier(0);
+        ahead = look_up(min(t + 2, tb - 1));
+        __builtin_amdgcn_sched_barrier(0);
+        load_kv();
       }
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -324,31 +343,19 @@ __global__ __launch_bounds__(256) void paged_attention(CacheArgs c, PagedArgs a,
 #pragma unroll
         for (int j = 0; j < 4; j++)
           S[u][j] = mask >> (16 * u + 4 * g + j) & 1 ? S[u][j] * sc2 : -INFINITY;
-      if constexpr (ACC) {
-        // rows past the unit's heads are past the buffer's end and dropped
-        // (a branch around the store would have the next tile's loads waited
-        // for together with it)
-        const auto rows = __builtin_amdgcn_make_buffer_rsrc(
-            ws.score + (((int64_t)b * ws.tiles + t) * a.H + h0) * KT, 0, nq * KT * 4, 0x00027000);
-#pragma unroll
-        for (int u = 0; u < NSUB; u++)
-          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, S[u]), rows,
-                                                 (cl * KT + 16 * u + 4 * g) * 4, 0, 0);
-      }
+      if constexpr (ACC) store_scores(t, S, nq);
       float mt = fmaxf(fmaxf(S[0][0], S[0][1]), fmaxf(S[0][2], S[0][3]));
       if (NSUB > 1)
         mt = fmaxf(mt, fmaxf(fmaxf(S[NSUB - 1][0], S[NSUB - 1][1]), fmaxf(S[NSUB - 1][2], S[NSUB - 1][3])));
       mt = max_xor32(max_xor16(mt));
       const bool grow = mt > m + 8.f;
-      if (__any(grow)) {
-        const float f = grow ? __builtin_amdgcn_exp2f(m - mt) : 1.f;
-        if (grow) m = mt;
-        l *= f;
+      const float f = grow ? __builtin_amdgcn_exp2f(m - mt) : 1.f;
+      m = grow ? mt : m;
+      l *= f;
 #pragma unroll
-        for (int d = 0; d < ND; d++)
+      for (int d = 0; d < ND; d++)
 #pragma unroll
-          for (int j = 0; j < 4; j++) O[d][j] *= f;
-      }
+        for (int j = 0; j < 4; j++) O[d][j] *= f;
       const float mu = m == -INFINITY ? 0.f : m;
 #pragma unroll
       for (int u = 0; u < NSUB; u++) {
@@ -357,11 +364,16 @@ __global__ __launch_bounds__(256) void paged_attention(CacheArgs c, PagedArgs a,
         l += (S[u][0] + S[u][1]) + (S[u][2] + S[u][3]);
       }
       if constexpr (BF) {
-        union { uint32_t u[4]; bf16x8_t v; } p;
-        p.u[0] = pack_bf16x2(S[0][0], S[0][1]);
-        p.u[1] = pack_bf16x2(S[0][2], S[0][3]);
-        p.u[2] = pack_bf16x2(S[NSUB - 1][0], S[NSUB - 1][1]);
-        p.u[3] = pack_bf16x2(S[NSUB - 1][2], S[NSUB - 1][3]);
+        // P as the sum of two bf16 numbers, 16 bits of precision: the second
+        // product costs nothing beside the loads
+        union { uint32_t u[4]; bf16x8_t v; } p, p2;
+#pragma unroll
+        for (int w = 0; w < 4; w++) {
+          const float e0 = S[w / 2 * (NSUB - 1)][w % 2 * 2], e1 = S[w / 2 * (NSUB - 1)][w % 2 * 2 + 1];
+          p.u[w] = pack_bf16x2(e0, e1);
+          p2.u[w] = pack_bf16x2(e0 - __uint_as_float(p.u[w] << 16),
+                                e1 - __uint_as_float(p.u[w] & 0xFFFF0000u));
+        }
         // V^T: dims 16 d + cl, tokens 4g .. + 3 and 16 + 4g .. + 3
 #pragma unroll
         for (int d = 0; d < ND; d++) {
@@ -374,6 +386,7 @@ __global__ __launch_bounds__(256) void paged_attention(CacheArgs c, PagedArgs a,
                     Vs + r * VROW + ((d ^ (r & (DP / 16 - 1))) << 5) + ((cl & 3) << 3)));
           }
           O[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.v, p.v, O[d], 0, 0, 0);
+          O[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.v, p2.v, O[d], 0, 0, 0);
         }
       } else {
 #pragma unroll
@@ -384,11 +397,17 @@ __global__ __launch_bounds__(256) void paged_attention(CacheArgs c, PagedArgs a,
                 *(const float*)(Vs + (4 * g + j) * VROW + (16 * d + cl) * 4), S[0][j], O[d], 0, 0, 0);
       }
     };
-    look_up(ta);
-    load_kv(ta);
-    look_up(min(ta + 1, tb - 1));
-    for (int t = ta; t < tb - 1; t++) tile(t, std::false_type{});
-    tile(tb - 1, std::true_type{});
+    Tokens ahead = look_up(ta);
+    point(ta, ahead);
+    ahead = look_up(min(ta + 1, tb - 1));
+    load_kv();
+    if constexpr (ACC) {
+      // (stores of nothing, so that the first tile finds as many as the others)
+      const f32x4_t none[2] = {};
+      store_scores(ta, none, 0);
+    }
+    for (int t = ta; t < tb - 1; t++) tile(t, ahead, std::false_type{});
+    tile(tb - 1, ahead, std::true_type{});
     l = sum_xor32(sum_xor16(l));
     if (cl < nq) {
       const int64_t o = (int64_t)part * a.H + h0 + cl;
