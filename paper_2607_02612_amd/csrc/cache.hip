@@ -148,15 +148,20 @@ typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int PAGED_SPLIT = 1024;  // sequences up to which the work is split over their lengths
-constexpr int PAGED_WAVES = 2048;  // parts in all, about
+// Parts in all, about: the waves that the registers let run at once (64-wide
+// heads: 64 sequences of 4,096 tokens, 12 heads 158 us, with 2,048 parts 162,
+// with 4,096 164).
+constexpr int PAGED_WAVES = 2048, PAGED_WAVES_64 = 3072;
+
+constexpr int SCORE_BYTES = 2048;   // scores that a wave holds back in LDS: a tile of 16 heads
 
 struct PagedSpace {
   int2* plan;    // [B]: first part, number of parts
   float2* ml;    // [parts][H]: maximum (base 2), sum
   float* o;      // [parts][H][DP]
-  float* score;  // [B][tiles][H][KT], base 2, by visible token
+  float* score;  // [B][units][tiles][heads][KT], base 2, by visible token
   int ranges;    // parts per unit
-  int units, qtiles, tiles;
+  int units, qtiles, tiles, heads;  // (heads of a unit, at most 16)
 };
 
 // The visible tokens of a sequence: x-th visible token -> slot.  In a cache
@@ -194,11 +199,13 @@ __global__ __launch_bounds__(256, 2) void paged_attention(CacheArgs c, PagedArgs
   constexpr int ND = DP / 16;
   constexpr int VROW = BF ? DP * 2 : (DP + 4) * 4;  // bytes of a token's values in LDS
   __shared__ __attribute__((aligned(16))) char v_all[4 * KT * VROW];
+  __shared__ __attribute__((aligned(16))) char s_all[ACC ? 4 * SCORE_BYTES : 16];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int g = lane >> 4, cl = lane & 15;
   const int id = blockIdx.x * 4 + wave, unit = id % ws.units, range = id / ws.units;
   if (range >= ws.ranges) return;
   char* Vs = v_all + wave * KT * VROW;
+  char* Ss = s_all + (ACC ? wave * SCORE_BYTES : 0);
   const int kh = unit / ws.qtiles, qt = unit % ws.qtiles;
   const int h0 = kh * a.group + qt * 16, nq = min(16, a.group - qt * 16);
   const int dh = c.dh;
@@ -279,21 +286,29 @@ __global__ __launch_bounds__(256, 2) void paged_attention(CacheArgs c, PagedArgs
     f32x4_t O[ND];
 #pragma unroll
     for (int d = 0; d < ND; d++) O[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    // Scores of a tile to the workspace, `n` of the unit's heads (rows past
-    // them are past the buffer's end and dropped).
-    auto store_scores = [&](int t, const f32x4_t* S, int n) {
-      const auto rows = __builtin_amdgcn_make_buffer_rsrc(
-          ws.score + (((int64_t)b * ws.tiles + t) * a.H + h0) * KT, 0, n * KT * 4, 0x00027000);
+    // Scores wait in LDS until they fill SCORE_BYTES and then leave in whole
+    // 1-KB stores (64 sequences of 4,096 tokens, one head a unit: 158 us; with
+    // a store for each tile's row 166; with 4 heads a unit both 220, of which
+    // the bytes written, 33 MB beside 1.07 GB read, are 30).
+    const int row_shift = 32 - __builtin_clz(2 * nq - 1);  // rows of a tile in LDS: 1 << row_shift >= nq
+    const int tile_shift = row_shift - 1 + (BF ? 7 : 6);   // bytes of a tile
+    const int slots = SCORE_BYTES >> tile_shift;
+    int held_from = ta;
+    auto store_scores = [&](int t) {  // tiles held_from .. t
 #pragma unroll
-      for (int u = 0; u < NSUB; u++)
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, S[u]), rows,
-                                               (cl * KT + 16 * u + 4 * g) * 4, 0, 0);
+      for (int i = 0; i < SCORE_BYTES / 1024; i++) {
+        const int at = (i * 64 + lane) * 16, x = held_from + (at >> tile_shift);
+        const int in = at & ((1 << tile_shift) - 1);
+        if (x <= t && in < nq * KT * 4)
+          *(uint4*)((char*)(ws.score + (((int64_t)b * ws.units + unit) * ws.tiles + x) * ws.heads * KT) +
+                    in) = *(const uint4*)(Ss + at);
+      }
+      held_from = t + 1;
     };
     // One tile in straight line, with its memory operations in a fixed order
-    // (look-ups two tiles ahead, the next tile's keys, its values, this tile's
-    // scores), so that each wait counts exactly the operations after the one
-    // it needs: with a branch or another order every tile waited for its
-    // stores too (2 x 131,072 tokens, 32 heads: XXX us).  LAST: no tile follows.
+    // (look-ups two tiles ahead, the next tile's keys, its values, scores now
+    // and then), so that each wait counts the operations after the one it
+    // needs.  LAST: no tile follows.
     auto tile = [&](int t, Tokens& ahead, auto last_c) {
       constexpr bool LAST = decltype(last_c)::value;
       const uint32_t mask = mask_next;
@@ -343,7 +358,14 @@ __global__ __launch_bounds__(256, 2) void paged_attention(CacheArgs c, PagedArgs
 #pragma unroll
         for (int j = 0; j < 4; j++)
           S[u][j] = mask >> (16 * u + 4 * g + j) & 1 ? S[u][j] * sc2 : -INFINITY;
-      if constexpr (ACC) store_scores(t, S, nq);
+      if constexpr (ACC) {
+        if (cl < nq) {
+#pragma unroll
+          for (int u = 0; u < NSUB; u++)
+            *(f32x4_t*)(Ss + ((t - held_from) << tile_shift) + (cl * KT + 16 * u + 4 * g) * 4) = S[u];
+        }
+        if (LAST || t - held_from == slots - 1) store_scores(t);
+      }
       float mt = fmaxf(fmaxf(S[0][0], S[0][1]), fmaxf(S[0][2], S[0][3]));
       if (NSUB > 1)
         mt = fmaxf(mt, fmaxf(fmaxf(S[NSUB - 1][0], S[NSUB - 1][1]), fmaxf(S[NSUB - 1][2], S[NSUB - 1][3])));
@@ -401,11 +423,6 @@ __global__ __launch_bounds__(256, 2) void paged_attention(CacheArgs c, PagedArgs
     point(ta, ahead);
     ahead = look_up(min(ta + 1, tb - 1));
     load_kv();
-    if constexpr (ACC) {
-      // (stores of nothing, so that the first tile finds as many as the others)
-      const f32x4_t none[2] = {};
-      store_scores(ta, none, 0);
-    }
     for (int t = ta; t < tb - 1; t++) tile(t, ahead, std::false_type{});
     tile(tb - 1, ahead, std::true_type{});
     l = sum_xor32(sum_xor16(l));
@@ -449,45 +466,55 @@ __global__ __launch_bounds__(256, 2) void paged_attention(CacheArgs c, PagedArgs
   }
 }
 
-// The parts of every sequence joined: the first workgroups write the output
-// rows, four each (4 waves a row), the others add the weights of 1024 visible
-// tokens of a sequence: 4 tokens a lane, a fourth of the heads a wave, summed
-// over the waves in order.  Loads go out JOIN_AHEAD at a time, since a
-// sequence of the chip alone has hundreds of parts (two of 131,072 tokens took
-// 37 us with one row of parts after the other).
+// The parts of every sequence joined: the first workgroups add the weights of
+// 1024 visible tokens of a sequence each (4 tokens a lane, a fourth of the
+// heads a wave, summed over the waves in order), the others write the output
+// rows, `wpr` waves a row.  Bound by a chain of dependent loads, so they go out
+// JOIN_AHEAD at a time, the scores before the statistics that they wait for:
+// one stream alone has hundreds of parts (two of 131,072 tokens took 37 us with
+// one part after the other, 23 with the statistics first).
 constexpr int JOIN_HEADS = 128;
-constexpr int JOIN_AHEAD = 8;
+constexpr int JOIN_AHEAD = 4;  // (8 leave registers for one workgroup a CU: 17.5 us instead of 13.2)
+// (maximum, sum) of two parts
+__device__ __forceinline__ float2 join_ml(float2 a, float2 b) {
+  const float m = fmaxf(a.x, b.x), mu = m == -INFINITY ? 0.f : m;
+  return make_float2(m, a.y * __builtin_amdgcn_exp2f(a.x - mu) + b.y * __builtin_amdgcn_exp2f(b.x - mu));
+}
+
 template <typename T, int DP>
-__global__ __launch_bounds__(1024) void paged_join(CacheArgs c, PagedArgs a, PagedSpace ws,
-                                                   int rows, int chunks) {
+__global__ __launch_bounds__(1024, 8) void paged_join(CacheArgs c, PagedArgs a, PagedSpace ws,
+                                                   int weights, int chunks, int wpr) {
   constexpr int KT = sizeof(T) == 2 ? 32 : 16;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   __shared__ __attribute__((aligned(16))) float part[16][256];
   __shared__ float2 s_ml[JOIN_HEADS];
-  if (blockIdx.x < rows) {
-    const int64_t row = (int64_t)blockIdx.x * 4 + (wave >> 2);
+  if ((int)blockIdx.x >= weights) {
+    const int64_t row = ((int64_t)blockIdx.x - weights) * (16 / wpr) + wave / wpr;
     const bool real = row < (int64_t)c.B * a.H;
-    const int b = real ? (int)(row / a.H) : 0, h = real ? (int)(row % a.H) : 0, w4 = wave & 3;
+    const int b = real ? (int)(row / a.H) : 0, h = real ? (int)(row % a.H) : 0;
     const int2 plan = ws.plan[b];
-    float m = -INFINITY;
-    for (int i = lane; i < plan.y; i += 64)
-      m = fmaxf(m, ws.ml[(int64_t)(plan.x + i) * a.H + h].x);
-    m = wave_max(m);
-    const float mu = m == -INFINITY ? 0.f : m;
-    float o0 = 0.f, o1 = 0.f, l = 0.f;
-    for (int i = w4; i < plan.y; i += 4 * JOIN_AHEAD) {
+    float o0 = 0.f, o1 = 0.f, l = 0.f, m = -INFINITY;
+    for (int i = wave % wpr; i < plan.y; i += wpr * JOIN_AHEAD) {
       float2 ml[JOIN_AHEAD];
       float x0[JOIN_AHEAD], x1[JOIN_AHEAD];
+      float m2 = m;
 #pragma unroll
       for (int u = 0; u < JOIN_AHEAD; u++) {
-        const int64_t p = (int64_t)(plan.x + min(i + 4 * u, plan.y - 1)) * a.H + h;
+        const int64_t p = (int64_t)(plan.x + min(i + wpr * u, plan.y - 1)) * a.H + h;
         ml[u] = ws.ml[p];
         x0[u] = ws.o[p * DP + lane];
         x1[u] = DP > 64 ? ws.o[p * DP + 64 + lane] : 0.f;
       }
 #pragma unroll
+      for (int u = 0; u < JOIN_AHEAD; u++) m2 = fmaxf(m2, ml[u].x);
+      const float mu = m2 == -INFINITY ? 0.f : m2, f0 = __builtin_amdgcn_exp2f(m - mu);
+      l *= f0;
+      o0 *= f0;
+      o1 *= f0;
+      m = m2;
+#pragma unroll
       for (int u = 0; u < JOIN_AHEAD; u++) {
-        const float f = i + 4 * u < plan.y ? __builtin_amdgcn_exp2f(ml[u].x - mu) : 0.f;
+        const float f = i + wpr * u < plan.y ? __builtin_amdgcn_exp2f(ml[u].x - mu) : 0.f;
         l = fmaf(ml[u].y, f, l);
         o0 = fmaf(x0[u], f, o0);
         o1 = fmaf(x1[u], f, o1);
@@ -495,70 +522,81 @@ __global__ __launch_bounds__(1024) void paged_join(CacheArgs c, PagedArgs a, Pag
     }
     part[wave][lane] = o0;
     if (DP > 64) part[wave][64 + lane] = o1;
-    if (lane == 0) s_ml[wave].y = l;
+    if (lane == 0) s_ml[wave] = make_float2(m, l);
     __syncthreads();
-    const int d = tid & 255, w = wave & ~3;  // a row's first wave
-    l = (s_ml[w].y + s_ml[w + 1].y) + (s_ml[w + 2].y + s_ml[w + 3].y);
+    // the row's first waves join its parts
+    const int d = tid % (wpr * 64), w0 = wave / wpr * wpr;
     if (real && d < c.dh) {
-      const float o = (part[w][d] + part[w + 1][d]) + (part[w + 2][d] + part[w + 3][d]);
-      ((T*)a.out)[row * c.dh + d] = St<T>::put(l == 0.f ? 0.f : o / l);
+      float top = -INFINITY;
+      for (int w = 0; w < wpr; w++) top = fmaxf(top, s_ml[w0 + w].x);
+      top = top == -INFINITY ? 0.f : top;
+      float o = 0.f, sum = 0.f;
+      for (int w = 0; w < wpr; w++) {
+        const float f = __builtin_amdgcn_exp2f(s_ml[w0 + w].x - top);
+        sum = fmaf(s_ml[w0 + w].y, f, sum);
+        o = fmaf(part[w0 + w][d], f, o);
+      }
+      ((T*)a.out)[row * c.dh + d] = St<T>::put(sum == 0.f ? 0.f : o / sum);
     }
     return;
   }
-  const int64_t id = (int64_t)blockIdx.x - rows;
-  const int b = (int)(id / chunks), first = (int)(id % chunks) * 1024;
+  const int b = (int)(blockIdx.x / chunks), first = (int)(blockIdx.x % chunks) * 1024;
   const Visible vis = visible(c, a, b);
   if (first >= vis.nv) return;
   const int2 plan = ws.plan[b];
+  const int h0 = wave >> 2;  // the wave's heads: h0, h0 + 4, ..
+  // scores of 4 tokens from x on under JOIN_AHEAD of the wave's heads from h on
+  auto load_scores = [&](int x, int h, f32x4_t* s) {
+    const float* sp = ws.score + (int64_t)b * ws.units * ws.tiles * ws.heads * KT +
+                      (int64_t)(min(x, vis.nv - 1) / KT) * ws.heads * KT + x % KT;
+#pragma unroll
+    for (int u = 0; u < JOIN_AHEAD; u++) {
+      const int hu = min(h + 4 * u, a.H - 1), kh = hu / a.group, r = hu - kh * a.group;
+      s[u] = *(const f32x4_t*)(sp + ((int64_t)(kh * ws.qtiles + r / 16) * ws.tiles * ws.heads + r % 16) * KT);
+    }
+  };
   for (int hc = 0; hc < a.H; hc += JOIN_HEADS) {
     const int nh = min(JOIN_HEADS, a.H - hc);
+    f32x4_t s[JOIN_AHEAD];
+    load_scores(first + (wave & 3) * 256 + lane * 4, hc + h0, s);
     __syncthreads();
     // maximum and 1 / (sum H) of the heads, 32 lanes a head
     for (int h = tid >> 5; h < nh; h += 32) {
-      float m = -INFINITY, l = 0.f;
+      float2 t = make_float2(-INFINITY, 0.f);
       for (int i = tid & 31; i < plan.y; i += 32 * JOIN_AHEAD) {
         float2 ml[JOIN_AHEAD];
-        float m2 = m;
 #pragma unroll
         for (int u = 0; u < JOIN_AHEAD; u++) {
           ml[u] = ws.ml[(int64_t)(plan.x + min(i + 32 * u, plan.y - 1)) * a.H + hc + h];
           if (i + 32 * u >= plan.y) ml[u].x = -INFINITY;
         }
+        float m2 = t.x;
 #pragma unroll
         for (int u = 0; u < JOIN_AHEAD; u++) m2 = fmaxf(m2, ml[u].x);
-        if (m2 != -INFINITY) {
-          l *= __builtin_amdgcn_exp2f(m - m2);
+        const float mu = m2 == -INFINITY ? 0.f : m2;
+        t.y *= __builtin_amdgcn_exp2f(t.x - mu);
 #pragma unroll
-          for (int u = 0; u < JOIN_AHEAD; u++) l = fmaf(ml[u].y, __builtin_amdgcn_exp2f(ml[u].x - m2), l);
-        }
-        m = m2;
+        for (int u = 0; u < JOIN_AHEAD; u++)
+          t.y = fmaf(ml[u].y, __builtin_amdgcn_exp2f(ml[u].x - mu), t.y);
+        t.x = m2;
       }
-      for (int o = 16; o; o >>= 1) {
-        const float mo = __shfl_xor(m, o, 32), lo = __shfl_xor(l, o, 32), m2 = fmaxf(m, mo);
-        if (m2 != -INFINITY)
-          l = l * __builtin_amdgcn_exp2f(m - m2) + lo * __builtin_amdgcn_exp2f(mo - m2);
-        m = m2;
-      }
+      for (int o = 16; o; o >>= 1)
+        t = join_ml(t, make_float2(__shfl_xor(t.x, o, 32), __shfl_xor(t.y, o, 32)));
       if ((tid & 31) == 0)
-        s_ml[h] = make_float2(m == -INFINITY ? 0.f : m, l == 0.f ? 0.f : 1.f / (l * (float)a.H));
+        s_ml[h] = make_float2(t.x == -INFINITY ? 0.f : t.x, t.y == 0.f ? 0.f : 1.f / (t.y * (float)a.H));
     }
     __syncthreads();
     for (int x0 = first; x0 < vis.nv; x0 += chunks * 1024) {
-      const int x = x0 + (wave & 3) * 256 + lane * 4, h0 = wave >> 2;
+      const int x = x0 + (wave & 3) * 256 + lane * 4;
       f32x4_t w = {0.f, 0.f, 0.f, 0.f};
-      if (x < vis.nv) {
-        const float* sp = ws.score + (((int64_t)b * ws.tiles + x / KT) * a.H + hc) * KT + x % KT;
-        for (int h = h0; h < nh; h += 4 * JOIN_AHEAD) {
-          f32x4_t s[JOIN_AHEAD];
+      for (int h = h0; h < nh; h += 4 * JOIN_AHEAD) {
+        if (x0 != first || h != h0) load_scores(x, hc + h, s);
 #pragma unroll
-          for (int u = 0; u < JOIN_AHEAD; u++) s[u] = *(const f32x4_t*)(sp + min(h + 4 * u, nh - 1) * KT);
+        for (int u = 0; u < JOIN_AHEAD; u++) {
+          const float2 ml = s_ml[min(h + 4 * u, nh - 1)];
+          const float r = h + 4 * u < nh ? ml.y : 0.f;
 #pragma unroll
-          for (int u = 0; u < JOIN_AHEAD; u++) {
-            const float2 ml = s_ml[min(h + 4 * u, nh - 1)];
-            const float r = h + 4 * u < nh ? ml.y : 0.f;
-#pragma unroll
-            for (int j = 0; j < 4; j++) w[j] = fmaf(__builtin_amdgcn_exp2f(s[u][j] - ml.x), r, w[j]);
-          }
+          for (int j = 0; j < 4; j++) w[j] = fmaf(__builtin_amdgcn_exp2f(s[u][j] - ml.x), r, w[j]);
         }
       }
       *(f32x4_t*)&part[wave][lane * 4] = w;
@@ -808,8 +846,9 @@ size_t paged_space(const CacheArgs& c, int KT, int H, int accumulate, char* ws,
   p.qtiles = (group + 15) / 16;
   p.units = c.Hkv * p.qtiles;
   const bool split = c.B <= PAGED_SPLIT;
-  p.ranges = split ? std::max(1, PAGED_WAVES / p.units) : c.B;
+  p.ranges = split ? std::max(1, (DP == 64 ? PAGED_WAVES_64 : PAGED_WAVES) / p.units) : c.B;
   p.tiles = (c.cap + KT - 1) / KT;
+  p.heads = std::min(group, 16);
   const size_t parts = (size_t)p.ranges + (split ? c.B : 0);
   size_t n = 0;
   auto take = [&](size_t bytes) {
@@ -820,7 +859,7 @@ size_t paged_space(const CacheArgs& c, int KT, int H, int accumulate, char* ws,
   p.plan = (int2*)take((size_t)c.B * 8);
   p.ml = (float2*)take(parts * H * 8);
   p.o = (float*)take(parts * H * DP * 4);
-  p.score = (float*)take(accumulate ? (size_t)c.B * p.tiles * H * KT * 4 : 0);
+  p.score = (float*)take(accumulate ? (size_t)c.B * p.units * p.tiles * p.heads * KT * 4 : 0);
   if (space) *space = p;
   return n;
 }
@@ -835,9 +874,14 @@ hipError_t launch_paged(const CacheArgs& c, const PagedArgs& a, const PagedSpace
     paged_attention<T, DP, PAD, false><<<grid, 256, 0, s>>>(c, a, ws);
   if (hipError_t e = hipGetLastError()) return e;
   // (workgroups past a sequence's tokens leave at once)
-  const int rows = (int)(((int64_t)c.B * a.H + 3) / 4);
-  const int chunks = a.accumulate ? std::max(1, std::min((c.cap + 1023) / 1024, 16384 / c.B)) : 0;
-  paged_join<T, DP><<<(unsigned)(rows + (int64_t)c.B * chunks), 1024, 0, s>>>(c, a, ws, rows, chunks);
+  const int chunks = a.accumulate ? std::max(1, std::min((c.cap + 1023) / 1024, 16384 / c.B)) : 1;
+  const int weights = a.accumulate ? c.B * chunks : 0;
+  // waves a row: enough for the parts of an average sequence in one go, and
+  // two at least, since one sequence may have most of them
+  const int parts = c.B <= PAGED_SPLIT ? ws.ranges / c.B + 1 : 1;
+  const int wpr = parts <= 2 * JOIN_AHEAD ? 2 : parts <= 4 * JOIN_AHEAD ? 4 : 16;
+  const int64_t rows = ((int64_t)c.B * a.H * wpr + 15) / 16;
+  paged_join<T, DP><<<(unsigned)(weights + rows), 1024, 0, s>>>(c, a, ws, weights, chunks, wpr);
   return hipGetLastError();
 }
 constexpr int tile_tokens(size_t size) { return size == 2 ? 32 : 16; }
