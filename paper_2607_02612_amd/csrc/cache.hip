@@ -180,9 +180,9 @@ __device__ __forceinline__ Visible visible(const CacheArgs& c, const PagedArgs& 
   v.n = v.nv = held(c, b);
   const int seen = c.seen[b];
   v.head = v.gap = 0;
-  v.by_pos = a.window < kNoWindow && seen != v.n;
+  v.by_pos = a.window > 0 && seen != v.n;
   v.oldest = (int)max((int64_t)seen - a.window, (int64_t)INT32_MIN);
-  if (a.window < kNoWindow && !v.by_pos && v.n - a.window > a.sinks) {
+  if (a.window > 0 && !v.by_pos && v.n - a.window > a.sinks) {
     v.head = a.sinks;
     v.nv = a.sinks + a.window;
     v.gap = v.n - v.nv;
@@ -644,142 +644,175 @@ __device__ __forceinline__ void move_row(const CacheArgs& c, int b, int2 m, int 
   }
 }
 
+// Inclusive sum over the lanes of a wave, by DPP shifts within rows of 16 and
+// the two row broadcasts.
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);  // row_shr 1
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);  // row_shr 2
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);  // row_shr 4
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);  // row_shr 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // row_bcast 15
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // row_bcast 31
+  return v;
+}
+
 // The choice, one workgroup of NT threads per sequence.  The budget-th largest
 // key is found from the top by digits of 12, 10 and 10 bits: counts of the
 // keys that share the digits found so far in bins, a sum over the bins from
-// the highest, the bin where it reaches the rank.  (The first digit holds the
-// sign, the exponent and three bits of the weight, so that weights of similar
-// size meet in few bins: the counts are LDS atomics, and lanes that hit one
-// address wait for each other.)  Each thread holds E neighbouring slots' keys
-// in registers, of longer sequences one chunk of NT E slots after the other,
-// read again in every round.  Then one pass in slot order lists the free
-// slots below the budget and hands them to the kept ones beyond it.  Bound by
-// the rounds' latency (barriers, bins); 64 sequences of 4,097 slots are read
-// in 0.5 us.
-constexpr int EVICT_BINS = 4096;
+// the highest, the bin where it reaches the rank; the search ends where the
+// rank takes all of a bin.  (The first digit holds the sign, the exponent and
+// three bits of the weight, so that weights of similar size meet in few bins:
+// the counts are LDS atomics, and lanes that hit one address wait for each
+// other.)  Threads hold E slots' keys in registers, NT apart; longer sequences
+// go through them in chunks that are read again in every round.  Then ranks in
+// slot order (ballots, and one sum over the waves' counts) list the free slots
+// below the budget and hand them to the kept ones beyond it.  Bound by the
+// latency of loads, atomics and barriers: 64 sequences of 4,097 slots are read
+// in 0.5 us and take 9.8 (15.3 with all digits searched, slots blocked over the
+// threads and shuffles through LDS).
 constexpr int EVICT_FEW = 32;  // moves that the choosing workgroup makes itself
 template <typename T, int NT, int E>
 __global__ __launch_bounds__(NT) void evict_select(CacheArgs c, EvictArgs a, EvictSpace ws) {
-  constexpr int NW = NT / 64;
+  constexpr int NW = NT / 64, CHUNK = NT * E;
   const int b = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int n = held(c, b), seen = c.seen[b];
+  const int n = held(c, b);
+  const int newest = (int)max((int64_t)c.seen[b] - a.recent, (int64_t)INT32_MIN);
   float* weight = c.weight + (int64_t)b * c.cap;
   int* pos = c.pos + (int64_t)b * c.cap;
   int* src = a.src + (int64_t)b * a.budget;
-  for (int x = tid; x < a.budget; x += NT) src[x] = x < n ? x : -1;
   if (n <= a.budget) {
+    for (int x = tid; x < a.budget; x += NT) src[x] = x < n ? x : -1;
     if (tid == 0) {
       ws.moves[b] = 0;
       c.len[b] = n;
     }
     return;
   }
-  __shared__ int bins[EVICT_BINS];
-  __shared__ int s_found[2], s_wave[2][NW];
-  // exclusive sum over the workgroup's threads (two values at once)
-  auto scan = [&](int u, int v, int* before_u, int* before_v, int* total_u, int* total_v) {
-    int iu = u, iv = v;
-    for (int o = 1; o < 64; o <<= 1) {
-      const int tu = __shfl_up(iu, o, 64), tv = __shfl_up(iv, o, 64);
-      if (lane >= o) {
-        iu += tu;
-        iv += tv;
-      }
-    }
-    __syncthreads();
-    if (lane == 63) {
-      s_wave[0][wave] = iu;
-      s_wave[1][wave] = iv;
-    }
-    __syncthreads();
-    int bu = 0, bv = 0, au = 0, av = 0;
-    for (int w = 0; w < NW; w++) {
-      const int tu = s_wave[0][w], tv = s_wave[1][w];
-      if (w < wave) {
-        bu += tu;
-        bv += tv;
-      }
-      au += tu;
-      av += tv;
-    }
-    *before_u = bu + iu - u;
-    *before_v = bv + iv - v;
-    *total_u = au;
-    *total_v = av;
-  };
   uint32_t key[E];
-  const int chunks = (n + NT * E - 1) / (NT * E);
+  const int chunks = (n + CHUNK - 1) / CHUNK;
   auto load = [&](int ch) {
+    float w[E];
+    int p[E];
 #pragma unroll
     for (int e = 0; e < E; e++) {
-      const int x = min((ch * NT + tid) * E + e, n - 1), p = pos[x];
-      key[e] = keep_key(weight[x], p < a.sinks || seen - p <= a.recent);
+      const int x = min(ch * CHUNK + e * NT + tid, n - 1);
+      w[e] = weight[x];
+      p[e] = pos[x];
     }
+#pragma unroll
+    for (int e = 0; e < E; e++) key[e] = keep_key(w[e], p[e] < a.sinks || p[e] >= newest);
   };
   load(0);
-  uint32_t prefix = 0;
-  int want = a.budget;  // rank of the key searched, among those with the prefix
+  __shared__ __attribute__((aligned(16))) int bins[4096 + 1024 + 1024];
+  __shared__ int s_found[3][2], s_wave[NW], s_count[E * NW + 1];
+  for (int i = tid; i < 4096 + 2048; i += NT) bins[i] = 0;
+  for (int x = tid; x < a.budget; x += NT) src[x] = x;
+  uint32_t least = 0;    // keys above it stay
+  int want = a.budget;   // and the first `want` of those equal to it
   constexpr int SHIFT[3] = {20, 10, 0};
+  __syncthreads();
 #pragma unroll
   for (int round = 0; round < 3; round++) {
     const int shift = SHIFT[round], nb = round ? 1024 : 4096;
-    const int per = nb / NT;  // bins per thread
-    for (int i = tid; i < nb; i += NT) bins[i] = 0;
-    __syncthreads();
+    int* bin = bins + (round == 0 ? 0 : round == 1 ? 4096 : 4096 + 1024);
     for (int ch = 0; ch < chunks; ch++) {
       if (chunks > 1 && (ch || round)) load(ch);
 #pragma unroll
       for (int e = 0; e < E; e++)
-        if ((ch * NT + tid) * E + e < n &&
-            (round == 0 || key[e] >> (shift + 10) == prefix >> (shift + 10)))
-          atomicAdd(&bins[key[e] >> shift & (nb - 1)], 1);
+        if (ch * CHUNK + e * NT + tid < n && (round == 0 || key[e] >> (shift + 10) == least >> (shift + 10)))
+          atomicAdd(&bin[key[e] >> shift & (nb - 1)], 1);
     }
     __syncthreads();
-    // thread t sums bins nb - 1 - t per .. down
+    // thread t sums the bins nb - per (t + 1) .. + per - 1
+    const int per = nb / NT;
     int mine = 0;
-    for (int i = 0; i < per; i++) mine += bins[nb - 1 - tid * per - i];
-    int above, unused0, unused1, unused2;
-    scan(mine, 0, &above, &unused0, &unused1, &unused2);
+    for (int i = 1; i <= per; i++) mine += bin[nb - tid * per - i];
+    const int upto = wave_scan(mine);
+    if (lane == 63) s_wave[wave] = upto;
+    __syncthreads();
+    int above = upto - mine;
+    for (int w = 0; w < wave; w++) above += s_wave[w];
     if (above < want && above + mine >= want) {
-      int i = nb - 1 - tid * per, left = want - above;
-      for (; left > bins[i]; i--) left -= bins[i];
-      s_found[0] = i;
-      s_found[1] = left;
+      int i = nb - tid * per - 1, left = want - above;
+      for (; left > bin[i]; i--) left -= bin[i];
+      s_found[round][0] = i;
+      s_found[round][1] = left == bin[i] ? 0 : left;
     }
     __syncthreads();
-    prefix |= (uint32_t)s_found[0] << shift;
-    want = s_found[1];
-    __syncthreads();
+    least |= (uint32_t)s_found[round][0] << shift;
+    want = s_found[round][1];
+    if (want == 0) break;  // the whole bin stays
   }
-  // keys above `prefix` stay, and the first `want` equal to it
+  if (want == 0) {
+    if (least) least--;  // (keys above it: the bin and those over it)
+    else want = INT32_MAX;
+  }
+  // exclusive sums, in slot order, of the chunk's counts by e and wave
+  auto sum_counts = [&]() {
+    __syncthreads();
+    if (wave == 0) {
+      int before = 0;
+      for (int i = 0; i < E * NW; i += 64) {
+        const int v = i + lane < E * NW ? s_count[i + lane] : 0, upto = wave_scan(v);
+        if (i + lane < E * NW) s_count[i + lane] = before + upto - v;
+        before += __builtin_amdgcn_readlane(upto, 63);
+      }
+      if (lane == 0) s_count[E * NW] = before;
+    }
+    __syncthreads();
+  };
+  const uint64_t below = (1ull << lane) - 1;
   int ties = 0, holes = 0, late = 0;
   int2* mv = ws.move + (int64_t)b * ws.room;
   for (int ch = 0; ch < chunks; ch++) {
     if (chunks > 1) load(ch);
-    const int x0 = (ch * NT + tid) * E;
-    int tie = 0;
+    const int x0 = ch * CHUNK + tid;
+    uint32_t keep = 0;  // one bit per e
+    static_assert(E <= 32 && CHUNK < 32768, "bits of a thread, two counts in a word");
+    if (want > 0 && want < INT32_MAX) {
+      __syncthreads();
 #pragma unroll
-    for (int e = 0; e < E; e++) tie += x0 + e < n && key[e] == prefix;
-    int rank, unused, more, unused2;
-    scan(tie, 0, &rank, &unused, &more, &unused2);
-    rank += ties;
-    ties += more;
-    uint64_t free = 0, over = 0;  // the thread's free slots, kept slots beyond the budget
-    static_assert(E <= 64, "one bit per slot");
+      for (int e = 0; e < E; e++) {
+        const uint64_t eq = __ballot(x0 + e * NT < n && key[e] == least);
+        if (lane == 0) s_count[e * NW + wave] = __popcll(eq);
+      }
+      sum_counts();
+#pragma unroll
+      for (int e = 0; e < E; e++) {
+        const bool eq = x0 + e * NT < n && key[e] == least;
+        const uint64_t m = __ballot(eq);
+        const int rank = ties + s_count[e * NW + wave] + (int)__popcll(m & below);
+        if (eq && rank < want) keep |= 1u << e;
+      }
+      ties += s_count[E * NW];
+    }
+    if (want == INT32_MAX) keep = ~0u;
+#pragma unroll
+    for (int e = 0; e < E; e++) keep |= (uint32_t)(key[e] > least) << e;
+    __syncthreads();
+    auto flags = [&](int e, uint64_t* hole, uint64_t* over) {
+      const int x = x0 + e * NT;
+      const bool k = keep >> e & 1;
+      *hole = __ballot(x < n && x < a.budget && !k);
+      *over = __ballot(x < n && x >= a.budget && k);
+    };
 #pragma unroll
     for (int e = 0; e < E; e++) {
-      if (x0 + e >= n) continue;
-      const bool eq = key[e] == prefix, keep = key[e] > prefix || (eq && rank < want);
-      rank += eq;
-      if (x0 + e < a.budget && !keep) free |= 1ull << e;
-      if (x0 + e >= a.budget && keep) over |= 1ull << e;
+      uint64_t hole, over;
+      flags(e, &hole, &over);
+      if (lane == 0) s_count[e * NW + wave] = (int)__popcll(hole) | (int)__popcll(over) << 16;
     }
-    int hi, li, nh, nl;
-    scan(__popcll(free), __popcll(over), &hi, &li, &nh, &nl);
-    for (hi += holes; free; free &= free - 1) mv[hi++].x = x0 + __builtin_ctzll(free);
-    for (li += late; over; over &= over - 1) mv[li++].y = x0 + __builtin_ctzll(over);
-    holes += nh;
-    late += nl;
+    sum_counts();
+#pragma unroll
+    for (int e = 0; e < E; e++) {
+      uint64_t hole, over;
+      flags(e, &hole, &over);
+      const int at = s_count[e * NW + wave];
+      if (hole >> lane & 1) mv[holes + (at & 0xFFFF) + (int)__popcll(hole & below)].x = x0 + e * NT;
+      if (over >> lane & 1) mv[late + (at >> 16) + (int)__popcll(over & below)].y = x0 + e * NT;
+    }
+    holes += s_count[E * NW] & 0xFFFF;
+    late += s_count[E * NW] >> 16;
   }
   __syncthreads();
   for (int i = tid; i < holes; i += NT) {

@@ -596,8 +596,7 @@ FUSION_API int fusion_paged_attention(const fusion_cache* c, const void* q, cons
   PagedArgs a{};
   a.q = q; a.q_row = strides[0]; a.q_head = strides[1]; a.out = out;
   a.H = heads; a.group = heads / c->kv_heads;
-  a.window = window == 0 ? kNoWindow : std::min(window, kNoWindow);
-  a.sinks = std::min(sinks, kNoWindow); a.accumulate = accumulate;
+  a.window = window; a.sinks = sinks; a.accumulate = accumulate;
   a.scale = (float)(1.0 / std::sqrt((double)c->dh)); a.ws = ws;
   hipStream_t s = (hipStream_t)stream;
   hipError_t err = c->precision == 1 ? launch_paged_attention<bf16_t>(ca, a, s)

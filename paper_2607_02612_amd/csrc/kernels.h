@@ -237,7 +237,7 @@ struct PagedArgs {
   const void* q;  // T [B][H][dh]
   int64_t q_row, q_head;
   void* out;  // T [B][H][dh]
-  int H, group, window, sinks, accumulate;
+  int H, group, window, sinks, accumulate;  // no limit: window = 0
   float scale;
   void* ws;
 };

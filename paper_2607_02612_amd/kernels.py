@@ -214,6 +214,11 @@ def _current(dev, *used):
     return raw
 
 
+def _no_grad(t, name):
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient, and none is computed: detach it")
+
+
 def _heads(t, name, dtype, heads, dh):
     """Checks a [rows, heads, dh] tensor of any row and head strides in whole
     16-byte pieces; returns its address and the two strides."""
@@ -222,8 +227,7 @@ def _heads(t, name, dtype, heads, dh):
         raise ValueError(f"{name} must be a tensor [rows, {heads}, {dh}]")
     if t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype}")
-    if t.requires_grad and torch.is_grad_enabled():
-        raise ValueError(f"{name} requires a gradient, and none is computed: detach it")
+    _no_grad(t, name)
     row, head, one = t.stride()
     p = t.data_ptr()
     if one != 1 or (row | head) & _PIECE[dtype] or p & 15:
@@ -257,11 +261,17 @@ def _offsets(cu):
     return a, ctypes.addressof(ctypes.c_char.from_buffer(a))
 
 
-def _count(v, name, lowest=0):
-    """A whole number, at most 2^30 (no sequence is longer)."""
+def _count(v, name, lowest=0, most=1 << 30):
+    """A whole number; beyond `most` (rows of a sequence, or the last position
+    there is) it makes no difference."""
+    if type(v) is int and lowest <= v <= most:
+        return v
     if int(v) != v or v < lowest:
         raise ValueError(f"{name} must be a whole number, at least {lowest}")
-    return min(int(v), 1 << 30)
+    return min(int(v), most)
+
+
+_LAST = (1 << 31) - 1  # position
 
 
 _Strides2, _Strides4, _Strides6 = (ctypes.c_int64 * n for n in (2, 4, 6))
@@ -271,27 +281,11 @@ def _out(out, rows, heads, dh, like):
     if out is None:
         return like.new_empty((rows, heads, dh))
     _need(out, "out", like.dtype)
+    _no_grad(out, "out")
     if tuple(out.shape) != (rows, heads, dh) or out.data_ptr() % 16:
         raise ValueError(f"out must be a 16-byte aligned tensor [{rows}, {heads}, {dh}]")
     _here(out)
     return out
-
-
-def _offsets(cu):
-    """Host row offsets as int32 (the library checks their order)."""
-    a = np.asarray(cu)
-    if a.ndim != 1 or len(a) < 2 or a.dtype.kind not in "iu":
-        raise ValueError("offsets must be [batch + 1] whole numbers")
-    if a.dtype != np.int32 and (a.min() < 0 or a.max() > 1 << 30):
-        raise ValueError("offsets must be in 0 .. 2^30")
-    return _host_i32(a)
-
-
-def _count(v, name, lowest=0):
-    """A whole number, at most 2^30 (no sequence is longer)."""
-    if int(v) != v or v < lowest:
-        raise ValueError(f"{name} must be a whole number, at least {lowest}")
-    return min(int(v), 1 << 30)
 
 
 def window_attention(q, k, v, cu, window=None, sinks=0, causal=True, size=None, out=None):
@@ -303,7 +297,8 @@ def window_attention(q, k, v, cu, window=None, sinks=0, causal=True, size=None, 
     output, say); cu: host offsets [batch + 1] (samples may be empty), rows
     from cu[-1] on take no part; size: float32 [M], scores += ln(size), a size
     of 0 hides the row.  Returns out [M, heads, dh]: rows that see nothing are
-    zero, rows from cu[-1] on are left as they were (zero if out is None)."""
+    zero, rows from cu[-1] on are left as they were (zero if out is None); a
+    given out does not overlap the inputs."""
     if not isinstance(q, torch.Tensor) or q.dim() != 3 or q.dtype not in _PREC:
         raise ValueError("q must be a bfloat16 or float32 tensor [rows, heads, dh]")
     M, heads, dh = q.shape
@@ -315,6 +310,7 @@ def window_attention(q, k, v, cu, window=None, sinks=0, causal=True, size=None, 
         raise ValueError("q, k and v must have the same rows")
     if size is not None:
         _need(size, "size", torch.float32)
+        _no_grad(size, "size")
         if tuple(size.shape) != (M,):
             raise ValueError("one size per row")
     dev = _here(q, k, v, size)
@@ -378,6 +374,8 @@ class TokenCache:
         if tuple(weight.shape) != (batch, max_pages * page_size) or pos.shape != weight.shape:
             raise ValueError("weight and pos must be [batch, max_pages * page_size]")
         self._tensors = (k, v, table, length, seen, weight, pos)
+        if any(t.requires_grad for t in self._tensors):
+            raise ValueError("the cache's tensors are written in place and have no gradients")
         if any(t.device != k.device for t in self._tensors):
             raise ValueError("the cache's tensors must be on one GPU")
         self._c = FusionCache(k.data_ptr(), v.data_ptr(), k.stride()[:3], v.stride()[:3],
@@ -436,8 +434,9 @@ class TokenCache:
 
 def cache_append(cache, k, v, cu=None):
     """Append key and value rows [rows, kv_heads, dh]: one per sequence, or
-    rows cu[i] .. cu[i+1]-1 to sequence i (cu: host offsets).  Their weight
-    starts at 0; rows past a sequence's capacity are dropped."""
+    rows cu[i] .. cu[i+1]-1 to sequence i (cu: host offsets, rows from cu[-1]
+    on take no part).  Their weight starts at 0; rows past a sequence's
+    capacity are dropped."""
     kp, k_row, k_head = _heads(k, "k", cache.dtype, cache.kv_heads, cache.dh)
     vp, v_row, v_head = _heads(v, "v", cache.dtype, cache.kv_heads, cache.dh)
     _here(k, v)
@@ -446,8 +445,8 @@ def cache_append(cache, k, v, cu=None):
         cu_h, cu_p = _offsets(cu)
         if len(cu_h) != cache.batch + 1:
             raise ValueError("offsets must be [batch + 1]")
-    rows = cache.batch if cu is None else int(cu_h[-1])
-    if k.shape[0] != rows or v.shape[0] != rows:
+    rows = k.shape[0]
+    if v.shape[0] != rows or (rows != cache.batch if cu is None else rows < cu_h[-1]):
         raise ValueError("rows do not match the sequences")
     check(_native.lib().fusion_cache_append(cache._ref, kp, vp,
                                             _Strides4(k_row, k_head, v_row, v_head), cu_p,
@@ -458,13 +457,14 @@ def paged_attention(q, cache, window=None, sinks=0, accumulate=True, out=None):
     """Attention of each sequence's newest token (appended before) over its
     cached tokens; with a window, over those among the last `window` positions
     or the first `sinks`.  q [batch, heads, dh]; returns out like q,
-    contiguous.  accumulate: cache.weight grows by the mean over the heads of
-    the attention probabilities."""
+    contiguous (a given out does not overlap the inputs).  accumulate:
+    cache.weight grows by the mean over the heads of the attention
+    probabilities."""
     if not isinstance(q, torch.Tensor) or q.dim() != 3 or q.shape[0] != cache.batch:
         raise ValueError("q must be a tensor [batch, heads, dh]")
     heads = q.shape[1]
     qp, q_row, q_head = _heads(q, "q", cache.dtype, heads, cache.dh)
-    window = 0 if window is None else _count(window, "window", 1)
+    window = 0 if window is None else _count(window, "window", 1, _LAST)
     _here(q)
     fresh = out is None
     out = _out(out, cache.batch, heads, cache.dh, q)
@@ -472,7 +472,8 @@ def paged_attention(q, cache, window=None, sinks=0, accumulate=True, out=None):
     stream = cache._ready(q, None if fresh else out)
     ws, n = cache._workspace("fusion_paged_attention_workspace_bytes", heads, acc)
     check(_native.lib().fusion_paged_attention(
-        cache._ref, qp, _Strides2(q_row, q_head), heads, window, _count(sinks, "sinks"), acc,
+        cache._ref, qp, _Strides2(q_row, q_head), heads, window,
+        _count(sinks, "sinks", 0, _LAST), acc,
         out.data_ptr(), ws.data_ptr(), n, stream))
     return out
 
@@ -488,7 +489,7 @@ def cache_evict(cache, budget, sinks=0, recent=0):
         raise ValueError("sinks and recent do not fit the budget")
     stream = cache._ready()
     ws, n = cache._workspace("fusion_cache_evict_workspace_bytes", budget)
-    src = torch.empty((cache.batch, budget), dtype=torch.int32, device=cache.device)
+    src = cache.table.new_empty((cache.batch, budget))
     check(_native.lib().fusion_cache_evict(cache._ref, budget, sinks, recent, src.data_ptr(),
                                            ws.data_ptr(), n, stream))
     return src

@@ -273,7 +273,7 @@ def _paged_ref(q, cache, window, sinks, dtype):
         n = int(length[b])
         k, v, see = _rows(cache, b, n)
         if window:
-            see = see & ((pos[b, :n] > seen[b] - 1 - window) | (pos[b, :n] < sinks))
+            see = see & ((pos[b, :n] > int(seen[b]) - 1 - window) | (pos[b, :n] < sinks))
         for h in range(hq):
             o, p, t, rel = _attend(q[b, h][None], k[:, h // g], v[:, h // g], see[None], 0.0, dtype)
             out[b, h], tol[b, h] = o[0], t[0]
@@ -377,6 +377,24 @@ def test_paged_attention_many_sequences(torch_cuda, B):
     assert (np.abs(_np(c.weight) - before - add) <= add_tol + U32 * (before + add)).all()
 
 
+@pytest.mark.parametrize("seen", [-(1 << 31), 0, (1 << 31) - 1])
+def test_extreme_positions(torch_cuda, seen):
+    """Positions and counts at the ends of their type: no wrapped sums."""
+    torch = torch_cuda
+    rng = np.random.default_rng(15)
+    c = _cache(torch, rng, "bf16", [70, 40], 1, 64, 16, 80, seen=[seen, seen])
+    ends = np.array([-(1 << 31), -1, 0, 1, (1 << 31) - 2, (1 << 31) - 1])
+    pos = rng.choice(ends, size=c.pos.shape).astype(np.int32)
+    c.pos.copy_(torch.from_numpy(pos))
+    q = _normal(torch, rng, "bf16", 2, 3, 64)
+    for window, sinks in ((1, 0), (5, 1), (1 << 30, 0)):
+        out, tol, _, _ = _paged_ref(_np(q), c, window, sinks, "bf16")
+        _close(_np(_kern().paged_attention(q, c, window, sinks)), out, tol, window)
+    w = c.weight.cpu().numpy()
+    want = [_evict_ref(n, seen, w[b], pos[b], c.capacity, 30, 1, 20)[0] for b, n in enumerate((70, 40))]
+    assert np.array_equal(_kern().cache_evict(c, 30, 1, 20).cpu().numpy(), np.array(want))
+
+
 def test_paged_attention_offsets_past_32_bits(torch_cuda):
     """Pages so far apart that element offsets pass 2^31, and byte offsets 2^32."""
     torch = torch_cuda
@@ -429,6 +447,8 @@ def test_cache_append(torch_cuda, dtype, counts):
                 state["seen"][b] += 1
             r += 1
     cu = None if counts is None else np.concatenate([[0], np.cumsum(n)])
+    if counts is not None:  # rows behind the last sequence take no part
+        k, v = (torch.cat([t, t[:3]]) for t in (k, v))
     _kern().cache_append(c, k, v, cu)
     for x in state:
         assert np.array_equal(_np(getattr(c, x)), state[x]), x
@@ -464,7 +484,7 @@ def _evict_ref(length, seen, weight, pos, cap, budget, sinks, recent):
     src[:min(n, budget)] = np.arange(min(n, budget))
     if n <= budget:
         return src, []
-    p, w = pos[:n].astype(np.int64), weight[:n].astype(np.float64)
+    p, w, seen = pos[:n].astype(np.int64), weight[:n].astype(np.float64), int(seen)
     safe = (p < sinks) | (p >= seen - recent)
     order = sorted(range(n), key=lambda x: (not safe[x], math.isnan(w[x]) and not safe[x],
                                             0 if safe[x] or math.isnan(w[x]) else -w[x], x))
@@ -670,6 +690,9 @@ def test_refusals_on_the_gpu(torch_cuda):
         lambda: kern.window_attention(q, k, k, [0, 2], out=q[:, :2]),
         lambda: kern.window_attention(q.half(), k.half(), k.half(), [0, 2]),
         lambda: kern.window_attention(q.requires_grad_(), k, k, [0, 2]),
+        lambda: kern.window_attention(q.detach(), k, k, [0, 2], size=torch.ones(
+            2, device="cuda", requires_grad=True)),
+        lambda: kern.cache_append(c, k, k, [0, 2, 3]),
         lambda: kern.window_attention(n(2, 4, 68)[:, :, 4:], k, k, [0, 2]),  # base, strides
         lambda: kern.paged_attention(n(3, 4, 64), c),
         lambda: kern.paged_attention(n(2, 4, 32), c),
