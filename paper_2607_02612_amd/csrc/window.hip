@@ -83,38 +83,33 @@ __device__ __forceinline__ bool sees(const WindowArgs& a, int i, int j) {
   if (a.causal) return j <= i && (i - j < a.window || j < a.sinks);
   return (i - j < a.window && j - i < a.window) || j < a.sinks;
 }
-// Whether all of rows i0 .. i1 see all of j0 .. j1, and whether none sees any.
-// (Without short cuts: each is one scalar condition, and the tile loop keeps
-// its branches simple.)
-__device__ __forceinline__ bool all_see(const WindowArgs& a, int i0, int i1, int j0, int j1) {
-  const bool near = (i1 - j0 < a.window) & ((a.causal != 0) | (j1 - i0 < a.window));
-  return (near | (j1 < a.sinks)) & ((a.causal == 0) | (j1 <= i0));
-}
-__device__ __forceinline__ bool none_see(const WindowArgs& a, int i0, int i1, int j0, int j1) {
-  const bool far = (i0 - j1 >= a.window) | ((a.causal == 0) & (j0 - i1 >= a.window));
-  return (far & (j0 >= a.sinks)) | ((a.causal != 0) & (j0 > i1));
-}
-// How a wave takes a tile of keys j0 .. j0 + keys - 1: not at all, or with or
-// without looking at each pair.
-enum { TILE_SKIP, TILE_WHOLE, TILE_EDGE };
-__device__ __forceinline__ int tile_mode(const WindowArgs& a, int n, int i0, int i1, int j0, int keys,
-                                         bool hidden) {
-  const bool edge = hidden | (j0 + keys > n) | !all_see(a, i0, i1, j0, j0 + keys - 1);
-  const bool skip = (i0 >= n) | none_see(a, i0, i1, j0, j0 + keys - 1);
-  return __builtin_amdgcn_readfirstlane(skip ? TILE_SKIP : edge ? TILE_EDGE : TILE_WHOLE);
-}
-
-// The rows that a row sees: lo .. lo + span, and those below first.
+// The rows that row i of a sample of n sees: those up to hi that are lo or
+// later, or below first.
 struct RowSpan {
-  int lo, first;
-  unsigned span;
+  int lo, hi, first;
 };
 __device__ __forceinline__ RowSpan row_span(const WindowArgs& a, int i, int n) {
   RowSpan r;
   r.lo = max(0, i - a.window + 1);
-  r.span = (unsigned)((a.causal ? min(i, n - 1) : min(n - 1, i + a.window - 1)) - r.lo);
   r.first = min(a.sinks, a.causal ? i + 1 : n);
+  r.hi = max(min(n - 1, a.causal ? i : i + a.window - 1), r.first - 1);
   return r;
+}
+
+// How rows i0 .. i1 take a tile of keys j0 .. j0 + keys - 1: not at all, with
+// no look at the pairs, with one at the later end or the earlier end of the
+// rows' spans, or with all there is (without short cuts, so that it is one
+// scalar value and the tile loop keeps its branches simple).
+enum { TILE_SKIP, TILE_WHOLE, TILE_LATE, TILE_EARLY, TILE_ALL };
+__device__ __forceinline__ int tile_mode(const WindowArgs& a, int n, int i0, int i1, int j0, int keys,
+                                         bool hidden) {
+  const RowSpan r0 = row_span(a, i0, n), r1 = row_span(a, i1, n);
+  const int j1 = j0 + keys - 1;
+  const bool late = j1 > r0.hi, early = (j0 < r1.lo) & (j1 >= r0.first);
+  const bool skip = (i0 >= n) | (j0 > r1.hi) | ((j1 < r0.lo) & (j0 >= r1.first));
+  const bool all = hidden | (early & (late | (j0 < a.sinks)));
+  return __builtin_amdgcn_readfirstlane(skip ? TILE_SKIP : all ? TILE_ALL : late ? TILE_LATE
+                                        : early ? TILE_EARLY : TILE_WHOLE);
 }
 
 // The query rows of a workgroup and the key tiles that any of them sees: the
@@ -250,7 +245,7 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
       load_size(pl.tile(it + 1));
     }
     hidden = SIZES && __builtin_amdgcn_readfirstlane(s_hidden[st]);
-    if (tile_mode(a, n, pl.q0, pl.q1, k0, WKT, hidden) == TILE_EDGE) {
+    if (tile_mode(a, n, pl.q0, pl.q1, k0, WKT, hidden) > TILE_WHOLE) {
       char* Vs = smem + st * 2 * TILEB + TILEB;
       uint32_t any = 0;
 #pragma unroll
@@ -277,8 +272,8 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
     if (it + 1 < pl.nt) put_size(st ^ 1);
     return ++it < pl.nt ? begin() : -1;
   };
-  auto compute = [&](auto edge_c) {
-    constexpr bool EDGE = decltype(edge_c)::value;
+  auto compute = [&](auto mode_c) {
+    constexpr int MODE = decltype(mode_c)::value;
     const char* Ks = smem + st * 2 * TILEB;
     const char* Vs = Ks + TILEB;
     f32x16_t S[2];
@@ -302,24 +297,23 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
 #pragma unroll
           for (int j = 0; j < 4; j++) S[x][4 * i4 + j] = fmaf(S[x][4 * i4 + j], sc2, ln[j]);
         }
-      if (EDGE && hidden)
+      if (MODE == TILE_ALL && hidden)
 #pragma unroll
         for (int x = 0; x < 2; x++)
 #pragma unroll
           for (int i = 0; i < 16; i++)
             if (lnS[st][x * 32 + 8 * (i / 4) + 4 * hl + i % 4] == -INFINITY) S[x][i] = -INFINITY;
     }
-    if (EDGE) {
-      const unsigned at = (unsigned)(k0 + 4 * hl - sp.lo);
-      const int first = sp.first - k0 - 4 * hl;
+    const int lo = sp.lo - k0 - 4 * hl, hi = sp.hi - k0 - 4 * hl, first = sp.first - k0 - 4 * hl;
 #pragma unroll
-      for (int x = 0; x < 2; x++)
+    for (int x = 0; x < 2; x++)
 #pragma unroll
-        for (int i = 0; i < 16; i++) {
-          const int key = x * 32 + 8 * (i / 4) + i % 4;
-          S[x][i] = (at + key <= sp.span) | (key < first) ? S[x][i] : -INFINITY;
-        }
-    }
+      for (int i = 0; i < 16; i++) {
+        const int key = x * 32 + 8 * (i / 4) + i % 4;
+        if (MODE == TILE_LATE) S[x][i] = key <= hi ? S[x][i] : -INFINITY;
+        if (MODE == TILE_EARLY) S[x][i] = key >= lo ? S[x][i] : -INFINITY;
+        if (MODE == TILE_ALL) S[x][i] = (key <= hi) & ((key >= lo) | (key < first)) ? S[x][i] : -INFINITY;
+      }
     float mt = -INFINITY;
 #pragma unroll
     for (int x = 0; x < 2; x++)
@@ -376,11 +370,19 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
   int mode = begin();
   while (mode >= 0) {
     while (mode == TILE_WHOLE) {
-      compute(std::false_type{});
+      compute(std::integral_constant<int, TILE_WHOLE>{});
       mode = next();
     }
-    while (mode == TILE_EDGE) {
-      compute(std::true_type{});
+    while (mode == TILE_LATE) {
+      compute(std::integral_constant<int, TILE_LATE>{});
+      mode = next();
+    }
+    while (mode == TILE_EARLY) {
+      compute(std::integral_constant<int, TILE_EARLY>{});
+      mode = next();
+    }
+    while (mode == TILE_ALL) {
+      compute(std::integral_constant<int, TILE_ALL>{});
       mode = next();
     }
     while (mode == TILE_SKIP) mode = next();
@@ -518,7 +520,7 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowA
     char* Vs = smem + st * 2 * TILEB + TILEB;
     bool bad = false;
     const bool hidden = SIZES && __builtin_amdgcn_readfirstlane(s_hidden[st]);  // some key of the tile has no size
-    if (tile_mode(a, n, pl.q0, pl.q1, k0, KT, hidden) == TILE_EDGE) {
+    if (tile_mode(a, n, pl.q0, pl.q1, k0, KT, hidden) > TILE_WHOLE) {
       bool any = false;
 #pragma unroll
       for (int u = 0; u < TILEB / (64 * WNW * 16); u++) {
@@ -565,14 +567,15 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowA
           if (hidden && ln[j] == -INFINITY) S[x][j] = -INFINITY;
         }
       }
-      if (mode == TILE_EDGE) {
-        const unsigned at = (unsigned)(k0 + 4 * g - sp.lo);
-        const int first = sp.first - k0 - 4 * g;
+      if (mode > TILE_WHOLE) {
+        const int lo = sp.lo - k0 - 4 * g, hi = sp.hi - k0 - 4 * g, first = sp.first - k0 - 4 * g;
 #pragma unroll
         for (int x = 0; x < NT; x++)
 #pragma unroll
-          for (int j = 0; j < 4; j++)
-            S[x][j] = (at + (16 * x + j) <= sp.span) | (16 * x + j < first) ? S[x][j] : -INFINITY;
+          for (int j = 0; j < 4; j++) {
+            const int key = 16 * x + j;
+            S[x][j] = (key <= hi) & ((key >= lo) | (key < first)) ? S[x][j] : -INFINITY;
+          }
       }
       float mt = -INFINITY;
 #pragma unroll
