@@ -210,6 +210,12 @@ __global__ __launch_bounds__(256, 2) void paged_attention(CacheArgs c, PagedArgs
   const int h0 = kh * a.group + qt * 16, nq = min(16, a.group - qt * 16);
   const int dh = c.dh;
   const float sc2 = a.scale * kLog2e;
+  // place of the 32-byte segment of a token's values in LDS (bf16): permuted so
+  // that 8 tokens cover the banks, and the halves of a segment swapped every 8
+  // tokens, so that 16 tokens' 16-byte pieces do
+  auto v_at = [](int r, int seg) {
+    return r * VROW + ((seg ^ (DP == 128 ? r & 7 : r >> 1 & 3)) << 5);
+  };
 
   auto segment = [&](int b, int ta, int tb, int part) {
     Visible vis = visible(c, a, b);
@@ -340,7 +346,7 @@ __global__ __launch_bounds__(256, 2) void paged_attention(CacheArgs c, PagedArgs
                                      see[u] ? x.w : 0);
           const int r = 16 * u + cl, p = 4 * s + g;
           if constexpr (BF)
-            *(uint4*)(Vs + r * VROW + (((p >> 1) ^ (r & (DP / 16 - 1))) << 5) + ((p & 1) << 4)) = v;
+            *(uint4*)(Vs + v_at(r, p >> 1) + ((p & 1) << 4 ^ (r >> 3 & 1) << 4)) = v;
           else
             *(uint4*)(Vs + r * VROW + p * 16) = v;
         }
@@ -405,7 +411,7 @@ __global__ __launch_bounds__(256, 2) void paged_attention(CacheArgs c, PagedArgs
             const int r = 16 * z + 4 * g + (cl >> 2);
             vf.h[z] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                 (__attribute__((address_space(3))) s16x4_t*)(
-                    Vs + r * VROW + ((d ^ (r & (DP / 16 - 1))) << 5) + ((cl & 3) << 3)));
+                    Vs + v_at(r, d) + ((cl & 3) << 3 ^ (r >> 3 & 1) << 4)));
           }
           O[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.v, p.v, O[d], 0, 0, 0);
           O[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.v, p2.v, O[d], 0, 0, 0);

@@ -41,10 +41,10 @@ struct WindowSeqs {
 // stays below 2^8, whose relative precision is that of 1), per row, so that
 // no row's result depends on another's; rows whose maximum stays multiply by 1.
 //
-// LDS rows are 2 DP bytes.  K's 16-byte pieces are XOR-permuted by the row
-// (mod 16 or 8), V's 32-byte segments by the row mod 4: the 16-byte reads of
-// consecutive rows and the 8-byte transposing reads of 4 rows spread over all
-// banks.  The copies write LDS in lane order, so the permutation is made in
+// LDS rows are 2 DP bytes.  K's 16-byte pieces are XOR-permuted by the row mod
+// 16 (64-wide: row / 2 mod 8), V's pairs of 32-byte segments by the row mod 4
+// (row / 2 mod 2): the 16-byte reads of 16 rows and the 8-byte transposing
+// reads of 4 rows spread over all banks, and no read waits for another.  The copies write LDS in lane order, so the permutation is made in
 // the source address.
 //
 // A probability of 0 does not take a value out of P V when that value is
@@ -167,6 +167,11 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
   const bf16_t* vg = (const bf16_t*)a.v + (int64_t)pl.base * a.v_row + (int64_t)kh * a.v_head;
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
   if (tid == 0) s_bad = -1;
+  // permutations of the 16-byte pieces of K's row r and of the 32-byte segments
+  // of V's: 16 pieces of 16 rows, and 4 rows of 64 bytes, cover the 256 bytes
+  // of the banks
+  auto k_swizzle = [](int r) { return DP == 128 ? r & 15 : r >> 1 & 7; };
+  auto v_swizzle = [](int r) { return (DP == 128 ? r & 3 : r >> 1 & 1) << 1; };
 
   // copy of one tile: the wave's rows r = (wave NC + u) RPC + lane / PPR
   auto copy_tile = [&](int t, int st) {
@@ -176,7 +181,7 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
 #pragma unroll
     for (int u = 0; u < NC; u++) {
       const int r = (wave * NC + u) * RPC + lane / PPR, rr = min(r, lim), p = lane % PPR;
-      const int pk = p ^ (r & (PPR - 1)), pv = p ^ ((r & 3) << 1);
+      const int pk = p ^ k_swizzle(r), pv = p ^ (v_swizzle(r) << 1);
       const unsigned dst = lds0 + st * 2 * TILEB + (wave * NC + u) * 1024;
       const unsigned ko = (unsigned)rr * (unsigned)a.k_row * 2 + pk * 16;
       const unsigned vo = (unsigned)rr * (unsigned)a.v_row * 2 + pv * 16;
@@ -228,7 +233,7 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
     for (int i = 0; i < 16; i++) O[d][i] = 0.f;
 
   // LDS addresses of the operands: K row c of a half, V rows of a 16-lane group
-  const int krow = c * ROWB, kx = c & (PPR - 1);
+  const int krow = c * ROWB, kx = k_swizzle(c);
   const int vkey = (lane & 15) >> 2;
   const int vcol = ((lane >> 4) & 1) * 32 + (lane & 3) * 8;  // bytes within a 64-byte dim tile
   int it = 0, st = 0, k0 = 0;  // the tile in hand: its number, LDS stage and first key
@@ -358,7 +363,7 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
 #pragma unroll
         for (int z = 0; z < 2; z++) {
           const int key = 16 * y + 8 * z + 4 * hl + vkey;  // key % 4 == vkey
-          const int seg = (d * 2 + (vcol >> 5)) ^ vkey;
+          const int seg = (d * 2 + (vcol >> 5)) ^ v_swizzle(vkey);
           vf.h[z] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
               (__attribute__((address_space(3))) s16x4_t*)(Vs + key * ROWB + seg * 32 + (vcol & 31)));
         }
