@@ -294,6 +294,7 @@ PAGED = [  # lengths, heads, kv_heads, dh, page, capacity, window, sinks, evicte
     ([4099, 17], 12, 12, 64, 27, 4099, 1000, 4, True),
     ([260, 33, 31], 17, 1, 128, 32, 288, 70, 90, False),
     ([3000], 6, 6, 64, 64, 3008, 257, 1, False),
+    ([60000], 64, 64, 8, 64, 60000, 100000, 2, True),
 ]
 
 
