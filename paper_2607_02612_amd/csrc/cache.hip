@@ -154,12 +154,11 @@ typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int PAGED_SPLIT = 1024;  // sequences up to which the work is split over their lengths
 // Parts in all, about: the waves that the registers let run at once (64-wide
-// heads: 64 sequences of 4,096 tokens, 12 heads 158 us, with 2,048 parts 162,
-// with 4,096 164).
+// heads, 64 sequences of 4,096 tokens, 12 heads: with 2,048 parts 2.5 % slower,
+// with 4,096 4 %).
 constexpr int PAGED_WAVES = 2048, PAGED_WAVES_64 = 3 * 1024;
 
-constexpr int LIST = 512;            // tokens of a part that are gathered at a time
-constexpr int SCORE_BYTES = 2048;   // scores that a wave holds back in LDS: a tile of 16 heads
+constexpr int LIST = 512;  // tokens of a part that are gathered at a time
 
 struct PagedSpace {
   int2* plan;    // [B]: first part, number of parts
@@ -208,15 +207,20 @@ __global__ __launch_bounds__(256, 2) void paged_attention(CacheArgs c, PagedArgs
   constexpr int ND = DP / 16;
   constexpr int VROW = BF ? DP * 2 : (DP + 4) * 4;  // bytes of a token's values in LDS
   __shared__ __attribute__((aligned(16))) char v_all[4 * KT * VROW];
-  __shared__ __attribute__((aligned(16))) char s_all[ACC ? 4 * SCORE_BYTES : 16];
-  __shared__ __attribute__((aligned(16))) int l_all[4 * LIST];
+  // LDS that a wave's values leave free: scores held back, or a list of tokens
+  // (allocated in units of 1280 bytes, 160 KB a CU, for the workgroups that run at once)
+  constexpr int SHARE = 160 * 1024 / (DP <= 64 ? 3 : 2) / 1280 * 1280 / 4;
+  constexpr int SCORE_BYTES = (SHARE - KT * VROW) / 1024 * 1024;
+  static_assert(SCORE_BYTES >= 2048 && SCORE_BYTES >= LIST * 4, "a tile of 16 heads, a list");
+  constexpr int SPARE = ACC ? SCORE_BYTES : LIST * 4;
+  __shared__ __attribute__((aligned(16))) char s_all[4 * SPARE];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int g = lane >> 4, cl = lane & 15;
   const int id = blockIdx.x * 4 + wave, unit = id % ws.units, range = id / ws.units;
   if (range >= ws.ranges) return;
   char* Vs = v_all + wave * KT * VROW;
-  char* Ss = s_all + (ACC ? wave * SCORE_BYTES : 0);
-  int* list = l_all + wave * LIST;
+  char* Ss = s_all + wave * SPARE;
+  int* list = (int*)Ss;
   const int kh = unit / ws.qtiles, qt = unit % ws.qtiles;
   const int h0 = kh * a.group + qt * 16, nq = min(16, a.group - qt * 16);
   const int dh = c.dh;
@@ -303,9 +307,10 @@ __global__ __launch_bounds__(256, 2) void paged_attention(CacheArgs c, PagedArgs
 #pragma unroll
     for (int d = 0; d < ND; d++) O[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     // Scores wait in LDS until they fill SCORE_BYTES and then leave in whole
-    // 1-KB stores (64 sequences of 4,096 tokens, one head a unit: 158 us; with
-    // a store for each tile's row 166; with 4 heads a unit both 220, of which
-    // the bytes written, 33 MB beside 1.07 GB read, are 30).
+    // 1-KB stores: writes among the reads cost the memory more than their bytes
+    // do, so they come together and seldom (64 sequences of 4,096 tokens, 4
+    // heads a unit, 33 MB written beside 1.07 GB read: 230 us with 12 KB held back,
+    // 239 with 2 KB, 209 without any scores written).
     const int row_shift = 32 - __builtin_clz(2 * nq - 1);  // rows of a tile in LDS: 1 << row_shift >= nq
     const int tile_shift = row_shift - 1 + (BF ? 7 : 6);   // bytes of a tile
     const int slots = SCORE_BYTES >> tile_shift;
@@ -460,6 +465,8 @@ __global__ __launch_bounds__(256, 2) void paged_attention(CacheArgs c, PagedArgs
     const int* pos = c.pos + (int64_t)b * c.cap;
     do {
       if (by_pos) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (its last reader is done)
+        __builtin_amdgcn_wave_barrier();
         int count = 0;
         for (; next < end && count <= LIST - 256; next += 256) {
           int at[4];
