@@ -99,17 +99,21 @@ __device__ __forceinline__ RowSpan row_span(const WindowArgs& a, int i, int n) {
 // How rows i0 .. i1 take a tile of keys j0 .. j0 + keys - 1: not at all, with
 // no look at the pairs, with one at the later end or the earlier end of the
 // rows' spans, or with all there is (without short cuts, so that it is one
-// scalar value and the tile loop keeps its branches simple).
-enum { TILE_SKIP, TILE_WHOLE, TILE_LATE, TILE_EARLY, TILE_ALL };
+// scalar value and the tile loop keeps its branches simple).  `halves`: the
+// ends' tiles of which the rows see one half only have modes of their own
+// (TILE_LATE_1: the first half, TILE_EARLY_2: the second).
+enum { TILE_SKIP, TILE_WHOLE, TILE_LATE, TILE_LATE_1, TILE_EARLY, TILE_EARLY_2, TILE_ALL };
 __device__ __forceinline__ int tile_mode(const WindowArgs& a, int n, int i0, int i1, int j0, int keys,
-                                         bool hidden) {
+                                         bool hidden, bool halves) {
   const RowSpan r0 = row_span(a, i0, n), r1 = row_span(a, i1, n);
   const int j1 = j0 + keys - 1;
   const bool late = j1 > r0.hi, early = (j0 < r1.lo) & (j1 >= r0.first);
   const bool skip = (i0 >= n) | (j0 > r1.hi) | ((j1 < r0.lo) & (j0 >= r1.first));
   const bool all = hidden | (early & (late | (j0 < a.sinks)));
-  return __builtin_amdgcn_readfirstlane(skip ? TILE_SKIP : all ? TILE_ALL : late ? TILE_LATE
-                                        : early ? TILE_EARLY : TILE_WHOLE);
+  const int mid = j0 + keys / 2;
+  const int at_end = TILE_LATE + (halves & (mid > r1.hi)), at_start = TILE_EARLY + (halves & (mid <= r0.lo));
+  return __builtin_amdgcn_readfirstlane(skip ? TILE_SKIP : all ? TILE_ALL : late ? at_end
+                                        : early ? at_start : TILE_WHOLE);
 }
 
 // The query rows of a workgroup and the key tiles that any of them sees: the
@@ -250,7 +254,7 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
       load_size(pl.tile(it + 1));
     }
     hidden = SIZES && __builtin_amdgcn_readfirstlane(s_hidden[st]);
-    if (tile_mode(a, n, pl.q0, pl.q1, k0, WKT, hidden) > TILE_WHOLE) {
+    if (tile_mode(a, n, pl.q0, pl.q1, k0, WKT, hidden, false) > TILE_WHOLE) {
       char* Vs = smem + st * 2 * TILEB + TILEB;
       uint32_t any = 0;
 #pragma unroll
@@ -270,7 +274,7 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
         __syncthreads();
       }
     }
-    return tile_mode(a, n, w0, w1, k0, WKT, hidden);
+    return tile_mode(a, n, w0, w1, k0, WKT, hidden, true);
   };
   // the next tile's mode, or -1 after the last
   auto next = [&]() {
@@ -279,11 +283,14 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
   };
   auto compute = [&](auto mode_c) {
     constexpr int MODE = decltype(mode_c)::value;
+    constexpr bool LATE = MODE == TILE_LATE || MODE == TILE_LATE_1;
+    constexpr bool EARLY = MODE == TILE_EARLY || MODE == TILE_EARLY_2;
+    constexpr int X0 = MODE == TILE_EARLY_2, X1 = MODE == TILE_LATE_1 ? 1 : 2;  // halves
     const char* Ks = smem + st * 2 * TILEB;
     const char* Vs = Ks + TILEB;
     f32x16_t S[2];
 #pragma unroll
-    for (int x = 0; x < 2; x++) {
+    for (int x = X0; x < X1; x++) {
 #pragma unroll
       for (int i = 0; i < 16; i++) S[x][i] = 0.f;
 #pragma unroll
@@ -295,7 +302,7 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
     // with sizes the scores of base 2; -inf for keys that the query does not see
     if (SIZES) {
 #pragma unroll
-      for (int x = 0; x < 2; x++)
+      for (int x = X0; x < X1; x++)
 #pragma unroll
         for (int i4 = 0; i4 < 4; i4++) {
           const f32x4_t ln = *(const f32x4_t*)(&lnS[st][x * 32 + 8 * i4 + 4 * hl]);
@@ -304,24 +311,24 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
         }
       if (MODE == TILE_ALL && hidden)
 #pragma unroll
-        for (int x = 0; x < 2; x++)
+        for (int x = X0; x < X1; x++)
 #pragma unroll
           for (int i = 0; i < 16; i++)
             if (lnS[st][x * 32 + 8 * (i / 4) + 4 * hl + i % 4] == -INFINITY) S[x][i] = -INFINITY;
     }
     const int lo = sp.lo - k0 - 4 * hl, hi = sp.hi - k0 - 4 * hl, first = sp.first - k0 - 4 * hl;
 #pragma unroll
-    for (int x = 0; x < 2; x++)
+    for (int x = X0; x < X1; x++)
 #pragma unroll
       for (int i = 0; i < 16; i++) {
         const int key = x * 32 + 8 * (i / 4) + i % 4;
-        if (MODE == TILE_LATE) S[x][i] = key <= hi ? S[x][i] : -INFINITY;
-        if (MODE == TILE_EARLY) S[x][i] = key >= lo ? S[x][i] : -INFINITY;
+        if (LATE) S[x][i] = key <= hi ? S[x][i] : -INFINITY;
+        if (EARLY) S[x][i] = key >= lo ? S[x][i] : -INFINITY;
         if (MODE == TILE_ALL) S[x][i] = (key <= hi) & ((key >= lo) | (key < first)) ? S[x][i] : -INFINITY;
       }
     float mt = -INFINITY;
 #pragma unroll
-    for (int x = 0; x < 2; x++)
+    for (int x = X0; x < X1; x++)
 #pragma unroll
       for (int i = 0; i < 16; i++) mt = fmaxf(mt, S[x][i]);
     mt = max_xor32(mt);
@@ -340,7 +347,7 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
     bf16x8_t pf[4];
     float lt[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int x = 0; x < 2; x++)
+    for (int x = X0; x < X1; x++)
 #pragma unroll
       for (int y = 0; y < 2; y++) {
         union { uint32_t u[4]; bf16x8_t v; } p;
@@ -356,7 +363,7 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
       }
     l += (lt[0] + lt[1]) + (lt[2] + lt[3]);
 #pragma unroll
-    for (int y = 0; y < 4; y++)
+    for (int y = 2 * X0; y < 2 * X1; y++)
 #pragma unroll
       for (int d = 0; d < ND; d++) {
         union { s16x4_t h[2]; bf16x8_t v; } vf;
@@ -382,8 +389,16 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
       compute(std::integral_constant<int, TILE_LATE>{});
       mode = next();
     }
+    while (mode == TILE_LATE_1) {
+      compute(std::integral_constant<int, TILE_LATE_1>{});
+      mode = next();
+    }
     while (mode == TILE_EARLY) {
       compute(std::integral_constant<int, TILE_EARLY>{});
+      mode = next();
+    }
+    while (mode == TILE_EARLY_2) {
+      compute(std::integral_constant<int, TILE_EARLY_2>{});
       mode = next();
     }
     while (mode == TILE_ALL) {
@@ -525,7 +540,7 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowA
     char* Vs = smem + st * 2 * TILEB + TILEB;
     bool bad = false;
     const bool hidden = SIZES && __builtin_amdgcn_readfirstlane(s_hidden[st]);  // some key of the tile has no size
-    if (tile_mode(a, n, pl.q0, pl.q1, k0, KT, hidden) > TILE_WHOLE) {
+    if (tile_mode(a, n, pl.q0, pl.q1, k0, KT, hidden, false) > TILE_WHOLE) {
       bool any = false;
 #pragma unroll
       for (int u = 0; u < TILEB / (64 * WNW * 16); u++) {
@@ -545,7 +560,7 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowA
       any_bad = true;
       __syncthreads();
     }
-    const int mode = tile_mode(a, n, w0, w1, k0, KT, hidden);
+    const int mode = tile_mode(a, n, w0, w1, k0, KT, hidden, false);
     if (mode != TILE_SKIP) {
       f32x4_t S[NT];
 #pragma unroll
