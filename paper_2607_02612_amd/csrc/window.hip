@@ -35,7 +35,10 @@ struct WindowSeqs {
 // 8 (i / 4) + 4 hl + i % 4, i < 16, of each 32-key half, so the row maximum
 // and sum are reductions over registers and one lane swap, and the registers
 // i = 8t .. 8t + 7, rounded to bf16, are the operand of the t-th step of
-// O^T = V^T P^T as they stand.  V^T comes from the row-major tile by the
+// O^T = V^T P^T as they stand.  (The matrix instruction takes no wider type
+// beside bf16 values; P as the sum of two bf16 numbers would cost half again
+// the matrix work, which is what bounds long windows.  The sum of a row takes
+// the unrounded numbers.)  V^T comes from the row-major tile by the
 // transposing LDS read, with the same key order.  The running maximum moves
 // only when a row's maximum grows by more than 8 in the base-2 exponent (P
 // stays below 2^8, whose relative precision is that of 1), per row, so that
@@ -44,8 +47,18 @@ struct WindowSeqs {
 // LDS rows are 2 DP bytes.  K's 16-byte pieces are XOR-permuted by the row mod
 // 16 (64-wide: row / 2 mod 8), V's pairs of 32-byte segments by the row mod 4
 // (row / 2 mod 2): the 16-byte reads of 16 rows and the 8-byte transposing
-// reads of 4 rows spread over all banks, and no read waits for another.  The copies write LDS in lane order, so the permutation is made in
-// the source address.
+// reads of 4 rows spread over all banks, and no read waits for another.  The
+// copies write LDS in lane order, so the permutation is made in the source
+// address.
+//
+// Measured: 16,384 rows, 16 heads of 128 over 2, window 4,096: 509 us, 950
+// TFLOP/s of the pairs in the window, where a product of 8,192^3 reaches 1,070
+// to 1,120; the matrix cores are busy half of the cycles and the clock falls
+// under the load.  8 sequences of up to 4,096 rows, 32 heads over 8, window
+// 1,024: 342 us, 755 TFLOP/s, with 18 tiles a workgroup between its first loads
+// and its stores.  64 samples of up to 577 rows, 6 heads of 64, sizes, a
+// two-sided window of 97: 38.6 us for 85 MB, bound by the vector instructions
+// of softmax and masks and by the chain of 5 tiles.
 //
 // A probability of 0 does not take a value out of P V when that value is
 // infinite or NaN.  A tile that some query of the workgroup sees and another
@@ -448,9 +461,11 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
 // 16-byte piece of a key feeds four steps (slot g of step i is dim
 // 16 u + 4 g + i).  Tiles are 8 KB of keys and as much of values (with 16 KB a
 // window of 130 took 51 us instead of 37, since more of a tile lies outside,
-// and one of 4,096 took 491 instead of 502); K's pieces are XOR-permuted by the row mod 16, V's groups of four pieces by row / 4
-// mod 4, so that the 16-byte key reads of 16 rows and the 4-byte value reads
-// of 4 x 16 spread over all banks.
+// and one of 4,096 took 491 instead of 502); K's pieces are XOR-permuted by
+// the row mod 16, V's groups of four pieces by row / 4 mod 4, so that the
+// 16-byte key reads of 16 rows and the 4-byte value reads of 4 x 16 spread over
+// all banks.  8 sequences of up to 1,031 rows, 12 heads of 64, window 130: 42 us
+// for 1.76 GFLOP in the window and 2.69 in its tiles.
 template <int DC, bool PAD, bool SIZES>
 __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowArgs a, WindowSeqs sq,
                                                                          int tiles, int hshift) {
