@@ -112,20 +112,23 @@ __device__ __forceinline__ RowSpan row_span(const WindowArgs& a, int i, int n) {
 // How rows i0 .. i1 take a tile of keys j0 .. j0 + keys - 1: not at all, with
 // no look at the pairs, with one at the later end or the earlier end of the
 // rows' spans, or with all there is (without short cuts, so that it is one
-// scalar value and the tile loop keeps its branches simple).  `halves`: the
-// ends' tiles of which the rows see one half only have modes of their own
-// (TILE_LATE_1: the first half, TILE_EARLY_2: the second).
-enum { TILE_SKIP, TILE_WHOLE, TILE_LATE, TILE_LATE_1, TILE_EARLY, TILE_EARLY_2, TILE_ALL };
+// scalar value and the tile loop keeps its branches simple).  Tiles of which the
+// rows see one half only have modes of their own (_1: the first half, _2: the
+// second): with HALVES of 1 those at the ends, with 2 also those with sinks.
+enum { TILE_SKIP, TILE_WHOLE, TILE_LATE, TILE_LATE_1, TILE_EARLY, TILE_EARLY_2, TILE_ALL, TILE_ALL_1 };
+template <int HALVES>
 __device__ __forceinline__ int tile_mode(const WindowArgs& a, int n, int i0, int i1, int j0, int keys,
-                                         bool hidden, bool halves) {
+                                         bool hidden) {
   const RowSpan r0 = row_span(a, i0, n), r1 = row_span(a, i1, n);
   const int j1 = j0 + keys - 1;
   const bool late = j1 > r0.hi, early = (j0 < r1.lo) & (j1 >= r0.first);
   const bool skip = (i0 >= n) | (j0 > r1.hi) | ((j1 < r0.lo) & (j0 >= r1.first));
   const bool all = hidden | (early & (late | (j0 < a.sinks)));
-  const int mid = j0 + keys / 2;
-  const int at_end = TILE_LATE + (halves & (mid > r1.hi)), at_start = TILE_EARLY + (halves & (mid <= r0.lo));
-  return __builtin_amdgcn_readfirstlane(skip ? TILE_SKIP : all ? TILE_ALL : late ? at_end
+  const int mid = j0 + keys / 2;  // the second half's first key
+  const int at_end = TILE_LATE + ((HALVES > 0) & (mid > r1.hi));
+  const int at_start = TILE_EARLY + ((HALVES > 0) & (mid <= r0.lo));
+  const int any = TILE_ALL + ((HALVES > 1) & ((mid > r1.hi) | ((j1 < r0.lo) & (mid >= r1.first))));
+  return __builtin_amdgcn_readfirstlane(skip ? TILE_SKIP : all ? any : late ? at_end
                                         : early ? at_start : TILE_WHOLE);
 }
 
@@ -267,7 +270,7 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
       load_size(pl.tile(it + 1));
     }
     hidden = SIZES && __builtin_amdgcn_readfirstlane(s_hidden[st]);
-    if (tile_mode(a, n, pl.q0, pl.q1, k0, WKT, hidden, false) > TILE_WHOLE) {
+    if (tile_mode<0>(a, n, pl.q0, pl.q1, k0, WKT, hidden) > TILE_WHOLE) {
       char* Vs = smem + st * 2 * TILEB + TILEB;
       uint32_t any = 0;
 #pragma unroll
@@ -287,7 +290,7 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
         __syncthreads();
       }
     }
-    return tile_mode(a, n, w0, w1, k0, WKT, hidden, true);
+    return tile_mode<1>(a, n, w0, w1, k0, WKT, hidden);
   };
   // the next tile's mode, or -1 after the last
   auto next = [&]() {
@@ -464,8 +467,9 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
 // and one of 4,096 took 491 instead of 502); K's pieces are XOR-permuted by
 // the row mod 16, V's groups of four pieces by row / 4 mod 4, so that the
 // 16-byte key reads of 16 rows and the 4-byte value reads of 4 x 16 spread over
-// all banks.  8 sequences of up to 1,031 rows, 12 heads of 64, window 130: 42 us
-// for 1.76 GFLOP in the window and 2.69 in its tiles.
+// all banks.  8 sequences of up to 1,031 rows, 12 heads of 64, window 130, 1.76
+// GFLOP in the window: 40.5 us (42.2 with whole tiles only, which made 2.69 of
+// them; with a window of 4,096 the loops for parts of a tile cost 1 %).
 template <int DC, bool PAD, bool SIZES>
 __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowArgs a, WindowSeqs sq,
                                                                          int tiles, int hshift) {
@@ -543,19 +547,22 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowA
 #pragma unroll
   for (int d = 0; d < NU; d++) O[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
-  for (int it = 0; it < pl.nt; it++) {
-    const int st = it & 1, t = pl.tile(it), k0 = t * KT;
+  int it = 0, st = 0, k0 = 0;  // the tile in hand: its number, LDS stage and first key
+  bool hidden = false;         // some key of it has no size
+  int mode = 0;                // how the wave takes it, or -1 after the last
+  auto begin = [&]() {
+    st = it & 1;
+    k0 = pl.tile(it) * KT;
     wait_copies();
     __syncthreads();
     if (it + 1 < pl.nt) {
       copy_tile(pl.tile(it + 1), st ^ 1);
       load_size(pl.tile(it + 1));
     }
-    const char* Ks = smem + st * 2 * TILEB;
     char* Vs = smem + st * 2 * TILEB + TILEB;
     bool bad = false;
-    const bool hidden = SIZES && __builtin_amdgcn_readfirstlane(s_hidden[st]);  // some key of the tile has no size
-    if (tile_mode(a, n, pl.q0, pl.q1, k0, KT, hidden, false) > TILE_WHOLE) {
+    hidden = SIZES && __builtin_amdgcn_readfirstlane(s_hidden[st]);
+    if (tile_mode<0>(a, n, pl.q0, pl.q1, k0, KT, hidden) > TILE_WHOLE) {
       bool any = false;
 #pragma unroll
       for (int u = 0; u < TILEB / (64 * WNW * 16); u++) {
@@ -575,78 +582,118 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowA
       any_bad = true;
       __syncthreads();
     }
-    const int mode = tile_mode(a, n, w0, w1, k0, KT, hidden, false);
-    if (mode != TILE_SKIP) {
-      f32x4_t S[NT];
+    mode = tile_mode<(NT > 1 ? 2 : 0)>(a, n, w0, w1, k0, KT, hidden);
+  };
+  auto next = [&]() {
+    if (it + 1 < pl.nt) put_size(st ^ 1);
+    if (++it < pl.nt) begin(); else mode = -1;
+  };
+  // 16-key parts X0 .. X1 - 1; EDGES: some may be unseen
+  auto compute = [&](auto x0_c, auto x1_c, auto edges_c) {
+    constexpr int X0 = decltype(x0_c)::value, X1 = decltype(x1_c)::value;
+    constexpr bool EDGES = decltype(edges_c)::value;
+    const char* Ks = smem + st * 2 * TILEB;
+    const char* Vs = Ks + TILEB;
+    f32x4_t S[NT];
 #pragma unroll
-      for (int x = 0; x < NT; x++) S[x] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int x = X0; x < X1; x++) S[x] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int u = 0; u < NU; u++) {
-        f32x4_t kf[NT];
+    for (int u = 0; u < NU; u++) {
+      f32x4_t kf[NT];
 #pragma unroll
-        for (int x = 0; x < NT; x++)
-          kf[x] = *(const f32x4_t*)(Ks + (16 * x + c) * ROWB + (((4 * u + g) ^ c) << 4));
+      for (int x = X0; x < X1; x++)
+        kf[x] = *(const f32x4_t*)(Ks + (16 * x + c) * ROWB + (((4 * u + g) ^ c) << 4));
 #pragma unroll
-        for (int i = 0; i < 4; i++)
+      for (int i = 0; i < 4; i++)
 #pragma unroll
-          for (int x = 0; x < NT; x++)
-            S[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[x][i], qf[u][i], S[x], 0, 0, 0);
+        for (int x = X0; x < X1; x++)
+          S[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[x][i], qf[u][i], S[x], 0, 0, 0);
+    }
+#pragma unroll
+    for (int x = X0; x < X1; x++) {
+      f32x4_t ln = {0.f, 0.f, 0.f, 0.f};
+      if (SIZES) ln = *(const f32x4_t*)(&lnS[st][16 * x + 4 * g]);
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        S[x][j] = fmaf(S[x][j], sc2, ln[j]);
+        if (EDGES && hidden && ln[j] == -INFINITY) S[x][j] = -INFINITY;
       }
+    }
+    if (EDGES && mode > TILE_WHOLE) {
+      const int lo = sp.lo - k0 - 4 * g, hi = sp.hi - k0 - 4 * g, first = sp.first - k0 - 4 * g;
 #pragma unroll
-      for (int x = 0; x < NT; x++) {
-        f32x4_t ln = {0.f, 0.f, 0.f, 0.f};
-        if (SIZES) ln = *(const f32x4_t*)(&lnS[st][16 * x + 4 * g]);
+      for (int x = X0; x < X1; x++)
 #pragma unroll
         for (int j = 0; j < 4; j++) {
-          S[x][j] = fmaf(S[x][j], sc2, ln[j]);
-          if (hidden && ln[j] == -INFINITY) S[x][j] = -INFINITY;
-        }
-      }
-      if (mode > TILE_WHOLE) {
-        const int lo = sp.lo - k0 - 4 * g, hi = sp.hi - k0 - 4 * g, first = sp.first - k0 - 4 * g;
-#pragma unroll
-        for (int x = 0; x < NT; x++)
-#pragma unroll
-          for (int j = 0; j < 4; j++) {
-            const int key = 16 * x + j;
-            S[x][j] = (key <= hi) & ((key >= lo) | (key < first)) ? S[x][j] : -INFINITY;
-          }
-      }
-      float mt = -INFINITY;
-#pragma unroll
-      for (int x = 0; x < NT; x++)
-#pragma unroll
-        for (int j = 0; j < 4; j++) mt = fmaxf(mt, S[x][j]);
-      mt = max_xor32(max_xor16(mt));
-      const bool grow = mt > m + 8.f;
-      if (__any(grow)) {
-        const float f = grow ? __builtin_amdgcn_exp2f(m - mt) : 1.f;
-        if (grow) m = mt;
-        l *= f;
-#pragma unroll
-        for (int d = 0; d < NU; d++)
-#pragma unroll
-          for (int j = 0; j < 4; j++) O[d][j] *= f;
-      }
-      const float mu = m == -INFINITY ? 0.f : m;
-#pragma unroll
-      for (int x = 0; x < NT; x++) {
-#pragma unroll
-        for (int j = 0; j < 4; j++) S[x][j] = __builtin_amdgcn_exp2f(S[x][j] - mu);
-        l += (S[x][0] + S[x][1]) + (S[x][2] + S[x][3]);
-      }
-#pragma unroll
-      for (int x = 0; x < NT; x++)
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-          const char* vr = Vs + (16 * x + 4 * g + j) * ROWB + (c & 3) * 4;
-#pragma unroll
-          for (int d = 0; d < NU; d++)
-            O[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(
-                *(const float*)(vr + (((4 * d + (c >> 2)) ^ (g << 2)) << 4)), S[x][j], O[d], 0, 0, 0);
+          const int key = 16 * x + j;
+          S[x][j] = (key <= hi) & ((key >= lo) | (key < first)) ? S[x][j] : -INFINITY;
         }
     }
-    if (it + 1 < pl.nt) put_size(st ^ 1);
+    float mt = -INFINITY;
+#pragma unroll
+    for (int x = X0; x < X1; x++)
+#pragma unroll
+      for (int j = 0; j < 4; j++) mt = fmaxf(mt, S[x][j]);
+    mt = max_xor32(max_xor16(mt));
+    const bool grow = mt > m + 8.f;
+    if (__any(grow)) {
+      const float f = grow ? __builtin_amdgcn_exp2f(m - mt) : 1.f;
+      if (grow) m = mt;
+      l *= f;
+#pragma unroll
+      for (int d = 0; d < NU; d++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) O[d][j] *= f;
+    }
+    const float mu = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int x = X0; x < X1; x++) {
+#pragma unroll
+      for (int j = 0; j < 4; j++) S[x][j] = __builtin_amdgcn_exp2f(S[x][j] - mu);
+      l += (S[x][0] + S[x][1]) + (S[x][2] + S[x][3]);
+    }
+#pragma unroll
+    for (int x = X0; x < X1; x++)
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        const char* vr = Vs + (16 * x + 4 * g + j) * ROWB + (c & 3) * 4;
+#pragma unroll
+        for (int d = 0; d < NU; d++)
+          O[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+              *(const float*)(vr + (((4 * d + (c >> 2)) ^ (g << 2)) << 4)), S[x][j], O[d], 0, 0, 0);
+      }
+  };
+  // (a loop for each set of parts, as above; where there is one set, one loop
+  // takes 126 registers, with which 4 waves share a SIMD, and two take 163)
+  constexpr std::integral_constant<int, 0> none;
+  constexpr std::integral_constant<int, NT / 2> half;
+  constexpr std::integral_constant<int, NT> whole;
+  begin();
+  if constexpr (NT > 1) {
+    while (mode >= 0) {
+      while (mode == TILE_LATE_1 || mode == TILE_ALL_1) {
+        compute(none, half, std::true_type{});
+        next();
+      }
+      while (mode == TILE_EARLY_2) {
+        compute(half, whole, std::true_type{});
+        next();
+      }
+      while (mode == TILE_LATE || mode == TILE_EARLY || mode == TILE_ALL) {
+        compute(none, whole, std::true_type{});
+        next();
+      }
+      while (mode == TILE_WHOLE) {
+        compute(none, whole, std::false_type{});
+        next();
+      }
+      while (mode == TILE_SKIP) next();
+    }
+  } else {
+    while (mode >= 0) {
+      if (mode != TILE_SKIP) compute(none, whole, std::true_type{});
+      next();
+    }
   }
   if (any_bad && w0 + c < n) {  // the values that were cleared, for the rows that see them
     for (int it = 0; it < pl.nt; it++)
