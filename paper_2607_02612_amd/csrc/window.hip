@@ -57,7 +57,7 @@ struct WindowSeqs {
 // under the load.  8 sequences of up to 4,096 rows, 32 heads over 8, window
 // 1,024: 342 us, 755 TFLOP/s, with 18 tiles a workgroup between its first loads
 // and its stores.  64 samples of up to 577 rows, 6 heads of 64, sizes, a
-// two-sided window of 97: 38.6 us for 85 MB, bound by the vector instructions
+// two-sided window of 97: 37.0 us for 85 MB, bound by the vector instructions
 // of softmax and masks and by the chain of 5 tiles.
 //
 // A probability of 0 does not take a value out of P V when that value is
@@ -162,6 +162,20 @@ __device__ __forceinline__ WindowPlan window_plan(const WindowArgs& a, const Win
   return p;
 }
 
+// The place of a workgroup in the line of row tiles times head units.
+// Workgroups go to the 8 XCDs in turn; with a window of at most NEAR_WINDOW
+// rows, NEAR row tiles in a row go to one of them, whose L2 then reads the keys
+// that they share once (64 samples of up to 577 rows, window 97: 38.6 us in
+// turn, 37.0 so; 4 of 4,096 rows, 12 heads of 80 over 4, window 512: 83, 78).
+// Longer windows are not bound by what they read, and under none the last rows
+// of a sample see most, so that an XCD with many of them ends late (window
+// 1,024: 352 us in turn, 365 so; 8 of 4,096 rows and no window: 288, 441).
+constexpr int NEAR = 8, NEAR_WINDOW = 512;
+__device__ __forceinline__ int place(const WindowArgs& a, int units) {
+  const unsigned b = blockIdx.x, run = NEAR * units, round = 8 * run, in = b % round;
+  return a.window <= NEAR_WINDOW && b - in + round <= gridDim.x ? b - in + in % 8 * run + in / 8 : b;
+}
+
 template <int DC, bool PAD, bool SIZES>
 __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_mfma(WindowArgs a, WindowSeqs sq,
                                                                      int tiles, int hshift) {
@@ -177,9 +191,9 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int hl = lane >> 5, c = lane & 31;
   const int per_group = a.group >> hshift, units = a.H >> hshift;
-  const int unit = blockIdx.x % units, kh = unit / per_group;
+  const int at = place(a, units), unit = at % units, kh = unit / per_group;
   const int h = unit % per_group * (1 << hshift) + kh * a.group + (wave & ((1 << hshift) - 1));
-  const WindowPlan pl = window_plan(a, sq, tiles - 1 - blockIdx.x / units,
+  const WindowPlan pl = window_plan(a, sq, tiles - 1 - at / units,
                                     32 * (WNW >> hshift), WKT);
   const int n = pl.n, dh = a.dh;
   const int w0 = pl.q0 + 32 * (wave >> hshift), w1 = min(w0 + 31, n - 1);
@@ -483,9 +497,9 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowA
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int g = lane >> 4, c = lane & 15;
   const int per_group = a.group >> hshift, units = a.H >> hshift;
-  const int unit = blockIdx.x % units, kh = unit / per_group;
+  const int at = place(a, units), unit = at % units, kh = unit / per_group;
   const int h = unit % per_group * (1 << hshift) + kh * a.group + (wave & ((1 << hshift) - 1));
-  const WindowPlan pl = window_plan(a, sq, tiles - 1 - blockIdx.x / units, 16 * (WNW >> hshift), KT);
+  const WindowPlan pl = window_plan(a, sq, tiles - 1 - at / units, 16 * (WNW >> hshift), KT);
   const int n = pl.n, dh = a.dh;
   const int w0 = pl.q0 + 16 * (wave >> hshift), w1 = min(w0 + 15, n - 1);
   const float* kg = (const float*)a.k + (int64_t)pl.base * a.k_row + (int64_t)kh * a.k_head;
