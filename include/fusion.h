@@ -475,8 +475,8 @@ FUSION_API int fusion_paged_attention(const fusion_cache* c, const void* q, cons
  * (ties to the lower slot; NaN below everything), budget in all.  Kept tokens
  * in slots below the budget stay where they are; those beyond move, lowest
  * slot first, into the slots that became free, lowest first, with their
- * weight and position.  len becomes the budget; what slots past it hold is
- * left as it was.  src: device int32 [batch][budget], the slot that each slot's
+ * weight and position (keys and values only where both slots have a page).
+ * len becomes the budget; what slots past it hold is left as it was.  src: device int32 [batch][budget], the slot that each slot's
  * token was in before the call, -1 past len.  ws as above
  * (fusion_cache_evict_workspace_bytes).  Errors: FUSION_E_INVALID_ARG,
  * FUSION_E_CAPACITY, FUSION_E_HIP. */

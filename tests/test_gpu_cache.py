@@ -198,6 +198,22 @@ def test_window_attention_strides_out_and_padding(torch_cuda):
     assert kern.window_attention(q[:0], k[:0], v[:0], [0, 0, 0]).shape == (0, 4, 64)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("causal", [True, False])
+def test_window_attention_ends_within_tiles(torch_cuda, dtype, dh, causal):
+    """Windows and first rows that end at, before and after halves of tiles."""
+    torch = torch_cuda
+    rng = np.random.default_rng(dh + causal)
+    cu = np.array([0, 197, 230])
+    q, k, v = (_normal(torch, rng, dtype, 230, 1, dh) for _ in range(3))
+    for window in (2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 95, 96, 97, 128, 129):
+        for sinks in (0, 1, 16, 33):
+            got = _kern().window_attention(q, k, v, cu, window, sinks, causal)
+            ref, tol = _window_ref(_np(q), _np(k), _np(v), cu, window, sinks, causal, None, dtype)
+            _close(_np(got), ref, tol, (window, sinks))
+
+
 @pytest.mark.parametrize("B", [127, 128, 129, 256, 448, 1000])
 def test_window_attention_many_samples(torch_cuda, B):
     """More samples than one launch describes."""
@@ -376,6 +392,23 @@ def test_paged_attention_many_sequences(torch_cuda, B):
     out, tol, add, add_tol = _paged_ref(_np(q), c, 60, 2, "bf16")
     _close(_np(_kern().paged_attention(q, c, 60, 2)), out, tol)
     assert (np.abs(_np(c.weight) - before - add) <= add_tol + U32 * (before + add)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_paged_attention_caches_in_and_out_of_order(torch_cuda, dtype):
+    """Sequences with and without evicted tokens in turn, several to a wave."""
+    torch = torch_cuda
+    rng = np.random.default_rng(77)
+    lengths = rng.integers(0, 300, size=40)
+    seen = lengths + np.where(np.arange(40) % 3 == 1, rng.integers(1, 90, size=40), 0)
+    cache = _cache(torch, rng, dtype, lengths, 64, 8, 16, 304, seen=seen)
+    q = _normal(torch, rng, dtype, 40, 64, 8)
+    before = _np(cache.weight)
+    got = _kern().paged_attention(q, cache, 100, 3)
+    ref, tol, add, add_tol = _paged_ref(_np(q), cache, 100, 3, dtype)
+    _close(_np(got), ref, tol)
+    after = before + add
+    _close(_np(cache.weight), after, add_tol + U32 * np.abs(after))
 
 
 @pytest.mark.parametrize("seen", [-(1 << 31), 0, (1 << 31) - 1])
