@@ -484,24 +484,31 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
 // all banks.  8 sequences of up to 1,031 rows, 12 heads of 64, window 130, 1.76
 // GFLOP in the window: 40.5 us (42.2 with whole tiles only, which made 2.69 of
 // them; with a window of 4,096 the loops for parts of a tile cost 1 %).
-template <int DC, bool PAD, bool SIZES>
+//
+// SPLIT: the waves share the keys of a row tile instead, 16 keys each of tiles
+// of twice the size, with a maximum, sum and output of their own that are
+// joined through LDS at the end (4 waves a row tile of 64-wide heads, 2 of
+// wider ones).  share_keys says when.
+template <int DC, bool PAD, bool SIZES, bool SPLIT>
 __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowArgs a, WindowSeqs sq,
                                                                          int tiles, int hshift) {
   constexpr int DP = DC <= 64 ? 64 : 128;
   constexpr int PPR = DP / 4, RPC = 64 / PPR;  // pieces per row, rows per copy
-  constexpr int TILEB = 8192, ROWB = DP * 4, KT = TILEB / ROWB;
-  constexpr int NC = KT / RPC / WNW, NT = KT / 16, NU = DC / 16;
+  constexpr int TILEB = SPLIT ? 16384 : 8192, ROWB = DP * 4, KT = TILEB / ROWB;
+  constexpr int PARTS = SPLIT ? KT / 16 : 1, KW = KT / PARTS;  // waves of a row tile, keys of each
+  constexpr int NC = KT / RPC / WNW, NT = KW / 16, NU = DC / 16;
   __shared__ __attribute__((aligned(16))) char smem[4 * TILEB];  // [stage][K, V]
   __shared__ __attribute__((aligned(16))) float lnS[2][KT];
   __shared__ int s_bad, s_hidden[2];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int g = lane >> 4, c = lane & 15;
+  const int part = wave % PARTS, who = wave / PARTS;
   const int per_group = a.group >> hshift, units = a.H >> hshift;
   const int at = place(a, units), unit = at % units, kh = unit / per_group;
-  const int h = unit % per_group * (1 << hshift) + kh * a.group + (wave & ((1 << hshift) - 1));
-  const WindowPlan pl = window_plan(a, sq, tiles - 1 - at / units, 16 * (WNW >> hshift), KT);
+  const int h = unit % per_group * (1 << hshift) + kh * a.group + (who & ((1 << hshift) - 1));
+  const WindowPlan pl = window_plan(a, sq, tiles - 1 - at / units, 16 * (WNW / PARTS >> hshift), KT);
   const int n = pl.n, dh = a.dh;
-  const int w0 = pl.q0 + 16 * (wave >> hshift), w1 = min(w0 + 15, n - 1);
+  const int w0 = pl.q0 + 16 * (who >> hshift), w1 = min(w0 + 15, n - 1);
   const float* kg = (const float*)a.k + (int64_t)pl.base * a.k_row + (int64_t)kh * a.k_head;
   const float* vg = (const float*)a.v + (int64_t)pl.base * a.v_row + (int64_t)kh * a.v_head;
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
@@ -596,7 +603,7 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowA
       any_bad = true;
       __syncthreads();
     }
-    mode = tile_mode<(NT > 1 ? 2 : 0)>(a, n, w0, w1, k0, KT, hidden);
+    mode = tile_mode<(NT > 1 ? 2 : 0)>(a, n, w0, w1, k0 + part * KW, KW, hidden);
   };
   auto next = [&]() {
     if (it + 1 < pl.nt) put_size(st ^ 1);
@@ -606,8 +613,9 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowA
   auto compute = [&](auto x0_c, auto x1_c, auto edges_c) {
     constexpr int X0 = decltype(x0_c)::value, X1 = decltype(x1_c)::value;
     constexpr bool EDGES = decltype(edges_c)::value;
-    const char* Ks = smem + st * 2 * TILEB;
+    const char* Ks = smem + st * 2 * TILEB + part * KW * ROWB;
     const char* Vs = Ks + TILEB;
+    const int kp = k0 + part * KW;
     f32x4_t S[NT];
 #pragma unroll
     for (int x = X0; x < X1; x++) S[x] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -626,7 +634,7 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowA
 #pragma unroll
     for (int x = X0; x < X1; x++) {
       f32x4_t ln = {0.f, 0.f, 0.f, 0.f};
-      if (SIZES) ln = *(const f32x4_t*)(&lnS[st][16 * x + 4 * g]);
+      if (SIZES) ln = *(const f32x4_t*)(&lnS[st][part * KW + 16 * x + 4 * g]);
 #pragma unroll
       for (int j = 0; j < 4; j++) {
         S[x][j] = fmaf(S[x][j], sc2, ln[j]);
@@ -634,7 +642,7 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowA
       }
     }
     if (EDGES && mode > TILE_WHOLE) {
-      const int lo = sp.lo - k0 - 4 * g, hi = sp.hi - k0 - 4 * g, first = sp.first - k0 - 4 * g;
+      const int lo = sp.lo - kp - 4 * g, hi = sp.hi - kp - 4 * g, first = sp.first - kp - 4 * g;
 #pragma unroll
       for (int x = X0; x < X1; x++)
 #pragma unroll
@@ -709,6 +717,31 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowA
       next();
     }
   }
+  if constexpr (SPLIT) {  // the parts of a row tile joined, by the first of its waves
+    __syncthreads();
+    f32x4_t* Os = (f32x4_t*)smem + lane;
+    float2* ml = (float2*)(smem + WNW * NU * 1024) + lane;
+#pragma unroll
+    for (int d = 0; d < NU; d++) Os[(wave * NU + d) * 64] = O[d];
+    ml[wave * 64] = make_float2(m, l);
+    __syncthreads();
+    if (part != 0) return;
+    float top = m;
+#pragma unroll
+    for (int p = 1; p < PARTS; p++) top = fmaxf(top, ml[(wave + p) * 64].x);
+    const float mu = top == -INFINITY ? 0.f : top, f0 = __builtin_amdgcn_exp2f(m - mu);
+    l *= f0;
+#pragma unroll
+    for (int d = 0; d < NU; d++) O[d] *= f0;
+#pragma unroll
+    for (int p = 1; p < PARTS; p++) {
+      const float2 x = ml[(wave + p) * 64];
+      const float f = __builtin_amdgcn_exp2f(x.x - mu);
+      l = fmaf(x.y, f, l);
+#pragma unroll
+      for (int d = 0; d < NU; d++) O[d] += Os[((wave + p) * NU + d) * 64] * f;
+    }
+  }
   if (any_bad && w0 + c < n) {  // the values that were cleared, for the rows that see them
     for (int it = 0; it < pl.nt; it++)
       for (int j = pl.tile(it) * KT; j < min(n, pl.tile(it) * KT + KT); j++) {
@@ -753,25 +786,55 @@ hipError_t for_samples(const int32_t* cu_host, int batch, int rows, F launch) {
   return hipSuccess;
 }
 
+// Whether the waves of a workgroup share the keys of its row tiles, `parts` waves
+// a tile, instead of having a row tile each: where that many more workgroups
+// still run at once (2 a CU), or where the rows see so many keys that the last
+// workgroups' chains of tiles are what the call takes (fp32, one sample, causal;
+// row tiles each / shared: 1,536 rows, 6 heads of 64, window 964, 144
+// workgroups, 59 us / 31; 512 rows, 16 heads of 128, window 300, 128: 40 / 25;
+// 4,096 rows, 6 heads of 64, no window, 384: 234 / 160; but 2,048 rows, window
+// 200, 192: 21 / 26, and 5,120, window 1,000, 480: 94 / 109).
+bool share_keys(const WindowArgs& a, const int32_t* cu_host, int batch, int rows, int units,
+                int parts) {
+  int64_t groups = 0, longest = 0;
+  for (int i = 0; i < batch; i++) {
+    const int64_t n = cu_host[i + 1] - cu_host[i];
+    groups += (n + rows - 1) / rows;
+    longest = std::max(longest, n);
+  }
+  groups *= units;
+  return groups * parts <= 512 || std::min(longest, (int64_t)a.window * (a.causal ? 1 : 2)) >= 4 * groups;
+}
+
 template <typename T, int DC, bool PAD>
 hipError_t launch_mfma(const WindowArgs& a, const int32_t* cu_host, int batch, hipStream_t s) {
   // heads of a group per workgroup, 1 << hshift
   const int hshift = a.group % 4 == 0 ? 2 : a.group % 2 == 0 ? 1 : 0;
   const int rows = (sizeof(T) == 2 ? 32 : 16) * (WNW >> hshift);
-  return for_samples(cu_host, batch, rows, [&](const WindowSeqs& sq, int tiles) {
-    const dim3 grid((unsigned)tiles * (a.H >> hshift));
-    if constexpr (sizeof(T) == 2) {
+  if constexpr (sizeof(T) == 2) {
+    return for_samples(cu_host, batch, rows, [&](const WindowSeqs& sq, int tiles) {
+      const dim3 grid((unsigned)tiles * (a.H >> hshift));
       if (a.size)
         window_attention_mfma<DC, PAD, true><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
       else
         window_attention_mfma<DC, PAD, false><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
-    } else {
-      if (a.size)
-        window_attention_mfma_f32<DC, PAD, true><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
-      else
-        window_attention_mfma_f32<DC, PAD, false><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
-    }
-  });
+    });
+  } else {
+    const auto run = [&](auto split_c, int rows, int hshift) {
+      constexpr bool SPLIT = decltype(split_c)::value;
+      return for_samples(cu_host, batch, rows, [&](const WindowSeqs& sq, int tiles) {
+        const dim3 grid((unsigned)tiles * (a.H >> hshift));
+        if (a.size)
+          window_attention_mfma_f32<DC, PAD, true, SPLIT><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
+        else
+          window_attention_mfma_f32<DC, PAD, false, SPLIT><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
+      });
+    };
+    constexpr int parts = DC <= 64 ? 4 : 2;
+    return share_keys(a, cu_host, batch, rows, a.H >> hshift, parts)
+               ? run(std::true_type{}, 16 * (WNW / parts), 0)
+               : run(std::false_type{}, rows, hshift);
+  }
 }
 
 }  // namespace

@@ -214,6 +214,30 @@ def test_window_attention_ends_within_tiles(torch_cuda, dtype, dh, causal):
             _close(_np(got), ref, tol, (window, sinks))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("dh", [64, 72, 128])
+@pytest.mark.parametrize("rows", [130, 2000])
+def test_window_attention_few_and_many_row_tiles(torch_cuda, dtype, dh, rows):
+    """Calls whose waves share the keys of a row tile, and calls of many row
+    tiles, with infinities and NaN in rows that are not seen."""
+    torch = torch_cuda
+    rng = np.random.default_rng(rows + dh)
+    q, k, v = (_normal(torch, rng, dtype, rows + 61, 9, dh) for _ in range(3))
+    cu = [0, rows, rows + 61]
+    v[rows + 20] = float("nan")
+    v[rows + 21] = float("-inf")
+    k[rows + 20:rows + 22] = float("inf")
+    size = torch.ones(rows + 61, device="cuda")
+    size[rows + 20:rows + 22] = 0
+    for heads, causal in ((1, True), (9, False)):
+        got = _kern().window_attention(q[:, :heads], k[:, :heads], v[:, :heads], cu, 70, 3, causal, size)
+        kz, vz = _np(k[:, :heads]), _np(v[:, :heads])
+        kz[~np.isfinite(kz)] = 0
+        vz[~np.isfinite(vz)] = 0
+        ref, tol = _window_ref(_np(q[:, :heads]), kz, vz, cu, 70, 3, causal, _np(size), dtype)
+        _close(_np(got), ref, tol)
+
+
 @pytest.mark.parametrize("B", [127, 128, 129, 256, 448, 1000])
 def test_window_attention_many_samples(torch_cuda, B):
     """More samples than one launch describes."""
