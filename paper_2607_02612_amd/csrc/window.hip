@@ -51,6 +51,11 @@ struct WindowSeqs {
 // copies write LDS in lane order, so the permutation is made in the source
 // address.
 //
+// SPLIT: the waves share the keys of a row tile instead, 32 keys each, with a
+// maximum, sum and output of their own that are joined through LDS at the end
+// (4 waves a row tile of 64-wide heads, with tiles of 128 keys, 2 of wider
+// ones).  share_keys says when.
+//
 // Measured: 16,384 rows, 16 heads of 128 over 2, window 4,096: 509 us, 950
 // TFLOP/s of the pairs in the window, where a product of 8,192^3 reaches 1,070
 // to 1,120; the matrix cores are busy half of the cycles and the clock falls
@@ -71,7 +76,6 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int WKT = 64;  // keys per tile
 constexpr int WNW = 4;   // waves per workgroup
 
 // global -> LDS copy of 16 bytes per lane (lane l's land at the wave-uniform
@@ -176,27 +180,31 @@ __device__ __forceinline__ int place(const WindowArgs& a, int units) {
   return a.window <= NEAR_WINDOW && b - in + round <= gridDim.x ? b - in + in % 8 * run + in / 8 : b;
 }
 
-template <int DC, bool PAD, bool SIZES>
-__global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_mfma(WindowArgs a, WindowSeqs sq,
+template <int DC, bool PAD, bool SIZES, bool SPLIT>
+__global__ __launch_bounds__(64 * WNW, DC == 64 && !SPLIT ? 3 : 2) void window_attention_mfma(WindowArgs a, WindowSeqs sq,
                                                                      int tiles, int hshift) {
   constexpr int DP = DC <= 64 ? 64 : 128;  // dims of an LDS row; DC of them take part
   constexpr int PPR = DP / 8;             // 16-byte pieces per row
   constexpr int RPC = 64 / PPR;           // rows per copy
-  constexpr int NC = WKT / RPC / WNW;     // copies of K (and of V) per wave and tile
-  constexpr int ROWB = DP * 2, TILEB = WKT * ROWB;
+  constexpr int PARTS = SPLIT ? (DC == 64 ? 4 : 2) : 1;  // waves of a row tile
+  constexpr int KW = SPLIT ? 32 : 64, KT = KW * PARTS;   // keys of a wave, of a tile
+  constexpr int NX = KW / 32;
+  constexpr int NC = KT / RPC / WNW;      // copies of K (and of V) per wave and tile
+  constexpr int ROWB = DP * 2, TILEB = KT * ROWB;
   constexpr int KS = DC / 16, ND = DC / 32;
   __shared__ __attribute__((aligned(16))) char smem[4 * TILEB];  // [stage][K, V]
-  __shared__ __attribute__((aligned(16))) float lnS[2][WKT];
-  __shared__ int s_bad, s_hidden[2];
+  __shared__ __attribute__((aligned(16))) float lnS[2][KT];
+  __shared__ int s_bad, s_hidden[2][2];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int hl = lane >> 5, c = lane & 31;
+  const int part = wave % PARTS, who = wave / PARTS;
   const int per_group = a.group >> hshift, units = a.H >> hshift;
   const int at = place(a, units), unit = at % units, kh = unit / per_group;
-  const int h = unit % per_group * (1 << hshift) + kh * a.group + (wave & ((1 << hshift) - 1));
+  const int h = unit % per_group * (1 << hshift) + kh * a.group + (who & ((1 << hshift) - 1));
   const WindowPlan pl = window_plan(a, sq, tiles - 1 - at / units,
-                                    32 * (WNW >> hshift), WKT);
+                                    32 * (WNW / PARTS >> hshift), KT);
   const int n = pl.n, dh = a.dh;
-  const int w0 = pl.q0 + 32 * (wave >> hshift), w1 = min(w0 + 31, n - 1);
+  const int w0 = pl.q0 + 32 * (who >> hshift), w1 = min(w0 + 31, n - 1);
   const bf16_t* kg = (const bf16_t*)a.k + (int64_t)pl.base * a.k_row + (int64_t)kh * a.k_head;
   const bf16_t* vg = (const bf16_t*)a.v + (int64_t)pl.base * a.v_row + (int64_t)kh * a.v_head;
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
@@ -209,7 +217,7 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
 
   // copy of one tile: the wave's rows r = (wave NC + u) RPC + lane / PPR
   auto copy_tile = [&](int t, int st) {
-    const int k0 = t * WKT, lim = n - 1 - k0;
+    const int k0 = t * KT, lim = n - 1 - k0;
     const bf16_t* kt = kg + (int64_t)k0 * a.k_row;
     const bf16_t* vt = vg + (int64_t)k0 * a.v_row;
 #pragma unroll
@@ -231,13 +239,13 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
   };
   float size_next = 0.f;
   auto load_size = [&](int t) {
-    if (SIZES && tid < WKT) size_next = a.size[pl.base + min(t * WKT + tid, n - 1)];
+    if (SIZES && tid < KT) size_next = a.size[pl.base + min(t * KT + tid, n - 1)];
   };
   auto put_size = [&](int st) {
-    if (SIZES && tid < WKT) {
+    if (SIZES && tid < KT) {
       lnS[st][tid] = size_next > 0.f ? logf(size_next) * kLog2e : -INFINITY;
       const bool hidden = __any(!(size_next > 0.f));
-      if (tid == 0) s_hidden[st] = hidden;
+      if (lane == 0) s_hidden[st][wave] = hidden;
     }
   };
   copy_tile(pl.tile(0), 0);
@@ -276,15 +284,15 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
   // may meet; returns how the wave takes it
   auto begin = [&]() {
     st = it & 1;
-    k0 = pl.tile(it) * WKT;
+    k0 = pl.tile(it) * KT;
     wait_copies();
     __syncthreads();
     if (it + 1 < pl.nt) {
       copy_tile(pl.tile(it + 1), st ^ 1);
       load_size(pl.tile(it + 1));
     }
-    hidden = SIZES && __builtin_amdgcn_readfirstlane(s_hidden[st]);
-    if (tile_mode<0>(a, n, pl.q0, pl.q1, k0, WKT, hidden) > TILE_WHOLE) {
+    hidden = SIZES && __builtin_amdgcn_readfirstlane(s_hidden[st][0] | (KT > 64 ? s_hidden[st][1] : 0));
+    if (tile_mode<0>(a, n, pl.q0, pl.q1, k0, KT, hidden) > TILE_WHOLE) {
       char* Vs = smem + st * 2 * TILEB + TILEB;
       uint32_t any = 0;
 #pragma unroll
@@ -304,7 +312,7 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
         __syncthreads();
       }
     }
-    return tile_mode<1>(a, n, w0, w1, k0, WKT, hidden);
+    return tile_mode<(NX > 1)>(a, n, w0, w1, k0 + part * KW, KW, hidden);
   };
   // the next tile's mode, or -1 after the last
   auto next = [&]() {
@@ -315,10 +323,10 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
     constexpr int MODE = decltype(mode_c)::value;
     constexpr bool LATE = MODE == TILE_LATE || MODE == TILE_LATE_1;
     constexpr bool EARLY = MODE == TILE_EARLY || MODE == TILE_EARLY_2;
-    constexpr int X0 = MODE == TILE_EARLY_2, X1 = MODE == TILE_LATE_1 ? 1 : 2;  // halves
-    const char* Ks = smem + st * 2 * TILEB;
+    constexpr int X0 = MODE == TILE_EARLY_2, X1 = MODE == TILE_LATE_1 ? 1 : NX;  // halves
+    const char* Ks = smem + st * 2 * TILEB + part * KW * ROWB;
     const char* Vs = Ks + TILEB;
-    f32x16_t S[2];
+    f32x16_t S[NX];
 #pragma unroll
     for (int x = X0; x < X1; x++) {
 #pragma unroll
@@ -335,7 +343,7 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
       for (int x = X0; x < X1; x++)
 #pragma unroll
         for (int i4 = 0; i4 < 4; i4++) {
-          const f32x4_t ln = *(const f32x4_t*)(&lnS[st][x * 32 + 8 * i4 + 4 * hl]);
+          const f32x4_t ln = *(const f32x4_t*)(&lnS[st][part * KW + x * 32 + 8 * i4 + 4 * hl]);
 #pragma unroll
           for (int j = 0; j < 4; j++) S[x][4 * i4 + j] = fmaf(S[x][4 * i4 + j], sc2, ln[j]);
         }
@@ -344,9 +352,9 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
         for (int x = X0; x < X1; x++)
 #pragma unroll
           for (int i = 0; i < 16; i++)
-            if (lnS[st][x * 32 + 8 * (i / 4) + 4 * hl + i % 4] == -INFINITY) S[x][i] = -INFINITY;
+            if (lnS[st][part * KW + x * 32 + 8 * (i / 4) + 4 * hl + i % 4] == -INFINITY) S[x][i] = -INFINITY;
     }
-    const int lo = sp.lo - k0 - 4 * hl, hi = sp.hi - k0 - 4 * hl, first = sp.first - k0 - 4 * hl;
+    const int kp = k0 + part * KW + 4 * hl, lo = sp.lo - kp, hi = sp.hi - kp, first = sp.first - kp;
 #pragma unroll
     for (int x = X0; x < X1; x++)
 #pragma unroll
@@ -374,7 +382,7 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
         for (int i = 0; i < 16; i++) O[d][i] *= f;
     }
     const float mu = m == -INFINITY ? 0.f : m;
-    bf16x8_t pf[4];
+    bf16x8_t pf[2 * NX];
     float lt[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int x = X0; x < X1; x++)
@@ -419,17 +427,19 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
       compute(std::integral_constant<int, TILE_LATE>{});
       mode = next();
     }
-    while (mode == TILE_LATE_1) {
-      compute(std::integral_constant<int, TILE_LATE_1>{});
-      mode = next();
-    }
     while (mode == TILE_EARLY) {
       compute(std::integral_constant<int, TILE_EARLY>{});
       mode = next();
     }
-    while (mode == TILE_EARLY_2) {
-      compute(std::integral_constant<int, TILE_EARLY_2>{});
-      mode = next();
+    if constexpr (NX > 1) {
+      while (mode == TILE_LATE_1) {
+        compute(std::integral_constant<int, TILE_LATE_1>{});
+        mode = next();
+      }
+      while (mode == TILE_EARLY_2) {
+        compute(std::integral_constant<int, TILE_EARLY_2>{});
+        mode = next();
+      }
     }
     while (mode == TILE_ALL) {
       compute(std::integral_constant<int, TILE_ALL>{});
@@ -437,9 +447,44 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 ? 3 : 2) void window_attention_m
     }
     while (mode == TILE_SKIP) mode = next();
   }
+  if constexpr (SPLIT) {  // the parts of a row tile joined, by the first of its waves
+    __syncthreads();
+    constexpr int OTHERS = PARTS - 1;
+    float* Os = (float*)smem + lane;
+    float2* ml = (float2*)(smem + WNW / PARTS * OTHERS * ND * 4096) + lane;
+    if (part > 0) {
+      const int to = who * OTHERS + part - 1;
+#pragma unroll
+      for (int d = 0; d < ND; d++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) Os[((to * ND + d) * 16 + i) * 64] = O[d][i];
+      ml[to * 64] = make_float2(m, l);
+    }
+    __syncthreads();
+    if (part > 0) return;
+    float top = m;
+#pragma unroll
+    for (int p = 0; p < OTHERS; p++) top = fmaxf(top, ml[(who * OTHERS + p) * 64].x);
+    const float mu = top == -INFINITY ? 0.f : top, f0 = __builtin_amdgcn_exp2f(m - mu);
+    l *= f0;
+#pragma unroll
+    for (int d = 0; d < ND; d++)
+#pragma unroll
+      for (int i = 0; i < 16; i++) O[d][i] *= f0;
+#pragma unroll
+    for (int p = 0; p < OTHERS; p++) {
+      const int of = who * OTHERS + p;
+      const float f = __builtin_amdgcn_exp2f(ml[of * 64].x - mu);
+      l = fmaf(ml[of * 64].y, f, l);
+#pragma unroll
+      for (int d = 0; d < ND; d++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) O[d][i] = fmaf(Os[((of * ND + d) * 16 + i) * 64], f, O[d][i]);
+    }
+  }
   if (any_bad && w0 + c < n) {  // the values that were cleared, for the rows that see them
     for (int it = 0; it < pl.nt; it++)
-      for (int j = pl.tile(it) * WKT; j < min(n, pl.tile(it) * WKT + WKT); j++) {
+      for (int j = pl.tile(it) * KT; j < min(n, pl.tile(it) * KT + KT); j++) {
         if (!sees(a, w0 + c, j) || (SIZES && !(a.size[pl.base + j] > 0.f))) continue;
         const bf16_t* v = vg + (int64_t)j * a.v_row + 4 * hl;
 #pragma unroll
@@ -788,12 +833,15 @@ hipError_t for_samples(const int32_t* cu_host, int batch, int rows, F launch) {
 
 // Whether the waves of a workgroup share the keys of its row tiles, `parts` waves
 // a tile, instead of having a row tile each: where that many more workgroups
-// still run at once (2 a CU), or where the rows see so many keys that the last
-// workgroups' chains of tiles are what the call takes (fp32, one sample, causal;
-// row tiles each / shared: 1,536 rows, 6 heads of 64, window 964, 144
-// workgroups, 59 us / 31; 512 rows, 16 heads of 128, window 300, 128: 40 / 25;
-// 4,096 rows, 6 heads of 64, no window, 384: 234 / 160; but 2,048 rows, window
-// 200, 192: 21 / 26, and 5,120, window 1,000, 480: 94 / 109).
+// still run at once (2 a CU), or where hardly a window evens the rows out and
+// the last rows' chains of tiles are what the call takes.  One sample, causal
+// (row tiles each / shared, us; in brackets the workgroups without sharing):
+//   fp32: 512 rows, 16 heads of 128, window 300 [128] 40 / 25; 1,536, 6 of 64,
+//     964 [144] 59 / 31; 4,096, 6 of 64, none [384] 234 / 160; but 2,048, 6 of
+//     64, 200 [192] 21 / 26 and 5,120, 1,000 [480] 94 / 109
+//   bf16: 1,024, 16 of 128, none [128] 27 / 21; 4,096, 6 of 64, none [192] 69 /
+//     36; 8,192 [384] 139 / 118; but 16,384 [768] 310 / 420, 4,096, 400 [192]
+//     16.6 / 21, 8,192, 4,096 [384] 81 / 98 and 6 samples of 900 [288] 21 / 23
 bool share_keys(const WindowArgs& a, const int32_t* cu_host, int batch, int rows, int units,
                 int parts) {
   int64_t groups = 0, longest = 0;
@@ -803,7 +851,8 @@ bool share_keys(const WindowArgs& a, const int32_t* cu_host, int batch, int rows
     longest = std::max(longest, n);
   }
   groups *= units;
-  return groups * parts <= 512 || std::min(longest, (int64_t)a.window * (a.causal ? 1 : 2)) >= 4 * groups;
+  return groups * parts <= 512 || (a.causal && longest >= 5 * groups &&
+                                   groups * longest <= 400 * std::min((int64_t)a.window, longest));
 }
 
 template <typename T, int DC, bool PAD>
@@ -811,30 +860,27 @@ hipError_t launch_mfma(const WindowArgs& a, const int32_t* cu_host, int batch, h
   // heads of a group per workgroup, 1 << hshift
   const int hshift = a.group % 4 == 0 ? 2 : a.group % 2 == 0 ? 1 : 0;
   const int rows = (sizeof(T) == 2 ? 32 : 16) * (WNW >> hshift);
-  if constexpr (sizeof(T) == 2) {
+  const auto run = [&](auto split_c, int rows, int hshift) {
+    constexpr bool SPLIT = decltype(split_c)::value;
     return for_samples(cu_host, batch, rows, [&](const WindowSeqs& sq, int tiles) {
       const dim3 grid((unsigned)tiles * (a.H >> hshift));
-      if (a.size)
-        window_attention_mfma<DC, PAD, true><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
-      else
-        window_attention_mfma<DC, PAD, false><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
-    });
-  } else {
-    const auto run = [&](auto split_c, int rows, int hshift) {
-      constexpr bool SPLIT = decltype(split_c)::value;
-      return for_samples(cu_host, batch, rows, [&](const WindowSeqs& sq, int tiles) {
-        const dim3 grid((unsigned)tiles * (a.H >> hshift));
+      if constexpr (sizeof(T) == 2) {
+        if (a.size)
+          window_attention_mfma<DC, PAD, true, SPLIT><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
+        else
+          window_attention_mfma<DC, PAD, false, SPLIT><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
+      } else {
         if (a.size)
           window_attention_mfma_f32<DC, PAD, true, SPLIT><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
         else
           window_attention_mfma_f32<DC, PAD, false, SPLIT><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);
-      });
-    };
-    constexpr int parts = DC <= 64 ? 4 : 2;
-    return share_keys(a, cu_host, batch, rows, a.H >> hshift, parts)
-               ? run(std::true_type{}, 16 * (WNW / parts), 0)
-               : run(std::false_type{}, rows, hshift);
-  }
+      }
+    });
+  };
+  constexpr int parts = DC <= 64 ? 4 : 2;
+  return share_keys(a, cu_host, batch, rows, a.H >> hshift, parts)
+             ? run(std::true_type{}, (rows << hshift) / parts, 0)
+             : run(std::false_type{}, rows, hshift);
 }
 
 }  // namespace
