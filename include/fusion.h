@@ -472,11 +472,15 @@ FUSION_API int fusion_paged_attention(const fusion_cache* c, const void* q, cons
 /* Eviction by accumulated weight: a sequence with more than `budget` tokens
  * keeps those whose position is below sinks or among its last `recent`
  * (sinks + recent <= budget), and of the others the ones with the most weight
- * (ties to the lower slot; NaN below everything), budget in all.  Kept tokens
- * in slots below the budget stay where they are; those beyond move, lowest
- * slot first, into the slots that became free, lowest first, with their
- * weight and position (keys and values only where both slots have a page).
- * len becomes the budget; what slots past it hold is left as it was.  src: device int32 [batch][budget], the slot that each slot's
+ * (ties to the lower slot; NaN below everything), budget in all.  A token in a
+ * slot past the budget that has no page is stored nowhere and leaves before all
+ * others.  Kept tokens in slots below the budget stay where they are; those
+ * beyond move, lowest slot first, into the slots that became free, lowest
+ * first, with their weight and position, and with their keys and values where
+ * that slot has a page (a token that moves into one without is hidden from then
+ * on: slots below the budget should have pages).  len becomes the budget; what
+ * slots past it hold is left as it was.
+ * src: device int32 [batch][budget], the slot that each slot's
  * token was in before the call, -1 past len.  ws as above
  * (fusion_cache_evict_workspace_bytes).  Errors: FUSION_E_INVALID_ARG,
  * FUSION_E_CAPACITY, FUSION_E_HIP. */

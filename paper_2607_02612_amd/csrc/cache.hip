@@ -685,8 +685,9 @@ __global__ __launch_bounds__(1024, 8) void paged_join(CacheArgs c, PagedArgs a, 
 
 // -------------------------------------------------------------- evict --
 // Order of the tokens as unsigned integers: protected tokens above all, then
-// by weight (-0 equals 0), NaN below everything.
-__device__ __forceinline__ uint32_t keep_key(float w, bool safe) {
+// by weight (-0 equals 0), NaN below everything, and tokens that are `lost` too.
+__device__ __forceinline__ uint32_t keep_key(float w, bool safe, bool lost) {
+  if (lost) return 0u;
   if (safe) return 0xFFFFFFFFu;
   if (w != w) return 0u;
   const uint32_t u = __float_as_uint(w + 0.f);
@@ -735,7 +736,10 @@ __device__ __forceinline__ int wave_scan(int v) {
 // three bits of the weight, so that weights of similar size meet in few bins:
 // the counts are LDS atomics, and lanes that hit one address wait for each
 // other.)  Threads hold E slots' keys in registers, NT apart; longer sequences
-// go through them in chunks that are read again in every round.  Then ranks in
+// go through them in chunks that are read again in every round.  A token past
+// the budget whose slot has no page is lost: it was never stored, and moved into
+// a page it would stand for the keys that lie there.  (The budget's own slots
+// are as many as may stay and rank above it, so it never does.)  Then ranks in
 // slot order (ballots, and one sum over the waves' counts) list the free slots
 // below the budget and hand them to the kept ones beyond it.  Bound by the
 // latency of loads, atomics and barriers: 64 sequences of 4,097 slots are read
@@ -763,15 +767,18 @@ __global__ __launch_bounds__(NT) void evict_select(CacheArgs c, EvictArgs a, Evi
   const int chunks = (n + CHUNK - 1) / CHUNK;
   auto load = [&](int ch) {
     float w[E];
-    int p[E];
+    int p[E], page[E];
 #pragma unroll
     for (int e = 0; e < E; e++) {
       const int x = min(ch * CHUNK + e * NT + tid, n - 1);
       w[e] = weight[x];
       p[e] = pos[x];
+      page[e] = 0;
+      if (x >= a.budget) page[e] = page_of(c, b, quot((uint32_t)x, c.page));
     }
 #pragma unroll
-    for (int e = 0; e < E; e++) key[e] = keep_key(w[e], p[e] < a.sinks || p[e] >= newest);
+    for (int e = 0; e < E; e++)
+      key[e] = keep_key(w[e], p[e] < a.sinks || p[e] >= newest, page[e] < 0);
   };
   load(0);
   __shared__ __attribute__((aligned(16))) int bins[4096 + 1024 + 1024];
