@@ -136,7 +136,9 @@ __global__ __launch_bounds__(256) void append_lengths(CacheArgs c, AppendSeqs sq
 // transposed.  The next tile's keys and values are under way from the moment
 // the current ones are in LDS and S, its page numbers one tile earlier.
 // Values of hidden tokens are cleared, so that 0 times infinity or NaN does
-// not arise.
+// not arise.  Of a visible token it does: where a weight underflows, and where
+// the second of the two bf16 numbers that stand for it is 0 or negative; the
+// join mends it.
 //
 // With a window over a cache whose slots are out of order a wave gathers the
 // visible ones of its part first, LIST at a time (16 sequences of up to 4,099
@@ -544,6 +546,10 @@ __global__ __launch_bounds__(256, 2) void paged_attention(CacheArgs c, PagedArgs
 // JOIN_AHEAD at a time, the scores before the statistics that they wait for:
 // one stream alone has hundreds of parts (two of 131,072 tokens took 37 us with
 // one part after the other, 23 with the statistics first).
+//
+// Where parts of a row are not finite its waves look through the visible values:
+// the output of a dimension with infinite or NaN ones is their sum, since weights
+// are positive.
 constexpr int JOIN_HEADS = 128;
 constexpr int JOIN_AHEAD = 4;  // (8 leave registers for one workgroup a CU: 17.5 us instead of 13.2)
 // (maximum, sum) of two parts
@@ -559,6 +565,7 @@ __global__ __launch_bounds__(1024, 8) void paged_join(CacheArgs c, PagedArgs a, 
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   __shared__ __attribute__((aligned(16))) float part[16][256];
   __shared__ float2 s_ml[JOIN_HEADS];
+  __shared__ __attribute__((aligned(16))) char s_odd[16];
   if ((int)blockIdx.x >= weights) {
     const int64_t row = ((int64_t)blockIdx.x - weights) * (16 / wpr) + wave / wpr;
     const bool real = row < (int64_t)c.B * a.H;
@@ -593,22 +600,57 @@ __global__ __launch_bounds__(1024, 8) void paged_join(CacheArgs c, PagedArgs a, 
     }
     part[wave][lane] = o0;
     if (DP > 64) part[wave][64 + lane] = o1;
-    if (lane == 0) s_ml[wave] = make_float2(m, l);
+    const bool odd = __any(!(fabsf(o0) < INFINITY) | !(fabsf(o1) < INFINITY));
+    if (lane == 0) {
+      s_ml[wave] = make_float2(m, l);
+      s_odd[wave] = odd;
+    }
     __syncthreads();
     // the row's first waves join its parts
     const int d = tid % (wpr * 64), w0 = wave / wpr * wpr;
+    float o = 0.f, sum = 0.f;
     if (real && d < c.dh) {
       float top = -INFINITY;
       for (int w = 0; w < wpr; w++) top = fmaxf(top, s_ml[w0 + w].x);
       top = top == -INFINITY ? 0.f : top;
-      float o = 0.f, sum = 0.f;
       for (int w = 0; w < wpr; w++) {
         const float f = __builtin_amdgcn_exp2f(s_ml[w0 + w].x - top);
         sum = fmaf(s_ml[w0 + w].y, f, sum);
         o = fmaf(part[w0 + w][d], f, o);
       }
-      ((T*)a.out)[row * c.dh + d] = St<T>::put(sum == 0.f ? 0.f : o / sum);
+      o = sum == 0.f ? 0.f : o / sum;
     }
+    const uint4 odds = *(const uint4*)s_odd;
+    if (__builtin_amdgcn_readfirstlane(odds.x | odds.y | odds.z | odds.w)) {
+      __syncthreads();
+      float e0 = 0.f, e1 = 0.f;
+      if (real) {
+        const Visible vis = visible(c, a, b);
+        const int d1 = 64 + lane;
+        for (int i = wave % wpr; i < vis.nv; i += wpr * 2)
+#pragma unroll
+          for (int u = 0; u < 2; u++) {
+            const int x = vis.slot(min(i + wpr * u, vis.nv - 1));  // (twice the last one: the same sum)
+            const uint32_t pg = quot((uint32_t)x, c.page);
+            const int page = page_of(c, b, pg);
+            const bool see = (page >= 0) & vis.by_position(c.pos + (int64_t)b * c.cap, x, a.sinks);
+            const int64_t p = see ? page : 0, r = see ? x - (int)(pg * c.page.d) : 0;
+            const T* v = (const T*)c.v + p * c.v_page + r * c.v_row + h / a.group * c.v_head;
+            const float x0 = lane < c.dh ? St<T>::get(v[lane]) : 0.f;
+            const float x1 = d1 < c.dh ? St<T>::get(v[d1]) : 0.f;
+            e0 += see & !(fabsf(x0) < INFINITY) ? x0 : 0.f;
+            e1 += see & !(fabsf(x1) < INFINITY) ? x1 : 0.f;
+          }
+      }
+      part[wave][lane] = e0;
+      part[wave][64 + lane] = e1;
+      __syncthreads();
+      float e = 0.f;
+      if (d < c.dh)
+        for (int w = 0; w < wpr; w++) e += part[w0 + w][d];
+      o = e == 0.f || sum != sum ? o : e;  // (a NaN score makes all of a row NaN)
+    }
+    if (real && d < c.dh) ((T*)a.out)[row * c.dh + d] = St<T>::put(o);
     return;
   }
   const int b = (int)(blockIdx.x / chunks), first = (int)(blockIdx.x % chunks) * 1024;

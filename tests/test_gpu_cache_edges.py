@@ -1,5 +1,5 @@
-"""Token caches at their edges: slots without a page.  Helpers and tolerances are
-those of test_gpu_cache.py."""
+"""Token caches at their edges: slots without a page, values that are infinite or
+NaN and are seen.  Helpers and tolerances are those of test_gpu_cache.py."""
 import numpy as np
 import pytest
 
@@ -63,3 +63,53 @@ def test_cache_evict_drops_tokens_that_are_stored_nowhere(torch_cuda, case):
     q = _normal(torch, rng, dtype, len(lengths), 4, 24)
     out, tol, _, _ = _paged_ref(_np(q), c, None, 0, dtype)
     _close(_np(_kern().paged_attention(q, c)), out, tol)
+
+
+# -------------------------------------------- seen values that are not finite --
+def _with_values(out, tol, special, got):
+    """Rows that see infinities and NaN have their sum (weights are positive),
+    the others the finite answer.  special: sum of those values, 0 where none."""
+    odd = special != 0
+    assert odd.any() and not odd.all()
+    assert np.array_equal(got[odd], special[odd], equal_nan=True)
+    _close(np.where(odd, 0, got), np.where(odd, 0, out), tol)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("hq,hkv,dh", [(2, 2, 64), (8, 2, 72), (4, 1, 128)])
+@pytest.mark.parametrize("evicted", [True, False])
+def test_paged_attention_seen_infinities_and_nan(torch_cuda, dtype, hq, hkv, dh, evicted):
+    """Infinities and NaN among the cached values reach the output of a sequence
+    that sees them and no other, in sequences of one part and of many, and also
+    where their weight is below what fp32 holds."""
+    torch = torch_cuda
+    rng = np.random.default_rng(hq + dh + evicted)
+    c = _cache(torch, rng, dtype, [5000, 1, 77, 0, 300], hkv, dh, 16, 5008, evicted=evicted)
+    c.table[4, 3] = -1
+    for b, x, value in ((0, 3, "inf"), (0, 2500, "inf"), (0, 4990, "-inf"), (1, 0, "inf"), (2, 40, "nan"),
+                        (2, 70, "-inf"), (4, 50, "nan"), (4, 1, "-inf"), (4, 299, "inf")):
+        page = int(c.table[b, x // 16])
+        if page >= 0:
+            c.v[page, x % 16, :, x % 3::7] = float(value)
+    clean = c.v.nan_to_num(0, 0, 0)
+    pos, seen = c.pos.cpu().numpy(), c.seen.cpu().numpy()
+    q1 = _normal(torch, rng, dtype, 5, hq, dh)
+    for scale in (1, 40):
+        q = q1 * scale
+        for window, sinks in ((None, 0), (60, 2), (3000, 0)):
+            z = _kern().TokenCache(c.k, clean, c.table, c.length, c.seen, c.weight.clone(), c.pos)
+            out, tol, add, add_tol = _paged_ref(_np(q), z, window, sinks, dtype)
+            special = np.zeros(out.shape)
+            with np.errstate(invalid="ignore"):
+                for b in range(5):
+                    n = int(c.length[b])
+                    _, v, see = _rows(c, b, n)
+                    if window:
+                        see = see & ((pos[b, :n] > seen[b] - 1 - window) | (pos[b, :n] < sinks))
+                    for x in np.flatnonzero(see & ~np.isfinite(v).all((1, 2))):
+                        special[b] += np.where(np.isfinite(v[x]), 0, v[x]).repeat(hq // hkv, 0)
+            d = _kern().TokenCache(c.k, c.v, c.table, c.length, c.seen, c.weight.clone(), c.pos)
+            _with_values(out, tol, special, _np(_kern().paged_attention(q, d, window, sinks)))
+            # what a token draws does not depend on its values
+            _kern().paged_attention(q, z, window, sinks)
+            assert torch.equal(d.weight, z.weight)
