@@ -67,9 +67,11 @@ struct WindowSeqs {
 //
 // A probability of 0 does not take a value out of P V when that value is
 // infinite or NaN.  A tile that some query of the workgroup sees and another
-// does not is therefore searched for such values; if there are any, they are
-// cleared in LDS and, after the last tile, added to the rows that see them
-// (their weight is positive, so an infinity stays one).
+// does not is therefore searched for such values, and if there are any, they are
+// cleared in LDS.  Rows of a workgroup that cleared values, and rows whose
+// output is not finite, look through the values that they see after the last
+// tile: an output with infinite or NaN ones is their sum (weights are positive,
+// also one that underflowed, whose product with an infinity is NaN).
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
@@ -482,7 +484,16 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 && !SPLIT ? 3 : 2) void window_a
         for (int i = 0; i < 16; i++) O[d][i] = fmaf(Os[((of * ND + d) * 16 + i) * 64], f, O[d][i]);
     }
   }
-  if (any_bad && w0 + c < n) {  // the values that were cleared, for the rows that see them
+  l = sum_xor32(l);
+  // rows that see infinite or NaN values get their sum
+  float zero[4] = {0.f, 0.f, 0.f, 0.f};  // NaN where an output is not finite
+#pragma unroll
+  for (int d = 0; d < ND; d++)
+#pragma unroll
+    for (int i = 0; i < 16; i++) zero[i & 3] = fmaf(O[d][i], 0.f, zero[i & 3]);
+  const bool odd = any_bad | ((zero[0] + zero[1]) + (zero[2] + zero[3]) != 0.f);
+  if (odd && l == l && w0 + c < n) {  // (a NaN score makes all of a row NaN)
+    float sum[ND][16] = {};
     for (int it = 0; it < pl.nt; it++)
       for (int j = pl.tile(it) * KT; j < min(n, pl.tile(it) * KT + KT); j++) {
         if (!sees(a, w0 + c, j) || (SIZES && !(a.size[pl.base + j] > 0.f))) continue;
@@ -496,11 +507,14 @@ __global__ __launch_bounds__(64 * WNW, DC == 64 && !SPLIT ? 3 : 2) void window_a
             const float e[4] = {__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xFFFF0000u),
                                 __uint_as_float(x.y << 16), __uint_as_float(x.y & 0xFFFF0000u)};
 #pragma unroll
-            for (int q = 0; q < 4; q++) O[d][4 * i4 + q] += fabsf(e[q]) < INFINITY ? 0.f : e[q];
+            for (int q = 0; q < 4; q++) sum[d][4 * i4 + q] += fabsf(e[q]) < INFINITY ? 0.f : e[q];
           }
       }
+#pragma unroll
+    for (int d = 0; d < ND; d++)
+#pragma unroll
+      for (int i = 0; i < 16; i++) O[d][i] = sum[d][i] == 0.f ? O[d][i] : sum[d][i];
   }
-  l = sum_xor32(l);
   if (w0 + c < n) {
     const float r = l == 0.f ? 0.f : 1.f / l;
     bf16_t* out = (bf16_t*)a.out + ((int64_t)(pl.base + w0 + c) * a.H + h) * dh + 4 * hl;
@@ -787,7 +801,18 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowA
       for (int d = 0; d < NU; d++) O[d] += Os[((wave + p) * NU + d) * 64] * f;
     }
   }
-  if (any_bad && w0 + c < n) {  // the values that were cleared, for the rows that see them
+  l = sum_xor32(sum_xor16(l));
+  // rows that see infinite or NaN values get their sum
+  f32x4_t zero = {0.f, 0.f, 0.f, 0.f};  // NaN where an output is not finite
+#pragma unroll
+  for (int d = 0; d < NU; d++)
+#pragma unroll
+    for (int q = 0; q < 4; q++) zero[q] = fmaf(O[d][q], 0.f, zero[q]);
+  const bool odd = any_bad | ((zero[0] + zero[1]) + (zero[2] + zero[3]) != 0.f);
+  if (odd && l == l && w0 + c < n) {  // (a NaN score makes all of a row NaN)
+    f32x4_t sum[NU];
+#pragma unroll
+    for (int d = 0; d < NU; d++) sum[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     for (int it = 0; it < pl.nt; it++)
       for (int j = pl.tile(it) * KT; j < min(n, pl.tile(it) * KT + KT); j++) {
         if (!sees(a, w0 + c, j) || (SIZES && !(a.size[pl.base + j] > 0.f))) continue;
@@ -797,11 +822,14 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowA
           if (PAD && 16 * d + 4 * g >= dh) break;
           const f32x4_t x = *(const f32x4_t*)(v + 16 * d);
 #pragma unroll
-          for (int q = 0; q < 4; q++) O[d][q] += fabsf(x[q]) < INFINITY ? 0.f : x[q];
+          for (int q = 0; q < 4; q++) sum[d][q] += fabsf(x[q]) < INFINITY ? 0.f : x[q];
         }
       }
+#pragma unroll
+    for (int d = 0; d < NU; d++)
+#pragma unroll
+      for (int q = 0; q < 4; q++) O[d][q] = sum[d][q] == 0.f ? O[d][q] : sum[d][q];
   }
-  l = sum_xor32(sum_xor16(l));
   if (w0 + c < n) {
     const float r = l == 0.f ? 0.f : 1.f / l;
     float* out = (float*)a.out + ((int64_t)(pl.base + w0 + c) * a.H + h) * dh + 4 * g;

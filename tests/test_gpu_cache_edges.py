@@ -1,10 +1,11 @@
-"""Token caches at their edges: slots without a page, values that are infinite or
-NaN and are seen.  Helpers and tolerances are those of test_gpu_cache.py."""
+"""Windowed attention and token caches at their edges: slots without a page, values
+that are infinite or NaN and are seen.  Helpers and tolerances are those of
+test_gpu_cache.py."""
 import numpy as np
 import pytest
 
 from test_gpu_cache import (_cache, _close, _kern, _normal, _np, _paged_ref, _rows,  # noqa: F401
-                            torch_cuda)
+                            _window_ref, torch_cuda)
 
 pytestmark = pytest.mark.gpu
 
@@ -73,6 +74,67 @@ def _with_values(out, tol, special, got):
     assert odd.any() and not odd.all()
     assert np.array_equal(got[odd], special[odd], equal_nan=True)
     _close(np.where(odd, 0, got), np.where(odd, 0, out), tol)
+
+
+def _shares_keys(dtype, lengths, hq, hkv, dh, window, causal):
+    """Which of the two kernels a call takes (share_keys in window.hip)."""
+    group = hq // hkv
+    hshift = 2 if group % 4 == 0 else 1 if group % 2 == 0 else 0
+    rows, parts = (32 if dtype == "bf16" else 16) * (4 >> hshift), 4 if dh <= 64 else 2
+    groups, longest = sum(-(-n // rows) for n in lengths) * (hq >> hshift), max(lengths)
+    return groups * parts <= 512 or (causal and longest >= 5 * groups and
+                                     groups * longest <= 400 * min(window or 1 << 30, longest))
+
+
+def _copies(shared, dtype, lengths, hq, hkv, dh, window, causal):
+    """How often to repeat the samples so that the call's waves share the keys
+    of a row tile, or do not."""
+    for n in range(1, 400):
+        if _shares_keys(dtype, lengths * n, hq, hkv, dh, window, causal) == shared:
+            return n
+    raise AssertionError("no such call")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("hq,hkv,dh", [(2, 2, 64), (8, 2, 72), (4, 2, 128)])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("shared", [True, False])
+def test_window_attention_seen_infinities_and_nan(torch_cuda, dtype, hq, hkv, dh, causal, shared):
+    """Infinities and NaN reach every row that sees them and no other, whether
+    all rows of a tile see them or some, and also where the weight is below
+    what fp32 holds."""
+    torch = torch_cuda
+    rng = np.random.default_rng(hq + dh + causal)
+    lengths = [200, 0, 130]
+    cu1 = np.array([0, 200, 200, 330])
+    q, k, v = (_normal(torch, rng, dtype, 330, h, dh) for h in (hq, hkv, hkv))
+    size = torch.ones(330, device="cuda")
+    size[250] = 0
+    for row, value in ((1, "inf"), (5, "-inf"), (77, "inf"), (130, "nan"), (250, "nan"), (328, "-inf")):
+        v[row, :, row % 3::7] = float(value)
+    vn = _np(v)
+    i = np.arange(330)
+    for scale in (1, 12):  # 12: scores of hundreds, most weights underflow
+        for window, sinks in ((20, 3), (100, 0), (None, 0)):
+            see = np.abs(i[:, None] - i) < (window or 1000)
+            see |= (i < sinks) | ((i >= 200) & (i < 200 + sinks))
+            if causal:
+                see &= i <= i[:, None]
+            see &= ((i >= 200)[:, None] == (i >= 200)) & (i != 250)
+            special = np.zeros((330, hq, dh))
+            with np.errstate(invalid="ignore"):
+                for row in np.flatnonzero(~np.isfinite(vn).all((1, 2))):
+                    special[see[:, row]] += np.where(np.isfinite(vn[row]), 0, vn[row]).repeat(hq // hkv, 0)
+            vz = np.where(np.isfinite(vn), vn, 0)
+            n = _copies(shared, dtype, lengths, hq, hkv, dh, window, causal)
+            out, tol = _window_ref(_np(q * scale), _np(k * scale), vz, cu1, window, sinks, causal,
+                                   _np(size), dtype)
+            cu = np.concatenate([[0], np.cumsum(lengths * n)])
+            got = _kern().window_attention((q * scale).repeat(n, 1, 1), (k * scale).repeat(n, 1, 1),
+                                           v.repeat(n, 1, 1), cu, window, sinks, causal, size.repeat(n))
+            got = _np(got).reshape(n, 330, hq, dh)
+            assert np.array_equal(got, np.broadcast_to(got[:1], got.shape), equal_nan=True)
+            _with_values(out, tol, special, got[0])
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
