@@ -98,7 +98,7 @@ def attention(qkv, size, cu, heads, prop_attn=True, cls_tmax=None):
     out = torch.empty(M, d, dtype=qkv.dtype, device=qkv.device)
     cls = None
     if cls_tmax is not None:
-        cls = torch.empty((B, heads, cls_tmax), device=qkv.device)
+        cls = torch.empty((B, heads, cls_tmax), dtype=torch.float32, device=qkv.device)
     ws, n = _workspace(B, M, qkv.device)
     check(_native.lib().fusion_test_attention_ws(prec, qkv.data_ptr(), size.data_ptr(), cu_p, B,
                                                  heads, d, int(bool(prop_attn)), out.data_ptr(),
@@ -174,7 +174,7 @@ def topk_compact(x, size, origin, cu, keep_ratio, scores=None, heads=1, prune_w=
     if exit_logits is not None:
         _need(exit_logits, "exit_logits", torch.float32)
         C = exit_logits.shape[1]
-        logits = torch.empty((B, C), device=dev)
+        logits = torch.empty((B, C), dtype=torch.float32, device=dev)
         exit_block = torch.empty((B,), dtype=torch.int32, device=dev)
     ln_out = None
     ln_g = ln_b = None
@@ -400,7 +400,8 @@ class TokenCache:
         i32 = [torch.zeros(shape, dtype=torch.int32, device=dev)
                for shape in ((batch,), (batch,), (batch, n * page_size))]
         return cls(*kv, torch.arange(batch * n, dtype=torch.int32, device=dev).view(batch, n),
-                   i32[0], i32[1], torch.zeros((batch, n * page_size), device=dev), i32[2])
+                   i32[0], i32[1],
+                   torch.zeros((batch, n * page_size), dtype=torch.float32, device=dev), i32[2])
 
     k, v, table, length, seen, weight, pos = (
         property(lambda self, i=i: self._tensors[i]) for i in range(7))

@@ -99,7 +99,7 @@ class FusionModel:
 
     def alloc_outputs(self, batch: int):
         dev = self.device
-        logits = torch.empty(batch, self.info["classes"], device=dev)
+        logits = torch.empty(batch, self.info["classes"], dtype=torch.float32, device=dev)
         exit_block = torch.empty(batch, dtype=torch.int32, device=dev)
         counts = torch.empty(batch, self.info["layers"], dtype=torch.int32, device=dev)
         return logits, exit_block, counts
@@ -108,8 +108,8 @@ class FusionModel:
         L, T0 = self.info["layers"], self.info["n0"] + 1
         dev = self.device
         return dict(r=torch.full((L, batch), -1, dtype=torch.int32, device=dev),
-                    m=torch.full((L, batch), -1.0, device=dev),
-                    c=torch.full((L, batch), -1.0, device=dev),
+                    m=torch.full((L, batch), -1.0, dtype=torch.float32, device=dev),
+                    c=torch.full((L, batch), -1.0, dtype=torch.float32, device=dev),
                     merge_dst=torch.full((L, batch, T0), -1, dtype=torch.int32, device=dev),
                     ids=torch.full((L, batch, T0), -1, dtype=torch.int32, device=dev))
 
@@ -136,7 +136,7 @@ class FusionModel:
         """Packed hidden states after (block, stage); see fusion_debug_state."""
         B = check_run_args(self.info, self.device, images)
         d, T0 = self.info["d"], self.info["n0"] + 1
-        x = torch.zeros(B * T0, d, device="cuda")
+        x = torch.zeros(B * T0, d, dtype=torch.float32, device="cuda")
         cu = torch.zeros(B + 1, dtype=torch.int32, device="cuda")
         live = torch.zeros(B, dtype=torch.int32, device="cuda")
         n = c_int(0)
