@@ -20,6 +20,7 @@ from ctypes import byref, c_double, c_float
 
 import numpy as np
 import torch
+from torch.autograd import forward_ad
 
 from . import _native
 from ._native import FusionCache, FusionPackedOut, FusionRagged, check
@@ -217,6 +218,8 @@ def _current(dev, *used):
 def _no_grad(t, name):
     if t.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{name} requires a gradient, and none is computed: detach it")
+    if forward_ad._current_level >= 0 and forward_ad.unpack_dual(t).tangent is not None:
+        raise ValueError(f"{name} carries a tangent, and none is computed: pass its primal")
 
 
 def _heads(t, name, dtype, heads, dh):
@@ -376,6 +379,8 @@ class TokenCache:
         self._tensors = (k, v, table, length, seen, weight, pos)
         if any(t.requires_grad for t in self._tensors):
             raise ValueError("the cache's tensors are written in place and have no gradients")
+        for t, name in zip(self._tensors, ("k", "v", "table", "length", "seen", "weight", "pos")):
+            _no_grad(t, name)
         if any(t.device != k.device for t in self._tensors):
             raise ValueError("the cache's tensors must be on one GPU")
         self._c = FusionCache(k.data_ptr(), v.data_ptr(), k.stride()[:3], v.stride()[:3],

@@ -138,3 +138,25 @@ def test_binding_refuses_host_tensors_and_shapes():
     with pytest.raises(ValueError):  # host tensors
         kernels.TokenCache(t(8, 16, 2, 64), t(8, 16, 2, 64), i32(2, 4), i32(2), i32(2),
                            torch.zeros(2, 64), i32(2, 64))
+
+
+def test_binding_refuses_tangents():
+    """A dual tensor's tangent would be dropped in silence."""
+    from torch.autograd import forward_ad
+    t = torch.zeros(4, 2, 64, dtype=torch.bfloat16)
+    fake = type("Cache", (), dict(dtype=torch.bfloat16, batch=4, kv_heads=2, dh=64))()
+    with forward_ad.dual_level():
+        dual = forward_ad.make_dual(t, torch.ones_like(t))
+        size = forward_ad.make_dual(torch.ones(4), torch.ones(4))
+        for call in [lambda: kernels.window_attention(dual, t, t, [0, 4]),
+                     lambda: kernels.window_attention(t, dual, t, [0, 4]),
+                     lambda: kernels.window_attention(t, t, dual, [0, 4]),
+                     lambda: kernels.cache_append(fake, dual, t),
+                     lambda: kernels.cache_append(fake, t, dual),
+                     lambda: kernels.paged_attention(dual, fake)]:
+            with pytest.raises(ValueError, match="tangent"):
+                call()
+        with pytest.raises(ValueError, match="tangent"):
+            kernels._no_grad(size, "size")
+        kernels._no_grad(t, "q")  # without a tangent it passes
+    kernels._no_grad(t, "q")
