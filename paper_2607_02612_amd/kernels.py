@@ -489,8 +489,10 @@ def cache_evict(cache, budget, sinks=0, recent=0):
     last `recent` positions stay, and the others by accumulated weight.
     Returns src int32 [batch, budget]: the slot from which each slot's token
     came, -1 past the sequence's length."""
-    budget, sinks = _count(budget, "budget", 1), _count(sinks, "sinks")
-    recent = _count(recent, "recent")
+    budget, sinks = _count(budget, "budget", 1, _LAST), _count(sinks, "sinks", 0, _LAST)
+    recent = _count(recent, "recent", 0, _LAST)
+    if budget > 1 << 30:
+        raise ValueError("budget must be at most 2^30")
     if sinks + recent > budget:
         raise ValueError("sinks and recent do not fit the budget")
     stream = cache._ready()

@@ -160,3 +160,13 @@ def test_binding_refuses_tangents():
             kernels._no_grad(size, "size")
         kernels._no_grad(t, "q")  # without a tangent it passes
     kernels._no_grad(t, "q")
+
+
+@pytest.mark.parametrize("budget,sinks,recent", [
+    ((1 << 30) + 1, 0, 0), (1 << 31, 0, 0), (1 << 40, 4, 64), (1 << 30, 0, (1 << 30) + 1),
+    (1 << 30, 1 << 31, 0), (1 << 30, 1 << 29, (1 << 29) + 1), (0, 0, 0), (8, 4, 5), (8.5, 0, 0)])
+def test_binding_refuses_budgets(budget, sinks, recent):
+    """A budget beyond the library's range is refused, not cut (the result
+    would have another shape), nor are the counts that have to fit it."""
+    with pytest.raises(ValueError):
+        kernels.cache_evict(None, budget, sinks, recent)
