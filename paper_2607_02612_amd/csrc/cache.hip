@@ -50,6 +50,7 @@ struct OneRowEach {};
 // workgroup takes a sample's rows and moves its lengths on; else the lengths
 // move in a launch of their own, after all rows have read them.
 constexpr int APPEND_FEW = 8;  // rows of a sample up to which one workgroup takes them
+constexpr int APPEND_BLOCKS = 1 << 22;  // workgroups of a launch (2^32 threads are too many for one)
 
 template <typename T>
 __device__ __forceinline__ void append_row(const CacheArgs& c, const AppendArgs& a, int b, int r,
@@ -98,15 +99,16 @@ __global__ __launch_bounds__(256) void append_few(CacheArgs c, AppendArgs a, Seq
 
 template <typename T>
 __global__ __launch_bounds__(256) void append_many(CacheArgs c, AppendArgs a, AppendSeqs sq) {
-  const int r = sq.cu[0] + blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (r >= sq.cu[sq.n]) return;
-  int lo = 0, hi = sq.n - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (sq.cu[mid] <= r) lo = mid; else hi = mid - 1;
+  const int end = sq.cu[sq.n];
+  for (int r = sq.cu[0] + blockIdx.x * 4 + (threadIdx.x >> 6); r < end; r += gridDim.x * 4) {
+    int lo = 0, hi = sq.n - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (sq.cu[mid] <= r) lo = mid; else hi = mid - 1;
+    }
+    const int b = sq.first + lo, nth = r - sq.cu[lo];
+    append_row<T>(c, a, b, r, (int64_t)held(c, b) + nth, c.seen[b] + nth, threadIdx.x & 63, 64);
   }
-  const int b = sq.first + lo, nth = r - sq.cu[lo];
-  append_row<T>(c, a, b, r, (int64_t)held(c, b) + nth, c.seen[b] + nth, threadIdx.x & 63, 64);
 }
 
 __global__ __launch_bounds__(256) void append_lengths(CacheArgs c, AppendSeqs sq) {
@@ -169,6 +171,7 @@ struct PagedSpace {
   float* score;  // [B][units][tiles][heads][KT], base 2, by visible token
   int ranges;    // parts per unit
   int units, qtiles, tiles, heads;  // (heads of a unit, at most 16)
+  int block0;    // number of the launch's first workgroup
 };
 
 // The visible tokens of a sequence: x-th visible token -> slot.  In a cache
@@ -218,7 +221,7 @@ __global__ __launch_bounds__(256, 2) void paged_attention(CacheArgs c, PagedArgs
   __shared__ __attribute__((aligned(16))) char s_all[4 * SPARE];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int g = lane >> 4, cl = lane & 15;
-  const int id = blockIdx.x * 4 + wave, unit = id % ws.units, range = id / ws.units;
+  const int id = (blockIdx.x + ws.block0) * 4 + wave, unit = id % ws.units, range = id / ws.units;
   if (range >= ws.ranges) return;
   char* Vs = v_all + wave * KT * VROW;
   char* Ss = s_all + wave * SPARE;
@@ -566,8 +569,9 @@ __global__ __launch_bounds__(1024, 8) void paged_join(CacheArgs c, PagedArgs a, 
   __shared__ __attribute__((aligned(16))) float part[16][256];
   __shared__ float2 s_ml[JOIN_HEADS];
   __shared__ __attribute__((aligned(16))) char s_odd[16];
-  if ((int)blockIdx.x >= weights) {
-    const int64_t row = ((int64_t)blockIdx.x - weights) * (16 / wpr) + wave / wpr;
+  const int block = blockIdx.x + ws.block0;
+  if (block >= weights) {
+    const int64_t row = ((int64_t)block - weights) * (16 / wpr) + wave / wpr;
     const bool real = row < (int64_t)c.B * a.H;
     const int b = real ? (int)(row / a.H) : 0, h = real ? (int)(row % a.H) : 0;
     const int2 plan = ws.plan[b];
@@ -653,7 +657,7 @@ __global__ __launch_bounds__(1024, 8) void paged_join(CacheArgs c, PagedArgs a, 
     if (real && d < c.dh) ((T*)a.out)[row * c.dh + d] = St<T>::put(o);
     return;
   }
-  const int b = (int)(blockIdx.x / chunks), first = (int)(blockIdx.x % chunks) * 1024;
+  const int b = block / chunks, first = block % chunks * 1024;
   const Visible vis = visible(c, a, b);
   if (first >= vis.nv) return;
   const int2 plan = ws.plan[b];
@@ -978,7 +982,7 @@ hipError_t launch_cache_append(const CacheArgs& c, const AppendArgs& a, const in
     if (most <= APPEND_FEW) {
       append_few<T><<<sq.n, 256, 0, s>>>(c, a, sq);
     } else {
-      append_many<T><<<(rows + 3) / 4, 256, 0, s>>>(c, a, sq);
+      append_many<T><<<std::min((rows + 3) / 4, APPEND_BLOCKS), 256, 0, s>>>(c, a, sq);
       append_lengths<<<(sq.n + 255) / 256, 256, 0, s>>>(c, sq);
     }
     if (hipError_t e = hipGetLastError()) return e;
@@ -1020,12 +1024,15 @@ size_t paged_space(const CacheArgs& c, int KT, int H, int accumulate, char* ws,
 template <typename T, int DP, bool PAD>
 hipError_t launch_paged(const CacheArgs& c, const PagedArgs& a, const PagedSpace& ws,
                         hipStream_t s) {
-  const unsigned grid = (unsigned)(((int64_t)ws.units * ws.ranges + 3) / 4);
-  if (a.accumulate)
-    paged_attention<T, DP, PAD, true><<<grid, 256, 0, s>>>(c, a, ws);
-  else
-    paged_attention<T, DP, PAD, false><<<grid, 256, 0, s>>>(c, a, ws);
-  if (hipError_t e = hipGetLastError()) return e;
+  PagedSpace w = ws;
+  if (hipError_t e = in_launches(((int64_t)ws.units * ws.ranges + 3) / 4, 256, [&](int first, unsigned grid) {
+        w.block0 = first;
+        if (a.accumulate)
+          paged_attention<T, DP, PAD, true><<<grid, 256, 0, s>>>(c, a, w);
+        else
+          paged_attention<T, DP, PAD, false><<<grid, 256, 0, s>>>(c, a, w);
+      }))
+    return e;
   // (workgroups past a sequence's tokens leave at once)
   const int chunks = a.accumulate ? std::max(1, std::min((c.cap + 1023) / 1024, 16384 / c.B)) : 1;
   const int weights = a.accumulate ? c.B * chunks : 0;
@@ -1034,8 +1041,10 @@ hipError_t launch_paged(const CacheArgs& c, const PagedArgs& a, const PagedSpace
   const int parts = c.B <= PAGED_SPLIT ? ws.ranges / c.B + 1 : 1;
   const int wpr = parts <= 2 * JOIN_AHEAD ? 2 : parts <= 4 * JOIN_AHEAD ? 4 : 16;
   const int64_t rows = ((int64_t)c.B * a.H * wpr + 15) / 16;
-  paged_join<T, DP><<<(unsigned)(weights + rows), 1024, 0, s>>>(c, a, ws, weights, chunks, wpr);
-  return hipGetLastError();
+  return in_launches(weights + rows, 1024, [&](int first, unsigned grid) {
+    w.block0 = first;
+    paged_join<T, DP><<<grid, 1024, 0, s>>>(c, a, w, weights, chunks, wpr);
+  });
 }
 constexpr int tile_tokens(size_t size) { return size == 2 ? 32 : 16; }
 }  // namespace

@@ -199,6 +199,18 @@ template <typename T>
 hipError_t launch_window_attention(const WindowArgs& a, const int32_t* cu_host, int batch,
                                    hipStream_t s);
 
+// `blocks` workgroups of `threads` threads in launches of up to 2^30 threads
+// each (a launch holds less than 2^32): runs launch(first, count) for each.
+template <typename F>
+hipError_t in_launches(int64_t blocks, int threads, F launch) {
+  const int64_t most = (1 << 30) / threads;
+  for (int64_t first = 0; first < blocks; first += most) {
+    launch((int)first, (unsigned)(blocks - first < most ? blocks - first : most));
+    if (hipError_t e = hipGetLastError()) return e;
+  }
+  return hipSuccess;
+}
+
 // Quotient by a divisor fixed on the host: n / d for 0 <= n < 2^31 as
 // (mulhi(n, mul) + n) >> shift with mul = floor(2^32 (2^shift - d) / d) + 1,
 // shift = ceil(log2 d) (Granlund and Montgomery's division by invariants).

@@ -839,10 +839,12 @@ __global__ __launch_bounds__(64 * WNW, 2) void window_attention_mfma_f32(WindowA
   }
 }
 
-// Runs `launch(samples, tiles)` for all samples, as many at once as the
-// arguments of a launch hold, with tiles of `rows` rows.
+// Runs `launch(samples, tiles, grid)` for all samples, as many at once as the
+// arguments of a launch hold, with tiles of `rows` rows and `units` workgroups a
+// tile, from the last tile back (workgroup 0 has tile tiles - 1).
 template <typename F>
-hipError_t for_samples(const int32_t* cu_host, int batch, int rows, F launch) {
+hipError_t for_samples(const int32_t* cu_host, int batch, int rows, int units, F launch) {
+  constexpr int MOST = (1 << 30) / (64 * WNW);  // workgroups a launch; it holds less than 2^32 threads
   for (int f = 0; f < batch; f += WIN_SEQS) {
     WindowSeqs sq;
     sq.n = std::min(batch - f, WIN_SEQS);
@@ -852,9 +854,11 @@ hipError_t for_samples(const int32_t* cu_host, int batch, int rows, F launch) {
       sq.tile[i] = tiles;
       if (i < sq.n) tiles += (cu_host[f + i + 1] - cu_host[f + i] + rows - 1) / rows;
     }
-    if (tiles == 0) continue;
-    launch(sq, tiles);
-    if (hipError_t e = hipGetLastError()) return e;
+    for (int m; tiles > 0; tiles -= m) {
+      m = std::min(tiles, MOST / units);
+      launch(sq, tiles, (unsigned)(m * units));
+      if (hipError_t e = hipGetLastError()) return e;
+    }
   }
   return hipSuccess;
 }
@@ -890,8 +894,8 @@ hipError_t launch_mfma(const WindowArgs& a, const int32_t* cu_host, int batch, h
   const int rows = (sizeof(T) == 2 ? 32 : 16) * (WNW >> hshift);
   const auto run = [&](auto split_c, int rows, int hshift) {
     constexpr bool SPLIT = decltype(split_c)::value;
-    return for_samples(cu_host, batch, rows, [&](const WindowSeqs& sq, int tiles) {
-      const dim3 grid((unsigned)tiles * (a.H >> hshift));
+    const int units = a.H >> hshift;
+    return for_samples(cu_host, batch, rows, units, [&](const WindowSeqs& sq, int tiles, unsigned grid) {
       if constexpr (sizeof(T) == 2) {
         if (a.size)
           window_attention_mfma<DC, PAD, true, SPLIT><<<grid, 64 * WNW, 0, s>>>(a, sq, tiles, hshift);

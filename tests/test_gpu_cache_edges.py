@@ -175,3 +175,57 @@ def test_paged_attention_seen_infinities_and_nan(torch_cuda, dtype, hq, hkv, dh,
             # what a token draws does not depend on its values
             _kern().paged_attention(q, z, window, sinks)
             assert torch.equal(d.weight, z.weight)
+
+
+# ------------------------------------------------ more work than one launch holds --
+def test_window_attention_of_more_workgroups_than_a_launch(torch_cuda):
+    """140,000 rows of 4,096 narrow heads: each head equals the same head in a
+    call of few heads."""
+    torch = torch_cuda
+    torch.manual_seed(1)
+    rows, heads, dh = 140_000, 4096, 8
+    print(f"[window] {rows} rows, {heads} heads of {dh}", flush=True)
+    q = torch.randn(rows, heads, dh, dtype=torch.bfloat16, device="cuda")
+    k, v = (torch.randn(rows, 1, dh, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    cu = [0, 1, 70_001, rows]
+    got = _kern().window_attention(q, k, v, cu, 3, 1)
+    for h in range(0, heads, 1020):
+        assert torch.equal(got[:, h:h + 16], _kern().window_attention(q[:, h:h + 16], k, v, cu, 3, 1)), h
+
+
+def test_cache_append_of_more_rows_than_a_launch(torch_cuda):
+    """2^26 rows and a few more, a wave each."""
+    torch = torch_cuda
+    torch.manual_seed(2)
+    n = [(1 << 26) - 9, 40]
+    print(f"[append] {n}", flush=True)
+    c = _kern().TokenCache.empty(2, 1 << 26, 1, 8, page_size=1024)
+    k, v = (torch.randn(sum(n), 1, 8, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    _kern().cache_append(c, k, v, [0, n[0], sum(n)])
+    assert c.length.tolist() == n and c.seen.tolist() == n
+    for b, first in enumerate((0, n[0])):
+        for have, new in ((c.k, k), (c.v, v)):
+            assert torch.equal(have.view(2, -1, 1, 8)[b, :n[b]], new[first:first + n[b]])
+        assert torch.equal(c.pos[b, :n[b]], torch.arange(n[b], dtype=torch.int32, device="cuda"))
+
+
+def test_paged_attention_of_more_workgroups_than_a_launch(torch_cuda):
+    """65,536 sequences with 512 heads of their own: each sequence equals the
+    same one in a call of few."""
+    torch = torch_cuda
+    torch.manual_seed(3)
+    B, heads, dh = 65_536, 512, 8
+    print(f"[paged] {B} sequences, {heads} heads of {dh}", flush=True)
+    k, v = (torch.randn(4, 16, heads, dh, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    q = torch.randn(B, heads, dh, dtype=torch.bfloat16, device="cuda")
+    table = torch.arange(B, dtype=torch.int32, device="cuda").view(B, 1) % 4
+    length = torch.randint(0, 17, (B,), dtype=torch.int32, device="cuda")
+    weight, pos = torch.zeros(B, 16, device="cuda"), torch.arange(16, dtype=torch.int32, device="cuda").repeat(B, 1)
+    whole = _kern().TokenCache(k, v, table, length, length.clone(), weight, pos)
+    got = _kern().paged_attention(q, whole)
+    for b in range(0, B, 13_000):
+        s = slice(b, b + 1500)
+        w = torch.zeros(len(q[s]), 16, device="cuda")
+        part = _kern().TokenCache(k, v, table[s], length[s], length[s].clone(), w, pos[s])
+        assert torch.equal(got[s], _kern().paged_attention(q[s], part)), b
+        assert torch.equal(weight[s], w), b
