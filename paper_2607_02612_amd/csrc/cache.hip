@@ -316,8 +316,8 @@ __global__ __launch_bounds__(256, 2) void paged_attention(CacheArgs c, PagedArgs
     // do, so they come together and seldom (64 sequences of 4,096 tokens, 4
     // heads a unit, 33 MB written beside 1.07 GB read: 230 us with 12 KB held back,
     // 239 with 2 KB, 209 without any scores written).
-    const int row_shift = 32 - __builtin_clz(2 * nq - 1);  // rows of a tile in LDS: 1 << row_shift >= nq
-    const int tile_shift = row_shift - 1 + (BF ? 7 : 6);   // bytes of a tile
+    // (a tile's rows in LDS: the next power of two from nq on)
+    const int tile_shift = 31 - __builtin_clz(2 * nq - 1) + (BF ? 7 : 6);  // bytes of a tile
     const int slots = SCORE_BYTES >> tile_shift;
     int held_from = ta;
     auto store_scores = [&](int t) {  // tiles held_from .. t
@@ -867,10 +867,7 @@ __global__ __launch_bounds__(NT) void evict_select(CacheArgs c, EvictArgs a, Evi
     want = s_found[round][1];
     if (want == 0) break;  // the whole bin stays
   }
-  if (want == 0) {
-    if (least) least--;  // (keys above it: the bin and those over it)
-    else want = INT32_MAX;
-  }
+  if (want == 0) least--;  // (the whole bin stays; not the lowest, since n > budget)
   // exclusive sums, in slot order, of the chunk's counts by e and wave
   auto sum_counts = [&]() {
     __syncthreads();
@@ -893,7 +890,7 @@ __global__ __launch_bounds__(NT) void evict_select(CacheArgs c, EvictArgs a, Evi
     const int x0 = ch * CHUNK + tid;
     uint32_t keep = 0;  // one bit per e
     static_assert(E <= 32 && CHUNK < 32768, "bits of a thread, two counts in a word");
-    if (want > 0 && want < INT32_MAX) {
+    if (want > 0) {
       __syncthreads();
 #pragma unroll
       for (int e = 0; e < E; e++) {
@@ -910,7 +907,6 @@ __global__ __launch_bounds__(NT) void evict_select(CacheArgs c, EvictArgs a, Evi
       }
       ties += s_count[E * NW];
     }
-    if (want == INT32_MAX) keep = ~0u;
 #pragma unroll
     for (int e = 0; e < E; e++) keep |= (uint32_t)(key[e] > least) << e;
     __syncthreads();
