@@ -401,8 +401,15 @@ FUSION_API int fusion_test_topk_compact_ws(const fusion_ragged* in, const float*
  * (window 0: no limit; sinks: first rows that stay visible, such as CLS).
  * size: device fp32 [M] or NULL; scores += ln(size of the key row), as in
  * fusion_test_attention; a size that is not above 0 hides the row from all.
+ * The first `sinks` rows are seen by all; they themselves see no more than their
+ * window (and each other), also without `causal`.
  * A row that sees nothing gets zeros; a value of a row that a query does not
- * see has no influence on its output, whatever it is.
+ * see has no influence on its output, whatever it is.  An output with infinite or
+ * NaN values among the visible ones is their sum.
+ * Sums are fp32 and weights in them up to 2^8, so finite values whose sum over
+ * the visible rows times 2^8 passes fp32's range overflow.  Equal calls give
+ * equal bits; the same sample in a call of other samples may be summed in
+ * another order.
  * q: device [M][heads][dh], k, v: device [M][kv_heads][dh]; strides: HOST
  * int64 [6], row and head strides of q, k and v (row strides of k and v at
  * most 2^23); out: device
@@ -444,8 +451,9 @@ typedef struct fusion_cache {
 
 /* Append rows of keys and values: sequence i gets rows cu[i] .. cu[i+1]-1 of
  * k and v (cu: HOST int32 [batch + 1] as above; NULL: one row each), in its
- * slots from len on, with positions from seen on and weight 0; len and seen
- * grow.  Rows past the capacity are dropped and not counted.
+ * slots from len on, with positions from seen on and weight 0 (also the rows of
+ * a prompt: what they drew from each other is not counted); len and seen grow.
+ * Rows past the capacity are dropped and not counted.
  * k, v: device [rows][kv_heads][dh]; strides: HOST int64 [4], row and head
  * strides of k and v.  Errors: FUSION_E_INVALID_ARG, FUSION_E_HIP. */
 FUSION_API int fusion_cache_append(const fusion_cache* c, const void* k, const void* v,
@@ -456,8 +464,11 @@ FUSION_API int fusion_cache_append(const fusion_cache* c, const void* k, const v
  * seen - 1 - window or below sinks (window 0: all).  The work of all
  * sequences is split evenly over the chip and the parts are joined.  With
  * accumulate = 1 every slot's weight grows by the mean over the heads of its
- * attention probability (the token score of Eq. 8).  A sequence with nothing
- * visible gets zeros.
+ * attention probability (the token score of Eq. 8); the workspace then holds 4
+ * bytes per query head and slot of the capacity, however many are in use.  A
+ * sequence with nothing visible gets zeros; infinite and NaN values that are
+ * visible as above.  Equal calls give equal bits; how the lengths of the other
+ * sequences cut a sequence into parts decides the order of its sums.
  * q: device [batch][heads][dh], strides: HOST int64 [2]; out: device
  * [batch][heads][dh], contiguous.  ws: device buffer of ws_bytes >=
  * fusion_paged_attention_workspace_bytes, 256-byte aligned, any contents, not
@@ -480,8 +491,8 @@ FUSION_API int fusion_paged_attention(const fusion_cache* c, const void* q, cons
  * that slot has a page (a token that moves into one without is hidden from then
  * on: slots below the budget should have pages).  len becomes the budget; what
  * slots past it hold is left as it was.
- * src: device int32 [batch][budget], the slot that each slot's
- * token was in before the call, -1 past len.  ws as above
+ * src: device int32 [batch][budget], the slot that each slot's token was in
+ * before the call, -1 past len.  ws as above
  * (fusion_cache_evict_workspace_bytes).  Errors: FUSION_E_INVALID_ARG,
  * FUSION_E_CAPACITY, FUSION_E_HIP. */
 FUSION_API size_t fusion_cache_evict_workspace_bytes(const fusion_cache* c, int budget);

@@ -36,13 +36,16 @@ struct WindowSeqs {
 // and sum are reductions over registers and one lane swap, and the registers
 // i = 8t .. 8t + 7, rounded to bf16, are the operand of the t-th step of
 // O^T = V^T P^T as they stand.  (The matrix instruction takes no wider type
-// beside bf16 values; P as the sum of two bf16 numbers would cost half again
-// the matrix work, which is what bounds long windows.  The sum of a row takes
-// the unrounded numbers.)  V^T comes from the row-major tile by the
+// beside bf16 values.  P as the sum of two bf16 numbers, half again the matrix
+// work, brings the output's error against 64 bits from 0.0020 .. 0.0023 to the
+// 0.0016 of its own rounding and costs 11 % of the images below, 23 % of the
+// prompts and 32 % of the document, one sample of 197 rows nothing; the path's
+// own attention rounds P too, so all calls do.  The sum of a row takes the
+// unrounded numbers.)  V^T comes from the row-major tile by the
 // transposing LDS read, with the same key order.  The running maximum moves
 // only when a row's maximum grows by more than 8 in the base-2 exponent (P
 // stays below 2^8, whose relative precision is that of 1), per row, so that
-// no row's result depends on another's; rows whose maximum stays multiply by 1.
+// no other row's values enter a row's result; rows whose maximum stays multiply by 1.
 //
 // LDS rows are 2 DP bytes.  K's 16-byte pieces are XOR-permuted by the row mod
 // 16 (64-wide: row / 2 mod 8), V's pairs of 32-byte segments by the row mod 4
@@ -54,16 +57,18 @@ struct WindowSeqs {
 // SPLIT: the waves share the keys of a row tile instead, 32 keys each, with a
 // maximum, sum and output of their own that are joined through LDS at the end
 // (4 waves a row tile of 64-wide heads, with tiles of 128 keys, 2 of wider
-// ones).  share_keys says when.
+// ones).  share_keys says when, by the whole call: the order of a row's sums, and
+// with it the last bits, is the kernel's.
 //
 // Measured: 16,384 rows, 16 heads of 128 over 2, window 4,096: 509 us, 950
 // TFLOP/s of the pairs in the window, where a product of 8,192^3 reaches 1,070
 // to 1,120; the matrix cores are busy half of the cycles and the clock falls
 // under the load.  8 sequences of up to 4,096 rows, 32 heads over 8, window
-// 1,024: 342 us, 755 TFLOP/s, with 18 tiles a workgroup between its first loads
-// and its stores.  64 samples of up to 577 rows, 6 heads of 64, sizes, a
-// two-sided window of 97: 37.0 us for 85 MB, bound by the vector instructions
-// of softmax and masks and by the chain of 5 tiles.
+// 1,024: 343 us, 747 TFLOP/s, matrix cores busy 38 %, with 18 tiles a workgroup
+// between its first loads and its stores.  64 samples of up to 577 rows, 6 heads
+// of 64, sizes, a two-sided window of 97: 37.3 us for 85 MB (90 read, 21
+// written), bound by the vector instructions of softmax and masks and by the
+// chain of 5 tiles.
 //
 // A probability of 0 does not take a value out of P V when that value is
 // infinite or NaN.  A tile that some query of the workgroup sees and another
@@ -865,8 +870,12 @@ hipError_t for_samples(const int32_t* cu_host, int batch, int rows, int units, F
 
 // Whether the waves of a workgroup share the keys of its row tiles, `parts` waves
 // a tile, instead of having a row tile each: where that many more workgroups
-// still run at once (2 a CU), or where hardly a window evens the rows out and
-// the last rows' chains of tiles are what the call takes.  One sample, causal
+// still run at once (2 a CU: groups x parts <= 512), or where hardly a window
+// evens the rows out and the last rows' chains of tiles are what the call takes:
+// a chain is longest / (keys of a tile) tiles, which sharing divides by `parts`,
+// and what it costs is the work of workgroups that no longer run at once, groups
+// x min(window, longest).  The second rule's two factors are set by the points
+// below, on whose sides of it they lie, and by nothing else.  One sample, causal
 // (row tiles each / shared, us; in brackets the workgroups without sharing):
 //   fp32: 512 rows, 16 heads of 128, window 300 [128] 40 / 25; 1,536, 6 of 64,
 //     964 [144] 59 / 31; 4,096, 6 of 64, none [384] 234 / 160; but 2,048, 6 of

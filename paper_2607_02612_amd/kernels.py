@@ -294,7 +294,8 @@ def _out(out, rows, heads, dh, like):
 def window_attention(q, k, v, cu, window=None, sinks=0, causal=True, size=None, out=None):
     """Attention of packed rows: row i of a sample sees its rows j <= i with
     i - j < window or j < sinks; with causal=False those with |i - j| < window
-    or j < sinks.  window None: no limit.  q [M, heads, dh], k and v
+    or j < sinks (the first rows are seen by all, but see their own window
+    only).  window None: no limit.  q [M, heads, dh], k and v
     [M, kv_heads, dh], bfloat16 or float32, dh a multiple of 8 up to 128, any
     row and head strides in whole 16-byte pieces (views of one product's
     output, say); cu: host offsets [batch + 1] (samples may be empty), rows
@@ -441,8 +442,8 @@ class TokenCache:
 def cache_append(cache, k, v, cu=None):
     """Append key and value rows [rows, kv_heads, dh]: one per sequence, or
     rows cu[i] .. cu[i+1]-1 to sequence i (cu: host offsets, rows from cu[-1]
-    on take no part).  Their weight starts at 0; rows past a sequence's
-    capacity are dropped."""
+    on take no part).  Their weight starts at 0, that of a prompt's rows too;
+    rows past a sequence's capacity are dropped."""
     kp, k_row, k_head = _heads(k, "k", cache.dtype, cache.kv_heads, cache.dh)
     vp, v_row, v_head = _heads(v, "v", cache.dtype, cache.kv_heads, cache.dh)
     _here(k, v)
@@ -486,9 +487,11 @@ def paged_attention(q, cache, window=None, sinks=0, accumulate=True, out=None):
 
 def cache_evict(cache, budget, sinks=0, recent=0):
     """Bring every sequence down to `budget` tokens: the first `sinks` and
-    last `recent` positions stay, and the others by accumulated weight.
-    Returns src int32 [batch, budget]: the slot from which each slot's token
-    came, -1 past the sequence's length."""
+    last `recent` positions stay, and the others by accumulated weight, equal
+    ones by the lower slot (tokens that have drawn nothing yet, such as a
+    prompt's before the first steps, are equal).  A token past the budget
+    that no page holds leaves first.  Returns src int32 [batch, budget]: the
+    slot from which each slot's token came, -1 past the sequence's length."""
     budget, sinks = _count(budget, "budget", 1, _LAST), _count(sinks, "sinks", 0, _LAST)
     recent = _count(recent, "recent", 0, _LAST)
     if budget > 1 << 30:
