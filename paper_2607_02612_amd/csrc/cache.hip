@@ -604,7 +604,8 @@ __global__ __launch_bounds__(1024, 8) void paged_join(CacheArgs c, PagedArgs a, 
     }
     part[wave][lane] = o0;
     if (DP > 64) part[wave][64 + lane] = o1;
-    const bool odd = __any(!(fabsf(o0) < INFINITY) | !(fabsf(o1) < INFINITY));
+    // (where a score is NaN, the row is, whatever the values)
+    const bool odd = __any(!(fabsf(o0) < INFINITY) | !(fabsf(o1) < INFINITY)) && l == l;
     if (lane == 0) {
       s_ml[wave] = make_float2(m, l);
       s_odd[wave] = odd;
@@ -631,7 +632,7 @@ __global__ __launch_bounds__(1024, 8) void paged_join(CacheArgs c, PagedArgs a, 
       if (real) {
         const Visible vis = visible(c, a, b);
         const int d1 = 64 + lane;
-        for (int i = wave % wpr; i < vis.nv; i += wpr * 2)
+        for (int i = wave % wpr; i < vis.nv; i += wpr * 2) {
 #pragma unroll
           for (int u = 0; u < 2; u++) {
             const int x = vis.slot(min(i + wpr * u, vis.nv - 1));  // (twice the last one: the same sum)
@@ -645,6 +646,9 @@ __global__ __launch_bounds__(1024, 8) void paged_join(CacheArgs c, PagedArgs a, 
             e0 += see & !(fabsf(x0) < INFINITY) ? x0 : 0.f;
             e1 += see & !(fabsf(x1) < INFINITY) ? x1 : 0.f;
           }
+          // (NaN in all dimensions: nothing changes any more)
+          if (__all((lane >= c.dh || e0 != e0) & (d1 >= c.dh || e1 != e1))) break;
+        }
       }
       part[wave][lane] = e0;
       part[wave][64 + lane] = e1;
@@ -652,7 +656,7 @@ __global__ __launch_bounds__(1024, 8) void paged_join(CacheArgs c, PagedArgs a, 
       float e = 0.f;
       if (d < c.dh)
         for (int w = 0; w < wpr; w++) e += part[w0 + w][d];
-      o = e == 0.f || sum != sum ? o : e;  // (a NaN score makes all of a row NaN)
+      o = e == 0.f || sum != sum ? o : e;
     }
     if (real && d < c.dh) ((T*)a.out)[row * c.dh + d] = St<T>::put(o);
     return;

@@ -229,3 +229,43 @@ def test_paged_attention_of_more_workgroups_than_a_launch(torch_cuda):
         part = _kern().TokenCache(k, v, table[s], length[s], length[s].clone(), w, pos[s])
         assert torch.equal(got[s], _kern().paged_attention(q[s], part)), b
         assert torch.equal(weight[s], w), b
+
+
+# ------------------------------------------------------------- NaN all over --
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("dh", [64, 72])
+def test_nan_queries_and_rows_of_nan(torch_cuda, dtype, dh):
+    """A query that is NaN gives NaN for itself alone; a row of values that is
+    NaN throughout gives NaN to what sees it, beside infinities too."""
+    torch = torch_cuda
+    rng = np.random.default_rng(dh)
+    kern = _kern()
+    c = _cache(torch, rng, dtype, [700, 3, 1200, 0], 2, dh, 16, 1200)
+    q = _normal(torch, rng, dtype, 4, 6, dh)
+    want = kern.paged_attention(q, c, accumulate=False)
+    bad = q.clone()
+    bad[0, 3], bad[1] = float("nan"), float("nan")
+    got = kern.paged_attention(bad, c, accumulate=False)
+    assert got[0, 3].isnan().all() and got[1].isnan().all()
+    ok = torch.ones(4, 6, dtype=torch.bool, device="cuda")
+    ok[0, 3], ok[1] = False, False
+    assert torch.equal(got[ok], want[ok])
+    v = c.v.clone()
+    v[int(c.table[2, 40]), 5] = float("nan")
+    v[int(c.table[2, 70]), 5, :, ::2] = float("inf")
+    d = kern.TokenCache(c.k, v, *c._tensors[2:])
+    got = kern.paged_attention(q, d, accumulate=False)
+    assert got[2].isnan().all() and torch.equal(got[[0, 1, 3]], want[[0, 1, 3]])
+
+    q, k, v = (_normal(torch, rng, dtype, 300, h, dh) for h in (4, 2, 2))
+    want = kern.window_attention(q, k, v, [0, 300], 90, 1)
+    q[7, 1] = float("nan")
+    v[150] = float("nan")
+    v[160, :, ::2] = float("inf")
+    got = kern.window_attention(q, k, v, [0, 300], 90, 1)
+    odd = torch.zeros(300, 4, dtype=torch.bool, device="cuda")
+    odd[7, 1], odd[150:240] = True, True
+    assert got[odd].isnan().all()
+    odd[240:250] = True
+    assert bool((got[240:250, :, ::2] == float("inf")).all())
+    assert torch.equal(got[~odd], want[~odd])
