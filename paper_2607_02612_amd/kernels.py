@@ -269,9 +269,13 @@ def _count(v, name, lowest=0, most=1 << 30):
     there is) it makes no difference."""
     if type(v) is int and lowest <= v <= most:
         return v
-    if int(v) != v or v < lowest:
+    try:
+        n = int(v)
+    except (OverflowError, TypeError, ValueError):  # infinite, no number, NaN
+        n = None
+    if n is None or n != v or n < lowest:
         raise ValueError(f"{name} must be a whole number, at least {lowest}")
-    return min(int(v), most)
+    return min(n, most)
 
 
 _LAST = (1 << 31) - 1  # position

@@ -170,3 +170,15 @@ def test_binding_refuses_budgets(budget, sinks, recent):
     would have another shape), nor are the counts that have to fit it."""
     with pytest.raises(ValueError):
         kernels.cache_evict(None, budget, sinks, recent)
+
+
+@pytest.mark.parametrize("v", [float("inf"), -float("inf"), float("nan"), 2.5, -1, None, "3", [1]])
+def test_binding_refuses_what_is_no_count(v):
+    for budget, sinks, recent in ((v, 0, 0), (8, v, 0), (8, 0, v)):
+        with pytest.raises(ValueError):
+            kernels.cache_evict(None, budget, sinks, recent)
+    t = torch.zeros(2, 2, 64, dtype=torch.bfloat16)
+    fake = type("Cache", (), dict(dtype=torch.bfloat16, batch=2, kv_heads=2, dh=64))()
+    if v is not None:  # (no window)
+        with pytest.raises(ValueError, match="window"):
+            kernels.paged_attention(t, fake, window=v)
