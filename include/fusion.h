@@ -499,6 +499,97 @@ FUSION_API size_t fusion_cache_evict_workspace_bytes(const fusion_cache* c, int 
 FUSION_API int fusion_cache_evict(const fusion_cache* c, int budget, int sinks, int recent,
                                   int32_t* src, void* ws, size_t ws_bytes, void* stream);
 
+/* A cache in 4 bits: beside a fusion_cache whose k and v are bytes of two codes
+ * (the lower dim in the lower half), uint8 [pages][page_size][kv_heads][dh / 2],
+ * their strides in bytes and multiples of 16, dh a multiple of 32, and whose
+ * precision is the type of the rows that come in and of queries and outputs.
+ * Codes are e2m1 (0, 1/2, 1, 3/2, 2, 3, 4, 6 and a sign bit above), each 32 dims
+ * of a head times a scale 2^(s - 127), s one byte of
+ *   k, v  device uint8 [pages][page_size][kv_heads][dh / 32], strides of the
+ *         first three in bytes.
+ * A block of 32 values comes in with the scale that brings its largest magnitude
+ * to 4 .. 8 (s in 2 .. 252), each value rounded to the nearest number, ties to
+ * the even code, above 6 to 6.  A block with an infinite or NaN value gets s =
+ * 255: all 32 read as NaN.  Wherever this struct may be null, null means a cache
+ * that is not in 4 bits. */
+typedef struct fusion_cache_scales {
+  uint8_t* k;
+  uint8_t* v;
+  int64_t k_strides[3]; /* page, place in the page, head */
+  int64_t v_strides[3];
+} fusion_cache_scales;
+
+/* Rows for a cache, whose queries and keys turn by their position. */
+typedef struct fusion_rotary_rows {
+  const void* q; /* device [rows][heads][dh], or null with heads = 0 */
+  const void* k; /* device [rows][kv_heads][dh] */
+  const void* v;
+  int64_t q_strides[2], k_strides[2], v_strides[2]; /* row, head */
+  void* q_out;          /* device [rows][heads][dh], contiguous: turned queries */
+  void* k_out;          /* device [rows][kv_heads][dh], contiguous: turned keys; or null */
+  const float* freq;    /* device fp32 [half]: radians per position */
+  const int32_t* drop;  /* device int32 [batch], or null */
+  int32_t heads, half, interleaved;
+} fusion_rotary_rows;
+
+/* fusion_cache_append of rows whose queries and keys are turned on the way: with
+ * p the position of a row's token and t_j = p freq[j], a product in 64 bits, the
+ * dims (x, y) = (j, j + half), or (2j, 2j + 1) with interleaved = 1, become
+ * (x cos t_j - y sin t_j, y cos t_j + x sin t_j); dims from 2 half on stay (half:
+ * a multiple of 4, 2 half <= dh; 0: nothing turns).  drop: so many of each
+ * sequence's newest tokens (read as 0 .. len) leave before, with len and seen:
+ * tokens drafted and not kept, for instance.  They must lie in its last slots,
+ * where an append puts them and an eviction may not have left them.  Rows past
+ * the capacity are dropped, but their turned queries and keys are given out.
+ * Outputs lie apart from the inputs.
+ * Errors: FUSION_E_INVALID_ARG, FUSION_E_HIP. */
+FUSION_API int fusion_cache_append_rotary(const fusion_cache* c, const fusion_cache_scales* sc,
+                                          const fusion_rotary_rows* r, const int32_t* cu, void* stream);
+
+/* fusion_paged_attention and fusion_cache_evict over a cache in 4 bits.  Scores
+ * and outputs are those of the values that the codes stand for, in fp32 sums. */
+FUSION_API size_t fusion_cache4_attention_workspace_bytes(const fusion_cache* c,
+                                                          const fusion_cache_scales* sc, int heads,
+                                                          int accumulate);
+FUSION_API int fusion_cache4_attention(const fusion_cache* c, const fusion_cache_scales* sc,
+                                       const void* q, const int64_t* strides, int heads, int window,
+                                       int sinks, int accumulate, void* out, void* ws,
+                                       size_t ws_bytes, void* stream);
+FUSION_API size_t fusion_cache4_evict_workspace_bytes(const fusion_cache* c,
+                                                      const fusion_cache_scales* sc, int budget);
+FUSION_API int fusion_cache4_evict(const fusion_cache* c, const fusion_cache_scales* sc, int budget,
+                                   int sinks, int recent, int32_t* src, void* ws, size_t ws_bytes,
+                                   void* stream);
+
+/* Bounds of the pages' keys: lo and hi, device [pages][kv_heads][dh] of the
+ * cache's precision, contiguous, receive the least and the greatest value of each
+ * dim over the tokens of each page that a sequence holds (NaN has no part in
+ * them), of the pages that hold its last `newest` slots or, with newest = 0, of all.
+ * Other pages' bounds stay as they are.  Errors: FUSION_E_INVALID_ARG, FUSION_E_HIP. */
+FUSION_API int fusion_page_bounds(const fusion_cache* c, const fusion_cache_scales* sc, void* lo,
+                                  void* hi, int newest, void* stream);
+
+/* Attention of one query token per sequence over the pages that each key head
+ * chooses.  A page's score is the largest, over the query heads of the key head,
+ * of sum_d q_d (q_d >= 0 ? hi_d : lo_d), which no score of the page's tokens
+ * passes; summed in 64 bits and rounded to 32.  Of a sequence with more than
+ * `blocks` pages the first `first` and last `recent` ones (recent >= 1, first +
+ * recent <= blocks) and those with the highest scores are attended, `blocks` in
+ * all (ties to the lower page; a page whose score is NaN ranks above the others,
+ * one that the table does not name below them).  Weights are left as they are.
+ * q, strides, out and ws as in fusion_paged_attention.
+ * chosen: device int32 [batch][kv_heads][blocks], the chosen pages (their place in
+ * the sequence's row of the table) in ascending order, then -1.
+ * Errors: FUSION_E_INVALID_ARG, FUSION_E_CAPACITY, FUSION_E_HIP. */
+FUSION_API size_t fusion_block_attention_workspace_bytes(const fusion_cache* c,
+                                                         const fusion_cache_scales* sc, int heads,
+                                                         int blocks);
+FUSION_API int fusion_block_attention(const fusion_cache* c, const fusion_cache_scales* sc,
+                                      const void* lo, const void* hi, const void* q,
+                                      const int64_t* strides, int heads, int blocks, int first,
+                                      int recent, void* out, int32_t* chosen, void* ws,
+                                      size_t ws_bytes, void* stream);
+
 /* Message of the last failed call on this thread ("" if none). */
 FUSION_API const char* fusion_last_error(void);
 

@@ -66,6 +66,18 @@ class FusionCache(ctypes.Structure):
                 ("dh", c_int32)]
 
 
+class FusionScales(ctypes.Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("k_strides", c_int64 * 3),
+                ("v_strides", c_int64 * 3)]
+
+
+class FusionRotaryRows(ctypes.Structure):
+    _fields_ = [("q", c_void_p), ("k", c_void_p), ("v", c_void_p), ("q_strides", c_int64 * 2),
+                ("k_strides", c_int64 * 2), ("v_strides", c_int64 * 2), ("q_out", c_void_p),
+                ("k_out", c_void_p), ("freq", c_void_p), ("drop", c_void_p), ("heads", c_int32),
+                ("half", c_int32), ("interleaved", c_int32)]
+
+
 class FusionError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"{STATUS.get(code, code)}: {msg}")
@@ -131,6 +143,24 @@ SIGNATURES = [
     ("fusion_cache_evict_workspace_bytes", c_size_t, [POINTER(FusionCache), c_int]),
     ("fusion_cache_evict", c_int, [POINTER(FusionCache), c_int, c_int, c_int, c_void_p,
                                    c_void_p, c_size_t, c_void_p]),
+    ("fusion_cache_append_rotary", c_int, [POINTER(FusionCache), POINTER(FusionScales),
+                                           POINTER(FusionRotaryRows), c_void_p, c_void_p]),
+    ("fusion_cache4_attention_workspace_bytes", c_size_t, [POINTER(FusionCache),
+                                                           POINTER(FusionScales), c_int, c_int]),
+    ("fusion_cache4_attention", c_int, [POINTER(FusionCache), POINTER(FusionScales), c_void_p,
+                                        c_void_p, c_int, c_int, c_int, c_int, c_void_p, c_void_p,
+                                        c_size_t, c_void_p]),
+    ("fusion_cache4_evict_workspace_bytes", c_size_t, [POINTER(FusionCache), POINTER(FusionScales),
+                                                       c_int]),
+    ("fusion_cache4_evict", c_int, [POINTER(FusionCache), POINTER(FusionScales), c_int, c_int, c_int,
+                                    c_void_p, c_void_p, c_size_t, c_void_p]),
+    ("fusion_page_bounds", c_int, [POINTER(FusionCache), POINTER(FusionScales), c_void_p, c_void_p,
+                                   c_int, c_void_p]),
+    ("fusion_block_attention_workspace_bytes", c_size_t, [POINTER(FusionCache),
+                                                          POINTER(FusionScales), c_int, c_int]),
+    ("fusion_block_attention", c_int, [POINTER(FusionCache), POINTER(FusionScales), c_void_p, c_void_p,
+                                       c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_void_p,
+                                       c_void_p, c_void_p, c_size_t, c_void_p]),
     ("fusion_last_error", c_char_p, []),
 ]
 

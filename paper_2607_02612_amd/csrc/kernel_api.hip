@@ -321,9 +321,16 @@ int check_strides(int precision, const int64_t* strides, int n) {
   return FUSION_OK;
 }
 
-size_t elem_bytes(int precision) { return precision == 1 ? 2 : 4; }
+int check_space(const void* ws, size_t bytes, size_t need) {
+  if (!ws || (uintptr_t)ws % 256) return bad("workspace is null or not 256-byte aligned");
+  if (bytes < need)
+    return api_fail(FUSION_E_CAPACITY, ("the call needs " + std::to_string(need) +
+                                        " bytes of workspace").c_str());
+  return FUSION_OK;
+}
 
-int check_cache(const fusion_cache* c, CacheArgs* a) {
+// (sc: the scales of a cache in 4 bits, else null)
+int check_cache(const fusion_cache* c, CacheArgs* a, const fusion_cache_scales* sc = nullptr) {
   if (!c) return bad("cache is null");
   if (int rc = check_heads(c->precision, c->kv_heads, c->kv_heads, c->dh)) return rc;
   if (c->batch < 1 || c->batch > 65536) return bad("batch must be in 1 .. 65536");
@@ -335,22 +342,87 @@ int check_cache(const fusion_cache* c, CacheArgs* a) {
   if (!c->k || !c->v || !c->table || !c->len || !c->seen || !c->weight || !c->pos)
     return bad("null cache buffer");
   if (((uintptr_t)c->k | (uintptr_t)c->v) % 16) return bad("buffers must be 16-byte aligned");
-  if (int rc = check_strides(c->precision, c->k_strides, 3)) return rc;
-  if (int rc = check_strides(c->precision, c->v_strides, 3)) return rc;
+  if (sc) {
+    if (!sc->k || !sc->v) return bad("null scales");
+    if (c->dh % 32) return bad("a cache in 4 bits needs a head width that is a multiple of 32");
+    for (int i = 0; i < 3; i++) {
+      if (c->k_strides[i] < 0 || c->k_strides[i] % 16 || c->v_strides[i] < 0 || c->v_strides[i] % 16)
+        return bad("strides must be multiples of 16 bytes, not negative");
+      if (sc->k_strides[i] < 0 || sc->v_strides[i] < 0) return bad("strides must not be negative");
+    }
+  } else {
+    if (int rc = check_strides(c->precision, c->k_strides, 3)) return rc;
+    if (int rc = check_strides(c->precision, c->v_strides, 3)) return rc;
+  }
   *a = CacheArgs{c->k, c->v, c->k_strides[0], c->k_strides[1], c->k_strides[2],
                  c->v_strides[0], c->v_strides[1], c->v_strides[2], c->table, c->len, c->seen,
                  c->weight, c->pos, c->batch, c->pages, c->max_pages,
                  c->max_pages * c->page_size, c->kv_heads, c->dh,
-                 fast_div((uint32_t)c->page_size)};
+                 fast_div((uint32_t)c->page_size), nullptr, nullptr, 0, 0, 0, 0, 0, 0};
+  if (sc) {
+    a->ks = sc->k; a->vs = sc->v;
+    a->ks_page = sc->k_strides[0]; a->ks_row = sc->k_strides[1]; a->ks_head = sc->k_strides[2];
+    a->vs_page = sc->v_strides[0]; a->vs_row = sc->v_strides[1]; a->vs_head = sc->v_strides[2];
+  }
   return FUSION_OK;
 }
 
-int check_space(const void* ws, size_t bytes, size_t need) {
-  if (!ws || (uintptr_t)ws % 256) return bad("workspace is null or not 256-byte aligned");
-  if (bytes < need)
-    return api_fail(FUSION_E_CAPACITY, ("the call needs " + std::to_string(need) +
-                                        " bytes of workspace").c_str());
+// Queries, output and workspace of one new token per sequence.
+int check_queries(const fusion_cache* c, const void* q, const int64_t* strides, const void* out) {
+  if (!q || !strides || !out) return bad("null buffer");
+  if (int rc = check_strides(c->precision, strides, 2)) return rc;
+  if (((uintptr_t)q | (uintptr_t)out) % 16) return bad("buffers must be 16-byte aligned");
   return FUSION_OK;
+}
+PagedArgs paged_args(const fusion_cache* c, const void* q, const int64_t* strides, int heads, int window,
+                     int sinks, int accumulate, void* out, void* ws) {
+  PagedArgs a{};
+  a.q = q; a.q_row = strides[0]; a.q_head = strides[1]; a.out = out;
+  a.H = heads; a.group = heads / c->kv_heads;
+  a.window = window; a.sinks = sinks; a.accumulate = accumulate;
+  a.scale = (float)(1.0 / std::sqrt((double)c->dh)); a.ws = ws;
+  return a;
+}
+size_t paged_bytes(const fusion_cache* c, const CacheArgs& a, int heads, int accumulate) {
+  if (a.ks)
+    return c->precision == 1 ? paged4_workspace_bytes<bf16_t>(a, heads, accumulate)
+                             : paged4_workspace_bytes<float>(a, heads, accumulate);
+  return c->precision == 1 ? paged_workspace_bytes<bf16_t>(a, heads, accumulate)
+                           : paged_workspace_bytes<float>(a, heads, accumulate);
+}
+int paged_attention(const fusion_cache* c, const fusion_cache_scales* sc, const void* q,
+                    const int64_t* strides, int heads, int window, int sinks, int accumulate, void* out,
+                    void* ws, size_t ws_bytes, void* stream) {
+  CacheArgs ca;
+  if (int rc = check_cache(c, &ca, sc)) return rc;
+  if (int rc = check_heads(c->precision, heads, c->kv_heads, c->dh)) return rc;
+  if (window < 0 || sinks < 0) return bad("window and sinks must not be negative");
+  if (accumulate != 0 && accumulate != 1) return bad("accumulate must be 0 or 1");
+  if (int rc = check_queries(c, q, strides, out)) return rc;
+  if (int rc = check_space(ws, ws_bytes, paged_bytes(c, ca, heads, accumulate))) return rc;
+  const PagedArgs a = paged_args(c, q, strides, heads, window, sinks, accumulate, out, ws);
+  hipStream_t s = (hipStream_t)stream;
+  hipError_t err;
+  if (sc)
+    err = c->precision == 1 ? launch_paged4_attention<bf16_t>(ca, a, s) : launch_paged4_attention<float>(ca, a, s);
+  else
+    err = c->precision == 1 ? launch_paged_attention<bf16_t>(ca, a, s) : launch_paged_attention<float>(ca, a, s);
+  return err == hipSuccess ? FUSION_OK : hip_fail("launch_paged_attention", err);
+}
+int cache_evict(const fusion_cache* c, const fusion_cache_scales* sc, int budget, int sinks, int recent,
+                int32_t* src, void* ws, size_t ws_bytes, void* stream) {
+  CacheArgs ca;
+  if (int rc = check_cache(c, &ca, sc)) return rc;
+  if (budget < 1 || budget > kNoWindow) return bad("budget must be in 1 .. 2^30");
+  if (sinks < 0 || recent < 0 || (int64_t)sinks + recent > budget)
+    return bad("sinks and recent must not be negative and fit the budget together");
+  if (!src) return bad("null buffer");
+  if (int rc = check_space(ws, ws_bytes, evict_workspace_bytes(ca, budget))) return rc;
+  const EvictArgs a{budget, sinks, recent, src, ws};
+  hipStream_t s = (hipStream_t)stream;
+  hipError_t err = c->precision == 1 ? launch_cache_evict<bf16_t>(ca, a, s)
+                                     : launch_cache_evict<float>(ca, a, s);
+  return err == hipSuccess ? FUSION_OK : hip_fail("launch_cache_evict", err);
 }
 
 // Device address of `scratch` on the current device, looked up on the
@@ -576,32 +648,13 @@ FUSION_API size_t fusion_paged_attention_workspace_bytes(const fusion_cache* c, 
                                                          int accumulate) {
   CacheArgs ca;
   if (check_cache(c, &ca) || check_heads(c->precision, heads, c->kv_heads, c->dh)) return 0;
-  return paged_workspace_bytes(ca, elem_bytes(c->precision), heads, accumulate);
+  return paged_bytes(c, ca, heads, accumulate);
 }
 
 FUSION_API int fusion_paged_attention(const fusion_cache* c, const void* q, const int64_t* strides,
                                       int heads, int window, int sinks, int accumulate, void* out,
                                       void* ws, size_t ws_bytes, void* stream) {
-  CacheArgs ca;
-  if (int rc = check_cache(c, &ca)) return rc;
-  if (int rc = check_heads(c->precision, heads, c->kv_heads, c->dh)) return rc;
-  if (window < 0 || sinks < 0) return bad("window and sinks must not be negative");
-  if (accumulate != 0 && accumulate != 1) return bad("accumulate must be 0 or 1");
-  if (!q || !strides || !out) return bad("null buffer");
-  if (int rc = check_strides(c->precision, strides, 2)) return rc;
-  if (((uintptr_t)q | (uintptr_t)out) % 16) return bad("buffers must be 16-byte aligned");
-  if (int rc = check_space(ws, ws_bytes, paged_workspace_bytes(ca, elem_bytes(c->precision), heads,
-                                                               accumulate)))
-    return rc;
-  PagedArgs a{};
-  a.q = q; a.q_row = strides[0]; a.q_head = strides[1]; a.out = out;
-  a.H = heads; a.group = heads / c->kv_heads;
-  a.window = window; a.sinks = sinks; a.accumulate = accumulate;
-  a.scale = (float)(1.0 / std::sqrt((double)c->dh)); a.ws = ws;
-  hipStream_t s = (hipStream_t)stream;
-  hipError_t err = c->precision == 1 ? launch_paged_attention<bf16_t>(ca, a, s)
-                                     : launch_paged_attention<float>(ca, a, s);
-  return err == hipSuccess ? FUSION_OK : hip_fail("launch_paged_attention", err);
+  return paged_attention(c, nullptr, q, strides, heads, window, sinks, accumulate, out, ws, ws_bytes, stream);
 }
 
 FUSION_API size_t fusion_cache_evict_workspace_bytes(const fusion_cache* c, int budget) {
@@ -612,18 +665,117 @@ FUSION_API size_t fusion_cache_evict_workspace_bytes(const fusion_cache* c, int 
 
 FUSION_API int fusion_cache_evict(const fusion_cache* c, int budget, int sinks, int recent,
                                   int32_t* src, void* ws, size_t ws_bytes, void* stream) {
+  return cache_evict(c, nullptr, budget, sinks, recent, src, ws, ws_bytes, stream);
+}
+
+FUSION_API size_t fusion_cache4_attention_workspace_bytes(const fusion_cache* c,
+                                                          const fusion_cache_scales* sc, int heads,
+                                                          int accumulate) {
   CacheArgs ca;
-  if (int rc = check_cache(c, &ca)) return rc;
-  if (budget < 1 || budget > kNoWindow) return bad("budget must be in 1 .. 2^30");
-  if (sinks < 0 || recent < 0 || (int64_t)sinks + recent > budget)
-    return bad("sinks and recent must not be negative and fit the budget together");
-  if (!src) return bad("null buffer");
-  if (int rc = check_space(ws, ws_bytes, evict_workspace_bytes(ca, budget))) return rc;
-  const EvictArgs a{budget, sinks, recent, src, ws};
+  if (!sc) { bad("null scales"); return 0; }
+  if (check_cache(c, &ca, sc) || check_heads(c->precision, heads, c->kv_heads, c->dh)) return 0;
+  return paged_bytes(c, ca, heads, accumulate);
+}
+
+FUSION_API int fusion_cache4_attention(const fusion_cache* c, const fusion_cache_scales* sc, const void* q,
+                                       const int64_t* strides, int heads, int window, int sinks,
+                                       int accumulate, void* out, void* ws, size_t ws_bytes,
+                                       void* stream) {
+  if (!sc) return bad("null scales");
+  return paged_attention(c, sc, q, strides, heads, window, sinks, accumulate, out, ws, ws_bytes, stream);
+}
+
+FUSION_API size_t fusion_cache4_evict_workspace_bytes(const fusion_cache* c, const fusion_cache_scales* sc,
+                                                      int budget) {
+  CacheArgs ca;
+  if (!sc) { bad("null scales"); return 0; }
+  if (check_cache(c, &ca, sc) || budget < 1) return 0;
+  return evict_workspace_bytes(ca, budget);
+}
+
+FUSION_API int fusion_cache4_evict(const fusion_cache* c, const fusion_cache_scales* sc, int budget, int sinks,
+                                   int recent, int32_t* src, void* ws, size_t ws_bytes, void* stream) {
+  if (!sc) return bad("null scales");
+  return cache_evict(c, sc, budget, sinks, recent, src, ws, ws_bytes, stream);
+}
+
+FUSION_API int fusion_cache_append_rotary(const fusion_cache* c, const fusion_cache_scales* sc,
+                                          const fusion_rotary_rows* r, const int32_t* cu, void* stream) {
+  CacheArgs ca;
+  if (int rc = check_cache(c, &ca, sc)) return rc;
+  if (!r) return bad("rows are null");
+  if (r->heads < 0 || r->heads > 4096) return bad("heads must be in 0 .. 4096");
+  if (r->half < 0 || r->half % 4 || 2 * r->half > c->dh)
+    return bad("the frequencies must be a multiple of 4, for no more dims than a head has");
+  if (r->half > 0 && !r->freq) return bad("null frequencies");
+  if (r->interleaved != 0 && r->interleaved != 1) return bad("interleaved must be 0 or 1");
+  if (cu) {
+    if (int rc = check_rows(cu, c->batch)) return rc;
+    if (cu[c->batch] == 0 && !r->drop) return FUSION_OK;  // no rows
+  }
+  if (!cu || cu[c->batch] > 0) {
+    if (!r->k || !r->v || (r->heads > 0 && (!r->q || !r->q_out))) return bad("null buffer");
+  }
+  if (int rc = check_strides(c->precision, r->q_strides, 2)) return rc;
+  if (int rc = check_strides(c->precision, r->k_strides, 2)) return rc;
+  if (int rc = check_strides(c->precision, r->v_strides, 2)) return rc;
+  if (((uintptr_t)r->q | (uintptr_t)r->k | (uintptr_t)r->v | (uintptr_t)r->q_out | (uintptr_t)r->k_out) % 16)
+    return bad("buffers must be 16-byte aligned");
+  const RotaryArgs a{r->q, r->k, r->v, r->q_strides[0], r->q_strides[1], r->k_strides[0], r->k_strides[1],
+                     r->v_strides[0], r->v_strides[1], r->q_out, r->k_out, r->freq, r->drop,
+                     r->heads, r->half, r->interleaved};
   hipStream_t s = (hipStream_t)stream;
-  hipError_t err = c->precision == 1 ? launch_cache_evict<bf16_t>(ca, a, s)
-                                     : launch_cache_evict<float>(ca, a, s);
-  return err == hipSuccess ? FUSION_OK : hip_fail("launch_cache_evict", err);
+  hipError_t err = c->precision == 1 ? launch_append_rotary<bf16_t>(ca, a, cu, s)
+                                     : launch_append_rotary<float>(ca, a, cu, s);
+  return err == hipSuccess ? FUSION_OK : hip_fail("launch_append_rotary", err);
+}
+
+FUSION_API int fusion_page_bounds(const fusion_cache* c, const fusion_cache_scales* sc, void* lo, void* hi,
+                                  int newest, void* stream) {
+  CacheArgs ca;
+  if (int rc = check_cache(c, &ca, sc)) return rc;
+  if (newest < 0) return bad("newest must not be negative");
+  if (!lo || !hi) return bad("null buffer");
+  if (((uintptr_t)lo | (uintptr_t)hi) % 16) return bad("buffers must be 16-byte aligned");
+  const BoundsArgs a{lo, hi, newest};
+  hipStream_t s = (hipStream_t)stream;
+  hipError_t err = c->precision == 1 ? launch_page_bounds<bf16_t>(ca, a, s)
+                                     : launch_page_bounds<float>(ca, a, s);
+  return err == hipSuccess ? FUSION_OK : hip_fail("launch_page_bounds", err);
+}
+
+FUSION_API size_t fusion_block_attention_workspace_bytes(const fusion_cache* c,
+                                                         const fusion_cache_scales* sc, int heads,
+                                                         int blocks) {
+  CacheArgs ca;
+  if (check_cache(c, &ca, sc) || check_heads(c->precision, heads, c->kv_heads, c->dh)) return 0;
+  if (blocks < 1 || blocks > kNoWindow) { bad("blocks must be in 1 .. 2^30"); return 0; }
+  return c->precision == 1 ? block_workspace_bytes<bf16_t>(ca, heads, blocks)
+                           : block_workspace_bytes<float>(ca, heads, blocks);
+}
+
+FUSION_API int fusion_block_attention(const fusion_cache* c, const fusion_cache_scales* sc, const void* lo,
+                                      const void* hi, const void* q, const int64_t* strides, int heads,
+                                      int blocks, int first, int recent, void* out, int32_t* chosen,
+                                      void* ws, size_t ws_bytes, void* stream) {
+  CacheArgs ca;
+  if (int rc = check_cache(c, &ca, sc)) return rc;
+  if (int rc = check_heads(c->precision, heads, c->kv_heads, c->dh)) return rc;
+  if (blocks < 1 || blocks > kNoWindow) return bad("blocks must be in 1 .. 2^30");
+  if (first < 0 || recent < 1 || (int64_t)first + recent > blocks)
+    return bad("recent must be at least 1, first not negative, and the blocks hold both");
+  if (int rc = check_queries(c, q, strides, out)) return rc;
+  if (!lo || !hi || !chosen) return bad("null buffer");
+  if (((uintptr_t)lo | (uintptr_t)hi) % 16) return bad("buffers must be 16-byte aligned");
+  const size_t need = c->precision == 1 ? block_workspace_bytes<bf16_t>(ca, heads, blocks)
+                                        : block_workspace_bytes<float>(ca, heads, blocks);
+  if (int rc = check_space(ws, ws_bytes, need)) return rc;
+  BlockArgs a{paged_args(c, q, strides, heads, 0, 0, 0, out, ws), lo, hi, first, recent, chosen};
+  a.p.blocks = blocks;
+  hipStream_t s = (hipStream_t)stream;
+  hipError_t err = c->precision == 1 ? launch_block_attention<bf16_t>(ca, a, s)
+                                     : launch_block_attention<float>(ca, a, s);
+  return err == hipSuccess ? FUSION_OK : hip_fail("launch_block_attention", err);
 }
 
 }  // extern "C"

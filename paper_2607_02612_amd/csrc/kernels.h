@@ -226,7 +226,9 @@ __device__ __forceinline__ uint32_t quot(uint32_t n, FastDiv f) {
   return (__umulhi(n, f.mul) + n) >> f.shift;
 }
 
-// A paged token cache (strides in elements: page, place in the page, head).
+// A paged token cache (strides in elements: page, place in the page, head).  In
+// 4 bits k and v are bytes of two e2m1 codes, with a scale 2^(s - 127) for each
+// 32 dims in ks and vs (null: not in 4 bits).
 struct CacheArgs {
   void *k, *v;  // T
   int64_t k_page, k_row, k_head, v_page, v_row, v_head;
@@ -236,6 +238,8 @@ struct CacheArgs {
   int* pos;          // [B][cap]
   int B, pages, max_pages, cap, Hkv, dh;
   FastDiv page;
+  uint8_t *ks, *vs;
+  int64_t ks_page, ks_row, ks_head, vs_page, vs_row, vs_head;
 };
 struct AppendArgs {
   const void *k, *v;  // T [rows][Hkv][dh]
@@ -245,6 +249,20 @@ template <typename T>
 hipError_t launch_cache_append(const CacheArgs& c, const AppendArgs& a, const int32_t* cu_host,
                                hipStream_t s);
 
+// Appending of rows whose queries and keys turn by their position (rotary.hip);
+// the cache in any of its types.
+struct RotaryArgs {
+  const void *q, *k, *v;  // T [rows][heads][dh]; q null: H = 0
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head;
+  void *q_out, *k_out;    // T, contiguous; k_out may be null
+  const float* freq;      // [half] radians per position
+  const int* drop;        // [B] newest tokens that the rows replace, or null
+  int H, half, pairs;     // pairs: dims 2j and 2j + 1 turn together, else j and j + half
+};
+template <typename T>
+hipError_t launch_append_rotary(const CacheArgs& c, const RotaryArgs& a, const int32_t* cu_host,
+                                hipStream_t s);
+
 struct PagedArgs {
   const void* q;  // T [B][H][dh]
   int64_t q_row, q_head;
@@ -252,10 +270,37 @@ struct PagedArgs {
   int H, group, window, sinks, accumulate;  // no limit: window = 0
   float scale;
   void* ws;
+  int blocks;  // pages that are chosen, at most (block attention)
 };
-size_t paged_workspace_bytes(const CacheArgs& c, size_t elem, int H, int accumulate);
+template <typename T>
+size_t paged_workspace_bytes(const CacheArgs& c, int H, int accumulate);
 template <typename T>
 hipError_t launch_paged_attention(const CacheArgs& c, const PagedArgs& a, hipStream_t s);
+// The same over a cache in 4 bits, T the type of queries and output (cache4.hip).
+template <typename T>
+size_t paged4_workspace_bytes(const CacheArgs& c, int H, int accumulate);
+template <typename T>
+hipError_t launch_paged4_attention(const CacheArgs& c, const PagedArgs& a, hipStream_t s);
+
+// Least and greatest value of each dim over the tokens of a page (blocks.hip).
+struct BoundsArgs {
+  void *lo, *hi;  // T [pages][Hkv][dh]
+  int newest;     // of the pages of each sequence's last so many slots; 0: of all
+};
+template <typename T>
+hipError_t launch_page_bounds(const CacheArgs& c, const BoundsArgs& a, hipStream_t s);
+
+// Attention over the pages that the bounds choose.
+struct BlockArgs {
+  PagedArgs p;
+  const void *lo, *hi;  // T [pages][Hkv][dh]
+  int first, recent;    // pages that are always chosen
+  int* chosen;          // [B][Hkv][blocks]
+};
+template <typename T>
+size_t block_workspace_bytes(const CacheArgs& c, int H, int blocks);
+template <typename T>
+hipError_t launch_block_attention(const CacheArgs& c, const BlockArgs& a, hipStream_t s);
 
 struct EvictArgs {
   int budget, sinks, recent;

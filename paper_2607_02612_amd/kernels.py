@@ -11,7 +11,10 @@ stream; the caller's tensors are recorded on it, except by gemm.
 For long sequences and token caches: window_attention (a sliding window over
 packed rows), TokenCache with cache_append, paged_attention (one new token per
 sequence, adding up the attention weight of each cached token) and cache_evict
-(the tokens with the most weight stay).  They compute no gradients.
+(the tokens with the most weight stay).  TokenCache4 holds a cache in 4 bits,
+cache_append_rotary turns queries and keys by their position on their way in,
+and block_attention reads the pages that PageBounds and the query choose.  They
+compute no gradients.
 """
 from __future__ import annotations
 
@@ -23,7 +26,8 @@ import torch
 from torch.autograd import forward_ad
 
 from . import _native
-from ._native import FusionCache, FusionPackedOut, FusionRagged, check
+from ._native import (FusionCache, FusionPackedOut, FusionRagged, FusionRotaryRows, FusionScales,
+                      check)
 
 EPI = {"store": 0, "gelu": 1, "resid": 2, "f32": 3}
 
@@ -338,6 +342,15 @@ def window_attention(q, k, v, cu, window=None, sinks=0, causal=True, size=None, 
     return out
 
 
+def _apart(t, name):
+    """The elements of a tensor lie apart from each other."""
+    extent = t.shape[3]
+    for st, n in sorted(zip(t.stride()[:3], t.shape[:3])):
+        if n > 1 and st < extent:
+            raise ValueError(f"{name} must not overlap itself")
+        extent = st * (n - 1) + extent if n > 1 else extent
+
+
 class TokenCache:
     """A paged cache of keys and values with the attention weight that each
     cached token has drawn; holds the caller's tensors and their checks.
@@ -352,25 +365,36 @@ class TokenCache:
     update k, v, length, seen, weight and pos in place, and the caller may
     too, in stream order.  Pages that a call writes must not be shared."""
 
+    # entry points that take the cache, and what follows it in their arguments
+    _attention, _evict = "fusion_paged_attention", "fusion_cache_evict"
+    _scales, _more = None, ()
+
     def __init__(self, k, v, table, length, seen, weight, pos):
         if not isinstance(k, torch.Tensor) or k.dim() != 4 or k.dtype not in _PREC:
             raise ValueError("k must be a bfloat16 or float32 tensor [pages, page_size, "
                              "kv_heads, dh]")
+        self._pages(k, v)
+        self._take((k, v, table, length, seen, weight, pos), k.dtype, k.shape[3])
+        self._bytes(self._evict, 1)  # the library's checks
+
+    @staticmethod
+    def _pages(k, v):
         for t, name in ((k, "k"), (v, "v")):
             if not isinstance(t, torch.Tensor) or t.shape != k.shape or t.dtype != k.dtype:
                 raise ValueError("k and v must have the same shape and type")
             if not t.is_cuda:
                 raise ValueError(f"{name} must be on a GPU")
-            extent = t.shape[3]
-            for st, n in sorted(zip(t.stride()[:3], t.shape[:3])):
-                if n > 1 and st < extent:
-                    raise ValueError(f"{name} must not overlap itself")
-                extent = st * (n - 1) + extent if n > 1 else extent
+            _apart(t, name)
             if t.stride(3) != 1 or t.data_ptr() % 16 or \
                     any(st * t.element_size() % 16 for st in t.stride()[:3]):
                 raise ValueError(f"{name} must have contiguous heads, and strides and a base in "
                                  "whole 16-byte pieces")
-        pages, page_size, kv_heads, dh = k.shape
+
+    def _take(self, tensors, dtype, dh):
+        """Checks what every cache has; `tensors`: k, v, table, length, seen,
+        weight, pos and the tensors of a kind of cache."""
+        k, v, table, length, seen, weight, pos = tensors[:7]
+        pages, page_size, kv_heads = k.shape[:3]
         for t, name in ((table, "table"), (length, "length"), (seen, "seen"), (pos, "pos")):
             _need(t, name, torch.int32)
         _need(weight, "weight", torch.float32)
@@ -381,23 +405,23 @@ class TokenCache:
             raise ValueError("length and seen must be [batch]")
         if tuple(weight.shape) != (batch, max_pages * page_size) or pos.shape != weight.shape:
             raise ValueError("weight and pos must be [batch, max_pages * page_size]")
-        self._tensors = (k, v, table, length, seen, weight, pos)
+        self._tensors = tensors
         if any(t.requires_grad for t in self._tensors):
             raise ValueError("the cache's tensors are written in place and have no gradients")
-        for t, name in zip(self._tensors, ("k", "v", "table", "length", "seen", "weight", "pos")):
+        for t, name in zip(self._tensors, ("k", "v", "table", "length", "seen", "weight", "pos",
+                                           "k_scale", "v_scale")):
             _no_grad(t, name)
         if any(t.device != k.device for t in self._tensors):
             raise ValueError("the cache's tensors must be on one GPU")
         self._c = FusionCache(k.data_ptr(), v.data_ptr(), k.stride()[:3], v.stride()[:3],
                               table.data_ptr(), length.data_ptr(), seen.data_ptr(),
-                              weight.data_ptr(), pos.data_ptr(), _PREC[k.dtype], batch, pages,
+                              weight.data_ptr(), pos.data_ptr(), _PREC[dtype], batch, pages,
                               page_size, max_pages, kv_heads, dh)
         self._ref = byref(self._c)
         self._space, self._streams = {}, set()
-        self.batch, self.kv_heads, self.dh, self.dtype = batch, kv_heads, dh, k.dtype
+        self.batch, self.kv_heads, self.dh, self.dtype = batch, kv_heads, dh, dtype
         self.capacity, self.device = max_pages * page_size, k.device
         self._index = k.get_device()
-        self._bytes("fusion_cache_evict_workspace_bytes", 1)  # the library's checks
 
     @classmethod
     def empty(cls, batch, capacity, kv_heads, dh, page_size=64, dtype=torch.bfloat16):
@@ -420,7 +444,7 @@ class TokenCache:
         """Workspace of a call, asked once."""
         key = (entry, *args)
         if key not in self._space:
-            n = getattr(_native.lib(), entry)(self._ref, *args)
+            n = getattr(_native.lib(), entry + "_workspace_bytes")(self._ref, *self._more, *args)
             if n == 0:
                 check(-1)
             self._space[key] = n
@@ -443,6 +467,62 @@ class TokenCache:
         return torch.empty(n, dtype=torch.uint8, device=self.device), n
 
 
+class TokenCache4(TokenCache):
+    """A TokenCache that holds its keys and values in 4 bits: e2m1 numbers (0,
+    1/2, 1, 3/2, 2, 3, 4, 6 and a sign) times a power of two for each 32 dims of a
+    head, 4.25 bits a value.
+
+    k, v uint8 [pages, page_size, kv_heads, dh / 2], two codes a byte, the lower
+    dim in the lower half, dh a multiple of 32 up to 128; k_scale, v_scale uint8
+    [pages, page_size, kv_heads, dh / 32], s for a scale of 2^(s - 127), 255: the
+    block is NaN; strides as in a TokenCache, those of the scales in whole bytes.
+    dtype: of the rows that come in, of queries and of outputs.  cache_append,
+    cache_append_rotary, paged_attention, cache_evict, PageBounds and
+    block_attention take it as they take a TokenCache; rows are rounded to 4
+    bits when they are appended."""
+    _attention, _evict = "fusion_cache4_attention", "fusion_cache4_evict"
+
+    def __init__(self, k, v, k_scale, v_scale, table, length, seen, weight, pos,
+                 dtype=torch.bfloat16):
+        if dtype not in _PREC:
+            raise ValueError("rows must be bfloat16 or float32")
+        if not isinstance(k, torch.Tensor) or k.dim() != 4 or k.dtype != torch.uint8 or k.shape[3] % 16:
+            raise ValueError("k must be a uint8 tensor [pages, page_size, kv_heads, dh / 2], dh a "
+                             "multiple of 32")
+        self._pages(k, v)
+        for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            if not isinstance(t, torch.Tensor) or t.dtype != torch.uint8 or \
+                    tuple(t.shape) != (*k.shape[:3], k.shape[3] // 16):
+                raise ValueError(f"{name} must be a uint8 tensor [pages, page_size, kv_heads, dh / 32]")
+            if t.shape[3] > 1 and t.stride(3) != 1:
+                raise ValueError(f"{name} must have contiguous heads")
+            _apart(t, name)
+        self._take((k, v, table, length, seen, weight, pos, k_scale, v_scale), dtype, 2 * k.shape[3])
+        self._s = FusionScales(k_scale.data_ptr(), v_scale.data_ptr(), k_scale.stride()[:3],
+                               v_scale.stride()[:3])
+        self._scales = byref(self._s)
+        self._more = (self._scales,)
+        self._bytes(self._evict, 1)  # the library's checks
+
+    @classmethod
+    def empty(cls, batch, capacity, kv_heads, dh, page_size=64, dtype=torch.bfloat16):
+        """An empty cache on the current GPU with pages for `capacity` tokens of
+        every sequence.  In memory the heads of a page come before its tokens, so
+        that what a key head reads of a page lies together."""
+        n = -(-capacity // page_size)
+        dev = torch.device("cuda", torch.cuda.current_device())
+        u8 = [torch.zeros((batch * n, kv_heads, page_size, w), dtype=torch.uint8,
+                          device=dev).transpose(1, 2) for w in (dh // 2, dh // 2, dh // 32, dh // 32)]
+        i32 = [torch.zeros(shape, dtype=torch.int32, device=dev)
+               for shape in ((batch,), (batch,), (batch, n * page_size))]
+        return cls(*u8, torch.arange(batch * n, dtype=torch.int32, device=dev).view(batch, n),
+                   i32[0], i32[1],
+                   torch.zeros((batch, n * page_size), dtype=torch.float32, device=dev), i32[2],
+                   dtype=dtype)
+
+    k_scale, v_scale = (property(lambda self, i=i: self._tensors[i]) for i in (7, 8))
+
+
 def cache_append(cache, k, v, cu=None):
     """Append key and value rows [rows, kv_heads, dh]: one per sequence, or
     rows cu[i] .. cu[i+1]-1 to sequence i (cu: host offsets, rows from cu[-1]
@@ -459,6 +539,11 @@ def cache_append(cache, k, v, cu=None):
     rows = k.shape[0]
     if v.shape[0] != rows or (rows != cache.batch if cu is None else rows < cu_h[-1]):
         raise ValueError("rows do not match the sequences")
+    if cache._scales is not None:
+        rows = FusionRotaryRows(None, kp, vp, (0, 0), (k_row, k_head), (v_row, v_head))
+        check(_native.lib().fusion_cache_append_rotary(cache._ref, cache._scales, byref(rows), cu_p,
+                                                       cache._ready(k, v)))
+        return
     check(_native.lib().fusion_cache_append(cache._ref, kp, vp,
                                             _Strides4(k_row, k_head, v_row, v_head), cu_p,
                                             cache._ready(k, v)))
@@ -481,9 +566,9 @@ def paged_attention(q, cache, window=None, sinks=0, accumulate=True, out=None):
     out = _out(out, cache.batch, heads, cache.dh, q)
     acc = 1 if accumulate else 0
     stream = cache._ready(q, None if fresh else out)
-    ws, n = cache._workspace("fusion_paged_attention_workspace_bytes", heads, acc)
-    check(_native.lib().fusion_paged_attention(
-        cache._ref, qp, _Strides2(q_row, q_head), heads, window,
+    ws, n = cache._workspace(cache._attention, heads, acc)
+    check(getattr(_native.lib(), cache._attention)(
+        cache._ref, *cache._more, qp, _Strides2(q_row, q_head), heads, window,
         _count(sinks, "sinks", 0, _LAST), acc,
         out.data_ptr(), ws.data_ptr(), n, stream))
     return out
@@ -503,8 +588,142 @@ def cache_evict(cache, budget, sinks=0, recent=0):
     if sinks + recent > budget:
         raise ValueError("sinks and recent do not fit the budget")
     stream = cache._ready()
-    ws, n = cache._workspace("fusion_cache_evict_workspace_bytes", budget)
+    ws, n = cache._workspace(cache._evict, budget)
     src = cache.table.new_empty((cache.batch, budget))
-    check(_native.lib().fusion_cache_evict(cache._ref, budget, sinks, recent, src.data_ptr(),
-                                           ws.data_ptr(), n, stream))
+    check(getattr(_native.lib(), cache._evict)(cache._ref, *cache._more, budget, sinks, recent,
+                                               src.data_ptr(), ws.data_ptr(), n, stream))
     return src
+
+
+def cache_append_rotary(cache, q, k, v, freq, cu=None, interleaved=False, drop=None, rotated_k=False,
+                        out=None):
+    """cache_append of rows whose queries q [rows, heads, dh] and keys are turned
+    by their position on the way.  freq: float32 [n] on the GPU, radians per
+    position, n a multiple of 4 with 2 n <= dh (none: nothing turns): at position
+    p dims j and j + n (interleaved: 2j and 2j + 1) turn by the angle p freq[j], a
+    product in 64 bits; dims from 2 n on stay.  drop: int32 [batch] on the GPU or
+    None; so many of each sequence's newest tokens leave before, such as drafted
+    ones that were not kept (they lie in its last slots unless an eviction has
+    moved them).  Returns (turned queries, turned keys): both contiguous, rows
+    from cu[-1] on zero; the keys, as window_attention takes them, only with
+    `rotated_k`, else None; a given out takes the queries, lies apart from the
+    inputs, and its rows from cu[-1] on are left as they were."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q must be a tensor [rows, heads, dh]")
+    rows, heads = q.shape[:2]
+    dh = cache.dh
+    qp, q_row, q_head = _heads(q, "q", cache.dtype, heads, dh)
+    kp, k_row, k_head = _heads(k, "k", cache.dtype, cache.kv_heads, dh)
+    vp, v_row, v_head = _heads(v, "v", cache.dtype, cache.kv_heads, dh)
+    _need(freq, "freq", torch.float32)
+    _no_grad(freq, "freq")
+    if freq.dim() != 1 or freq.shape[0] % 4 or 2 * freq.shape[0] > dh:
+        raise ValueError("freq must hold a multiple of 4 frequencies, for no more dims than a head has")
+    if drop is not None:
+        _need(drop, "drop", torch.int32)
+        if tuple(drop.shape) != (cache.batch,):
+            raise ValueError("drop must be [batch]")
+    _here(q, k, v, freq, drop)
+    cu_p, used = None, rows
+    if cu is not None:
+        cu_h, cu_p = _offsets(cu)
+        if len(cu_h) != cache.batch + 1:
+            raise ValueError("offsets must be [batch + 1]")
+        used = int(cu_h[-1])
+    if k.shape[0] != rows or v.shape[0] != rows or (rows != cache.batch if cu is None else rows < used):
+        raise ValueError("rows do not match the sequences")
+    fresh = out is None
+    out = _out(out, rows, heads, dh, q)
+    keys = k.new_empty((rows, cache.kv_heads, dh)) if rotated_k else None
+    if used < rows:
+        for t in (out if fresh else None, keys):
+            if t is not None:
+                t[max(used, 0):].zero_()
+    r = FusionRotaryRows(qp, kp, vp, (q_row, q_head), (k_row, k_head), (v_row, v_head), out.data_ptr(),
+                         _ptr(keys), freq.data_ptr() or None, _ptr(drop), heads, freq.shape[0],
+                         1 if interleaved else 0)
+    check(_native.lib().fusion_cache_append_rotary(
+        cache._ref, cache._scales, byref(r), cu_p,
+        cache._ready(q, k, v, freq, drop, None if fresh else out)))
+    return out, keys
+
+
+class PageBounds:
+    """The least and the greatest value of each dim of the keys of every page of
+    a cache, by which block_attention chooses pages: lo, hi [pages, kv_heads, dh]
+    of the cache's dtype.  Made for what the cache holds, or from given tensors
+    as they are.  update() brings them up to date: after the cache has changed
+    and before block_attention."""
+
+    def __init__(self, cache, lo=None, hi=None):
+        shape = (cache.k.shape[0], cache.kv_heads, cache.dh)
+        self.cache, given = cache, lo is not None or hi is not None
+        if not given:
+            lo, hi = (torch.zeros(shape, dtype=cache.dtype, device=cache.device) for _ in range(2))
+        for t, name in ((lo, "lo"), (hi, "hi")):
+            _need(t, name, cache.dtype)
+            _no_grad(t, name)
+            if t.requires_grad:
+                raise ValueError("bounds are written in place and have no gradients")
+            if tuple(t.shape) != shape or t.device != cache.device or t.data_ptr() % 16:
+                raise ValueError(f"{name} must be a 16-byte aligned tensor {list(shape)} on the cache's GPU")
+        self.lo, self.hi, self._streams = lo, hi, set()
+        if not given:
+            self.update()
+
+    def _ready(self, *used):
+        raw = self.cache._ready(*used)
+        if raw not in self._streams:
+            _current(self.cache._index, self.lo, self.hi)
+            self._streams.add(raw)
+        return raw
+
+    def update(self, new=None):
+        """Bounds of the pages that hold the newest `new` slots of each sequence,
+        at least as many as rows were appended since (None: of all its pages, as
+        after an eviction)."""
+        new = 0 if new is None else _count(new, "new", 1)
+        c = self.cache
+        check(_native.lib().fusion_page_bounds(c._ref, c._scales, self.lo.data_ptr(), self.hi.data_ptr(),
+                                               new, self._ready()))
+
+
+def block_attention(q, cache, bounds, blocks, first=0, recent=1, out=None):
+    """paged_attention of each sequence's newest token over `blocks` pages that
+    each key head chooses: the sequence's `first` and `recent` ones, and of the
+    others those whose keys can score highest by their bounds with one of the key
+    head's queries (equal ones: the lower page).  Sequences of no more pages
+    are attended whole.  Weights stay as they are.  bounds: PageBounds of the
+    cache, up to date.  Returns (out like q, contiguous; chosen int32 [batch,
+    kv_heads, blocks], the pages by their place in the sequence, ascending, then
+    -1)."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 3 or q.shape[0] != cache.batch:
+        raise ValueError("q must be a tensor [batch, heads, dh]")
+    heads = q.shape[1]
+    qp, q_row, q_head = _heads(q, "q", cache.dtype, heads, cache.dh)
+    if not isinstance(bounds, PageBounds) or bounds.cache is not cache:
+        raise ValueError("bounds must be the PageBounds of the cache")
+    blocks, first = _count(blocks, "blocks", 1, _LAST), _count(first, "first", 0, _LAST)
+    recent = _count(recent, "recent", 1, _LAST)
+    if blocks > 1 << 30:
+        raise ValueError("blocks must be at most 2^30")
+    if first + recent > blocks:
+        raise ValueError("first and recent do not fit the blocks")
+    _here(q)
+    fresh = out is None
+    out = _out(out, cache.batch, heads, cache.dh, q)
+    stream = bounds._ready(q, None if fresh else out)
+    key = ("fusion_block_attention", heads, blocks)
+    n = cache._space.get(key)
+    if n is None:
+        n = _native.lib().fusion_block_attention_workspace_bytes(cache._ref, cache._scales, heads, blocks)
+        if n == 0:
+            check(-1)
+        cache._space[key] = n
+    ws = torch.empty(n, dtype=torch.uint8, device=cache.device)
+    chosen = cache.table.new_empty((cache.batch, cache.kv_heads, blocks))
+    check(_native.lib().fusion_block_attention(
+        cache._ref, cache._scales, bounds.lo.data_ptr(), bounds.hi.data_ptr(), qp,
+        _Strides2(q_row, q_head), heads, blocks, first, recent, out.data_ptr(), chosen.data_ptr(),
+        ws.data_ptr(), n, stream))
+    return out, chosen
