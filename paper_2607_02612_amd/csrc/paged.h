@@ -51,17 +51,6 @@ __device__ __forceinline__ void load8(const T* p, float* x) {
   }
 }
 template <typename T>
-__device__ __forceinline__ void load4(const T* p, float* x) {
-  if constexpr (sizeof(T) == 2) {
-    const uint2 u = *(const uint2*)p;
-    x[0] = __uint_as_float(u.x << 16); x[1] = __uint_as_float(u.x & 0xFFFF0000u);
-    x[2] = __uint_as_float(u.y << 16); x[3] = __uint_as_float(u.y & 0xFFFF0000u);
-  } else {
-    const float4 a = *(const float4*)p;
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-  }
-}
-template <typename T>
 __device__ __forceinline__ void store8(T* p, const float* x) {
   if constexpr (sizeof(T) == 2) {
     *(uint4*)p = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),

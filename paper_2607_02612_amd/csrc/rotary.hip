@@ -22,20 +22,58 @@ template <typename R> struct Turn {
   R c, s;
 };
 
-constexpr double kTwoPi = 6.283185307179586477;        // nearest to 2 pi
-constexpr double kTwoPiRest = 2.449293598294706414e-16;  // 2 pi - kTwoPi
+// The angle less the nearest multiple k of pi / 2 (pi / 2 as a sum of two numbers),
+// then the series of sine and cosine, whose first terms left out are below 2^-54 of
+// the result at pi / 4; k tells which of the two, and its sign.  (A general sincos
+// carries the reduction of any angle, at the cost of half the registers.)
+constexpr double kHalfPi = 1.570796326794896619;           // nearest to pi / 2
+constexpr double kHalfPiRest = 6.123233995736766036e-17;   // pi / 2 - kHalfPi
 template <typename R>
 __device__ __forceinline__ Turn<R> turn_of(double angle) {
-  const double k = rint(angle * (1.0 / kTwoPi));
-  const double r = fma(-k, kTwoPiRest, fma(-k, kTwoPi, angle));
-  double s, c;
-  sincos(r, &s, &c);
-  return {(R)c, (R)s};
+  const double k = rint(angle * (1.0 / kHalfPi));
+  double r = fma(-k, kHalfPiRest, fma(-k, kHalfPi, angle));
+  r = fabs(r) <= 0.8 ? r : r * 0.0;  // (beyond 2^50 an angle of 64 bits holds no part of a turn)
+  const double z = r * r;
+  double s = 1.0 / 355687428096000.0, c = 1.0 / 20922789888000.0;  // 17!, 16!
+  s = fma(s, z, -1.0 / 1307674368000.0);
+  s = fma(s, z, 1.0 / 6227020800.0);
+  s = fma(s, z, -1.0 / 39916800.0);
+  s = fma(s, z, 1.0 / 362880.0);
+  s = fma(s, z, -1.0 / 5040.0);
+  s = fma(s, z, 1.0 / 120.0);
+  s = fma(s, z, -1.0 / 6.0);
+  s = fma(s * z, r, r);
+  c = fma(c, z, -1.0 / 87178291200.0);
+  c = fma(c, z, 1.0 / 479001600.0);
+  c = fma(c, z, -1.0 / 3628800.0);
+  c = fma(c, z, 1.0 / 40320.0);
+  c = fma(c, z, -1.0 / 720.0);
+  c = fma(c, z, 1.0 / 24.0);
+  c = fma(c, z, -0.5);
+  c = fma(c, z, 1.0);
+  const int quarter = (int)(int64_t)k & 3;
+  const double x = quarter & 1 ? s : c, y = quarter & 1 ? c : s;
+  return {(R)(quarter == 1 || quarter == 2 ? -x : x), (R)(quarter >= 2 ? -y : y)};
 }
 
-// Dims d .. d + 7 of a row, turned (x: those dims; row: the row's memory).
+// Dims d .. d + 7 of a row as they lie in memory, and of a key or query that
+// turns in halves the dims that they turn with.
+template <typename T> struct Piece {
+  typedef typename std::conditional<sizeof(T) == 2, uint2, uint4>::type Quad;  // four values
+  Quad x[2], y[2];
+};
+__device__ __forceinline__ void widen(uint2 u, float* x) {
+  x[0] = __uint_as_float(u.x << 16); x[1] = __uint_as_float(u.x & 0xFFFF0000u);
+  x[2] = __uint_as_float(u.y << 16); x[3] = __uint_as_float(u.y & 0xFFFF0000u);
+}
+__device__ __forceinline__ void widen(uint4 u, float* x) {
+  x[0] = __uint_as_float(u.x); x[1] = __uint_as_float(u.y);
+  x[2] = __uint_as_float(u.z); x[3] = __uint_as_float(u.w);
+}
+
+// The piece's eight values, turned (turns: the row's angles).
 template <typename T, typename R>
-__device__ __forceinline__ void turn8(const RotaryArgs& a, const T* row, int d, const Turn<R>* turns,
+__device__ __forceinline__ void turn8(const RotaryArgs& a, const Piece<T>& p, int d, const Turn<R>* turns,
                                       float* x) {
   if (d >= 2 * a.half) return;
   if (a.pairs) {
@@ -55,7 +93,7 @@ __device__ __forceinline__ void turn8(const RotaryArgs& a, const T* row, int d, 
     const bool second = e >= a.half;
     const int j = second ? e - a.half : e;
     float y[4];
-    load4(row + (second ? j : j + a.half), y);
+    widen(p.y[h], y);
 #pragma unroll
     for (int i = 0; i < 4; i++) {
       const Turn<R> t = turns[j + i];
@@ -87,69 +125,77 @@ __device__ __forceinline__ uint32_t to_four(const float* x, uint32_t* scale) {
   return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6], x[7], s, 3);
 }
 
-// Row r of the call, to the slot `slot` of sequence b, position pos: `step` lanes
-// take eight dims each.  turns: LDS of the lanes' wave, 64 angles.
-template <typename T, bool FOUR, typename R>
-__device__ __forceinline__ void rotary_row(const CacheArgs& c, const RotaryArgs& a, FastDiv pieces,
-                                           Turn<R>* turns, int b, int64_t r, int64_t slot, int64_t pos,
-                                           int lane, int step) {
-  const int in_wave = lane & 63;
-  if (in_wave < a.half) turns[in_wave] = turn_of<R>((double)pos * (double)a.freq[in_wave]);
-  // (the angles are the wave's own, and its LDS operations stay in order)
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  const bool held = slot < c.cap;
-  int page = -1, place = 0;
-  if (held) {
-    if (lane == 0) {
-      c.weight[(int64_t)b * c.cap + slot] = 0.f;
-      c.pos[(int64_t)b * c.cap + slot] = (int)pos;
-    }
-    const uint32_t pg = quot((uint32_t)slot, c.page);
-    page = page_of(c, b, pg);
-    place = (int)(slot - (int64_t)pg * c.page.d);
+// Eight dims of a query, key or value row: where they come from.
+template <typename T> struct Task {
+  const T* row;
+  int vec, d;  // queries, then keys, then values; first dim
+  Piece<T> p;
+};
+// Task t of row r (all past the last: `real` false, nothing is read).
+template <typename T>
+__device__ __forceinline__ void load_task(const CacheArgs& c, const RotaryArgs& a, FastDiv pieces, int64_t r,
+                                          int t, bool real, Task<T>* k) {
+  typedef typename Piece<T>::Quad Quad;
+  k->vec = (int)quot((uint32_t)t, pieces);
+  k->d = (t - k->vec * (int)pieces.d) * 8;
+  const int key = k->vec - a.H, value = key - c.Hkv;
+  k->row = key < 0 ? (const T*)a.q + r * a.q_row + k->vec * a.q_head
+           : value < 0 ? (const T*)a.k + r * a.k_row + key * a.k_head
+                       : (const T*)a.v + r * a.v_row + value * a.v_head;
+  if (!real) return;
+  if constexpr (sizeof(T) == 2) {
+    const uint4 u = *(const uint4*)(k->row + k->d);
+    k->p.x[0] = make_uint2(u.x, u.y);
+    k->p.x[1] = make_uint2(u.z, u.w);
+  } else {
+    k->p.x[0] = *(const uint4*)(k->row + k->d);
+    k->p.x[1] = *(const uint4*)(k->row + k->d + 4);
   }
-  const int all = (a.H + 2 * c.Hkv) * (int)pieces.d;
-  for (int t = lane; t < all; t += step) {
-    const int vec = (int)quot((uint32_t)t, pieces), d = (t - vec * (int)pieces.d) * 8;
-    float x[8];
-    if (vec < a.H) {
-      const T* row = (const T*)a.q + r * a.q_row + vec * a.q_head;
-      load8(row + d, x);
-      turn8(a, row, d, turns, x);
-      store8((T*)a.q_out + (r * a.H + vec) * c.dh + d, x);
-      continue;
-    }
-    const bool key = vec < a.H + c.Hkv;
-    const int h = vec - a.H - (key ? 0 : c.Hkv);
-    const T* row = key ? (const T*)a.k + r * a.k_row + h * a.k_head
-                       : (const T*)a.v + r * a.v_row + h * a.v_head;
-    load8(row + d, x);
-    if (key) {
-      turn8(a, row, d, turns, x);
-      if (sizeof(T) == 2 && FOUR)
+  if (value < 0 && !a.pairs && k->d < 2 * a.half) {
 #pragma unroll
-        for (int i = 0; i < 8; i++) x[i] = bf16_to_f32(f32_to_bf16(x[i]));
-      if (a.k_out) store8((T*)a.k_out + (r * c.Hkv + h) * c.dh + d, x);
-    }
-    if constexpr (FOUR) {
-      uint32_t scale;
-      const uint32_t codes = to_four(x, &scale);
-      if (page < 0) continue;
-      uint8_t* to = key ? (uint8_t*)c.k + page * c.k_page + place * c.k_row + h * c.k_head
-                        : (uint8_t*)c.v + page * c.v_page + place * c.v_row + h * c.v_head;
-      uint8_t* sc = key ? c.ks + page * c.ks_page + place * c.ks_row + h * c.ks_head
-                        : c.vs + page * c.vs_page + place * c.vs_row + h * c.vs_head;
-      *(uint32_t*)(to + d / 2) = codes;
-      if ((t & 3) == 0) sc[d / 32] = (uint8_t)scale;
-    } else if (page >= 0) {
-      T* to = key ? (T*)c.k + page * c.k_page + place * c.k_row + h * c.k_head
-                  : (T*)c.v + page * c.v_page + place * c.v_row + h * c.v_head;
-      store8(to + d, x);
+    for (int h = 0; h < 2; h++) {
+      const int e = k->d + 4 * h;
+      k->p.y[h] = *(const Quad*)(k->row + (e >= a.half ? e - a.half : e + a.half));
     }
   }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (the next row's angles come after its reads)
-  __builtin_amdgcn_wave_barrier();
+}
+
+// The task's eight values, turned, to where they go: the call's outputs, and
+// place `place` of page `page` (below 0: none).
+template <typename T, bool FOUR, typename R>
+__device__ __forceinline__ void store_task(const CacheArgs& c, const RotaryArgs& a, const Task<T>& k,
+                                           const Turn<R>* turns, int64_t r, int page, int place) {
+  const int d = k.d, key = k.vec - a.H, value = key - c.Hkv;
+  float x[8];
+  widen(k.p.x[0], x);
+  widen(k.p.x[1], x + 4);
+  if (value < 0) turn8(a, k.p, d, turns, x);
+  if (key < 0) {
+    store8((T*)a.q_out + (r * a.H + k.vec) * c.dh + d, x);
+    return;
+  }
+  const int h = value < 0 ? key : value;
+  if (value < 0) {
+    if (sizeof(T) == 2 && FOUR)
+#pragma unroll
+      for (int i = 0; i < 8; i++) x[i] = bf16_to_f32(f32_to_bf16(x[i]));
+    if (a.k_out) store8((T*)a.k_out + (r * c.Hkv + h) * c.dh + d, x);
+  }
+  if constexpr (FOUR) {
+    uint32_t scale;
+    const uint32_t codes = to_four(x, &scale);
+    if (page < 0) return;
+    uint8_t* to = value < 0 ? (uint8_t*)c.k + page * c.k_page + place * c.k_row + h * c.k_head
+                            : (uint8_t*)c.v + page * c.v_page + place * c.v_row + h * c.v_head;
+    uint8_t* sc = value < 0 ? c.ks + page * c.ks_page + place * c.ks_row + h * c.ks_head
+                            : c.vs + page * c.vs_page + place * c.vs_row + h * c.vs_head;
+    *(uint32_t*)(to + d / 2) = codes;
+    if ((d & 31) == 0) sc[d / 32] = (uint8_t)scale;
+  } else if (page >= 0) {
+    T* to = value < 0 ? (T*)c.k + page * c.k_page + place * c.k_row + h * c.k_head
+                      : (T*)c.v + page * c.v_page + place * c.v_row + h * c.v_head;
+    store8(to + d, x);
+  }
 }
 
 // Slots in use, positions so far, both without the tokens that are replaced.
@@ -160,6 +206,15 @@ __device__ __forceinline__ Start start_of(const CacheArgs& c, const RotaryArgs& 
   const int n = held(c, b), drop = a.drop ? max(0, min(a.drop[b], n)) : 0;
   return {n - drop, (int)((uint32_t)c.seen[b] - (uint32_t)drop), drop};
 }
+// Page and place in it of a slot; page -1: not held.
+struct Place {
+  int page, place;
+};
+__device__ __forceinline__ Place place_of(const CacheArgs& c, int b, int64_t slot) {
+  if (slot >= c.cap) return {-1, 0};
+  const uint32_t pg = quot((uint32_t)slot, c.page);
+  return {page_of(c, b, pg), (int)(slot - (int64_t)pg * c.page.d)};
+}
 __device__ __forceinline__ void move_lengths(const CacheArgs& c, Start st, int b, int rows) {
   if (rows == 0 && st.drop == 0) return;
   const int fit = min(rows, c.cap - st.have);
@@ -167,11 +222,15 @@ __device__ __forceinline__ void move_lengths(const CacheArgs& c, Start st, int b
   c.seen[b] = (int)((uint32_t)st.seen + (uint32_t)fit);
 }
 
-// One workgroup per sequence, for few rows each: the lengths move on in it.
+// One workgroup per sequence, for few rows each: the lengths move on in it.  A
+// chain of loads bounds it, so the workgroup has a thread for every task (up to
+// 1024), whose first load goes out before the angles are computed.
 template <typename T, bool FOUR, typename Seqs>
-__global__ __launch_bounds__(256) void rotary_few(CacheArgs c, RotaryArgs a, FastDiv pieces, Seqs sq) {
+__global__ __launch_bounds__(1024) void rotary_few(CacheArgs c, RotaryArgs a, FastDiv pieces, FastDiv tasks,
+                                                   Seqs sq) {
   typedef typename std::conditional<FOUR, double, float>::type R;
-  __shared__ Turn<R> turns[4][64];
+  __shared__ Turn<R> turns[APPEND_FEW][64];
+  const int tid = threadIdx.x, threads = blockDim.x;
   int b = blockIdx.x, n = 1;
   int64_t r0 = b;
   if constexpr (std::is_same<Seqs, AppendSeqs>::value) {
@@ -179,36 +238,70 @@ __global__ __launch_bounds__(256) void rotary_few(CacheArgs c, RotaryArgs a, Fas
     r0 = sq.cu[blockIdx.x];
     n = sq.cu[blockIdx.x + 1] - sq.cu[blockIdx.x];
   }
+  const int total = n * (int)tasks.d;
+  Task<T> k;
+  auto load = [&](int t) {
+    const int i = (int)quot((uint32_t)t, tasks);
+    load_task(c, a, pieces, r0 + i, t - i * (int)tasks.d, true, &k);
+  };
+  if (tid < total) load(tid);
   const Start st = start_of(c, a, b);
-  __syncthreads();  // all waves have the lengths
-  if (threadIdx.x == 0) move_lengths(c, st, b, n);
-  const int wave = threadIdx.x >> 6;
-  if (n == 1) {
-    rotary_row<T, FOUR, R>(c, a, pieces, turns[wave], b, r0, st.have, st.seen, threadIdx.x, 256);
-  } else {
-    for (int i = wave; i < n; i += 4)
-      rotary_row<T, FOUR, R>(c, a, pieces, turns[wave], b, r0 + i, (int64_t)st.have + i,
-                             (int64_t)st.seen + i, threadIdx.x & 63, 64);
+  for (int i = tid; i < n * 64; i += threads)
+    if ((i & 63) < a.half)
+      turns[i >> 6][i & 63] = turn_of<R>((double)((int64_t)st.seen + (i >> 6)) * (double)a.freq[i & 63]);
+  if (tid < n && (int64_t)st.have + tid < c.cap) {
+    c.weight[(int64_t)b * c.cap + st.have + tid] = 0.f;
+    c.pos[(int64_t)b * c.cap + st.have + tid] = (int)((int64_t)st.seen + tid);
+  }
+  __syncthreads();  // (all waves have the lengths, too)
+  if (tid == 0) move_lengths(c, st, b, n);
+  for (int t = tid; t < total; t += threads) {
+    if (t != tid) load(t);
+    const int i = (int)quot((uint32_t)t, tasks);
+    const Place at = place_of(c, b, (int64_t)st.have + i);
+    store_task<T, FOUR, R>(c, a, k, turns[i], r0 + i, at.page, at.place);
   }
 }
 
-// A wave per row; the lengths move on in a launch of their own.
+// A wave per row, two tasks a lane at a time; the lengths move on in a launch of
+// their own.  Bound by its bytes: 16,384 bf16 rows of 48 heads of 128 (512 MB in and
+// out) take 112 us, 4.6 TB/s, where a copy reaches 5.1; 119 with one task at a
+// time.  A wave that goes on to further rows holds the series' constants and the
+// call's strides in registers that the tasks need (152).
 template <typename T, bool FOUR>
-__global__ __launch_bounds__(256) void rotary_many(CacheArgs c, RotaryArgs a, FastDiv pieces,
-                                                   AppendSeqs sq) {
+__global__ __launch_bounds__(256) void rotary_many(CacheArgs c, RotaryArgs a, FastDiv pieces, int tasks,
+                                                   int block0, AppendSeqs sq) {
   typedef typename std::conditional<FOUR, double, float>::type R;
-  __shared__ Turn<R> turns[4][64];
-  const int wave = threadIdx.x >> 6, end = sq.cu[sq.n];
-  for (int r = sq.cu[0] + blockIdx.x * 4 + wave; r < end; r += gridDim.x * 4) {
-    int lo = 0, hi = sq.n - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (sq.cu[mid] <= r) lo = mid; else hi = mid - 1;
-    }
-    const int b = sq.first + lo, nth = r - sq.cu[lo];
-    const Start st = start_of(c, a, b);
-    rotary_row<T, FOUR, R>(c, a, pieces, turns[wave], b, r, (int64_t)st.have + nth,
-                           (int64_t)st.seen + nth, threadIdx.x & 63, 64);
+  constexpr int U = 2;
+  __shared__ Turn<R> turns_all[4][64];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  Turn<R>* turns = turns_all[wave];
+  const int r = sq.cu[0] + (block0 + (int)blockIdx.x) * 4 + wave;
+  if (r >= sq.cu[sq.n]) return;
+  int lo = 0, hi = sq.n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (sq.cu[mid] <= r) lo = mid; else hi = mid - 1;
+  }
+  const int b = sq.first + lo, nth = r - sq.cu[lo];
+  const Start st = start_of(c, a, b);
+  const int64_t slot = (int64_t)st.have + nth, pos = (int64_t)st.seen + nth;
+  const Place at = place_of(c, b, slot);
+  if (lane < a.half) turns[lane] = turn_of<R>((double)pos * (double)a.freq[lane]);
+  if (lane == 0 && slot < c.cap) {
+    c.weight[(int64_t)b * c.cap + slot] = 0.f;
+    c.pos[(int64_t)b * c.cap + slot] = (int)pos;
+  }
+  // (the angles are the wave's own, and its LDS operations stay in order)
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  for (int t0 = lane; t0 < tasks; t0 += 64 * U) {
+    Task<T> k[U];
+#pragma unroll
+    for (int u = 0; u < U; u++) load_task(c, a, pieces, r, t0 + 64 * u, t0 + 64 * u < tasks, &k[u]);
+#pragma unroll
+    for (int u = 0; u < U; u++)
+      if (t0 + 64 * u < tasks) store_task<T, FOUR, R>(c, a, k[u], turns, r, at.page, at.place);
   }
 }
 
@@ -222,8 +315,11 @@ __global__ __launch_bounds__(256) void rotary_lengths(CacheArgs c, RotaryArgs a,
 template <typename T, bool FOUR>
 hipError_t launch_rotary(const CacheArgs& c, const RotaryArgs& a, const int32_t* cu_host, hipStream_t s) {
   const FastDiv pieces = fast_div((uint32_t)c.dh / 8);
+  const int tasks = (a.H + 2 * c.Hkv) * (c.dh / 8);
+  const FastDiv by_row = fast_div((uint32_t)tasks);
+  auto threads = [&](int rows) { return std::min((int64_t)1024, ((int64_t)rows * tasks + 63) / 64 * 64); };
   if (!cu_host) {
-    rotary_few<T, FOUR><<<c.B, 256, 0, s>>>(c, a, pieces, OneRowEach{});
+    rotary_few<T, FOUR><<<c.B, threads(1), 0, s>>>(c, a, pieces, by_row, OneRowEach{});
     return hipGetLastError();
   }
   AppendSeqs sq;
@@ -236,9 +332,12 @@ hipError_t launch_rotary(const CacheArgs& c, const RotaryArgs& a, const int32_t*
     for (int i = 0; i < sq.n; i++) most = std::max(most, sq.cu[i + 1] - sq.cu[i]);
     if (most <= APPEND_FEW) {
       if (rows == 0 && !a.drop) continue;
-      rotary_few<T, FOUR><<<sq.n, 256, 0, s>>>(c, a, pieces, sq);
+      rotary_few<T, FOUR><<<sq.n, threads(std::max(most, 1)), 0, s>>>(c, a, pieces, by_row, sq);
     } else {
-      rotary_many<T, FOUR><<<std::min((rows + 3) / 4, APPEND_BLOCKS), 256, 0, s>>>(c, a, pieces, sq);
+      if (hipError_t e = in_launches((rows + 3) / 4, 256, [&](int first, unsigned grid) {
+            rotary_many<T, FOUR><<<grid, 256, 0, s>>>(c, a, pieces, tasks, first, sq);
+          }))
+        return e;
       rotary_lengths<<<(sq.n + 255) / 256, 256, 0, s>>>(c, a, sq);
     }
     if (hipError_t e = hipGetLastError()) return e;

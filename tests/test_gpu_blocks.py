@@ -198,6 +198,35 @@ def test_ties_signs_and_no_bounds(torch_cuda, bits):
                 _close(_np(got), out, tol, blocks)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("pages", [100, 700, 5000])
+def test_scores_that_32_bits_cannot_tell_apart(torch_cuda, dtype, pages):
+    """Keys that are the same numbers in another order: their sums are equal,
+    and sums of 32 bits are not.  Some pages are higher or lower by little more
+    than 32 bits hold, some by far."""
+    torch = torch_cuda
+    rng = np.random.default_rng(pages)
+    kern = _kern()
+    base = rng.standard_normal(64)
+    x = np.stack([rng.permutation(base) for _ in range(pages)])
+    x = torch.from_numpy(x.astype(np.float32)).to(_dt(torch, dtype)).double().numpy()
+    x[rng.integers(0, pages, pages // 9)] += 2.0 ** -6  # (a bf16 number's last bits, at 2)
+    x[rng.integers(0, pages, pages // 9)] -= 2.0 ** -6
+    x[rng.integers(0, pages, 3)] += 1
+    k = torch.from_numpy(x).cuda().to(_dt(torch, dtype)).repeat_interleave(2, 0).view(-1, 1, 64)
+    c = kern.TokenCache.empty(1, 2 * pages, 1, 64, 2, _dt(torch, dtype))
+    kern.cache_append(c, k, k, [0, 2 * pages])
+    b = kern.PageBounds(c)
+    q = torch.ones(1, 3, 64, dtype=c.dtype, device="cuda")
+    q[0, 1:] = -4
+    q[0, 2, :32] = 4
+    for heads in (slice(0, 1), slice(0, 2), slice(0, 3)):
+        for blocks in (3, pages // 20, pages // 3, pages - 1):
+            _, chosen = kern.block_attention(q[:, heads], c, b, blocks, 1, 1)
+            want = choose_ref(_np(q[:, heads]), c, _np(b.lo), _np(b.hi), blocks, 1, 1)
+            assert np.array_equal(chosen.cpu().numpy(), want), (heads, blocks)
+
+
 def test_infinite_values_of_chosen_pages(torch_cuda):
     """An output dimension with infinite values among the attended ones is
     their sum; infinities in pages that are not chosen have no influence."""
