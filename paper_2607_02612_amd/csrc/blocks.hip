@@ -415,8 +415,9 @@ __global__ __launch_bounds__(1024) void block_choose(CacheArgs c, BlockArgs a, c
 }
 
 template <typename T, bool FOUR>
-size_t block_space(const CacheArgs& c, int H, int blocks, char* ws, PagedSpace* space, uint32_t** keys) {
-  size_t n = paged_space<T, FOUR>(c, H, 0, ws, space);
+size_t block_space(const CacheArgs& c, int H, int blocks, char* ws, PagedSpace* space, uint32_t** keys,
+                   int KT) {
+  size_t n = paged_space<T, FOUR>(c, H, 0, ws, space, KT);
   if (space) {
     *keys = (uint32_t*)(ws + n);
     space->sel = (const int*)(ws + n + round256((size_t)c.B * c.Hkv * c.max_pages * 4));
@@ -428,7 +429,7 @@ template <typename T, bool FOUR>
 hipError_t launch_blocks(const CacheArgs& c, const BlockArgs& a, hipStream_t s) {
   PagedSpace ws;
   uint32_t* keys;
-  block_space<T, FOUR>(c, a.p.H, a.p.blocks, (char*)a.p.ws, &ws, &keys);
+  block_space<T, FOUR>(c, a.p.H, a.p.blocks, (char*)a.p.ws, &ws, &keys, paged_tile<T, FOUR>(a.p));
   if (c.max_pages > a.p.blocks) {
     // (a batch has at most 2^34 slots, so units fit 2^31)
     const uint32_t units = (uint32_t)c.B * (uint32_t)((c.max_pages + SCORE_PAGES - 1) / SCORE_PAGES);
@@ -465,8 +466,8 @@ template hipError_t launch_page_bounds<bf16_t>(const CacheArgs&, const BoundsArg
 
 template <typename T>
 size_t block_workspace_bytes(const CacheArgs& c, int H, int blocks) {
-  return c.ks ? block_space<T, true>(c, H, blocks, nullptr, nullptr, nullptr)
-              : block_space<T, false>(c, H, blocks, nullptr, nullptr, nullptr);
+  return c.ks ? block_space<T, true>(c, H, blocks, nullptr, nullptr, nullptr, FLAT_KT)
+              : block_space<T, false>(c, H, blocks, nullptr, nullptr, nullptr, tile_tokens<T, false>());
 }
 template <typename T>
 hipError_t launch_block_attention(const CacheArgs& c, const BlockArgs& a, hipStream_t s) {

@@ -357,13 +357,13 @@ template hipError_t launch_cache_append<bf16_t>(const CacheArgs&, const AppendAr
 
 template <typename T>
 size_t paged_workspace_bytes(const CacheArgs& c, int H, int accumulate) {
-  return paged_space<T, false>(c, H, accumulate, nullptr, nullptr);
+  return paged_space<T, false>(c, H, accumulate, nullptr, nullptr, tile_tokens<T, false>());
 }
 
 template <typename T>
 hipError_t launch_paged_attention(const CacheArgs& c, const PagedArgs& a, hipStream_t s) {
   PagedSpace ws;
-  paged_space<T, false>(c, a.H, a.accumulate, (char*)a.ws, &ws);
+  paged_space<T, false>(c, a.H, a.accumulate, (char*)a.ws, &ws, tile_tokens<T, false>());
   return launch_paged_by_width<T, false, false>(c, a, ws, s);
 }
 template size_t paged_workspace_bytes<float>(const CacheArgs&, int, int);

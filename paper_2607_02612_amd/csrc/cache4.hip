@@ -5,13 +5,13 @@ namespace fusion {
 
 template <typename T>
 size_t paged4_workspace_bytes(const CacheArgs& c, int H, int accumulate) {
-  return paged_space<T, true>(c, H, accumulate, nullptr, nullptr);
+  return paged_space<T, true>(c, H, accumulate, nullptr, nullptr, FLAT_KT);
 }
 
 template <typename T>
 hipError_t launch_paged4_attention(const CacheArgs& c, const PagedArgs& a, hipStream_t s) {
   PagedSpace ws;
-  paged_space<T, true>(c, a.H, a.accumulate, (char*)a.ws, &ws);
+  paged_space<T, true>(c, a.H, a.accumulate, (char*)a.ws, &ws, paged_tile<T, true>(a));
   return launch_paged_by_width<T, true, false>(c, a, ws, s);
 }
 template size_t paged4_workspace_bytes<float>(const CacheArgs&, int, int);

@@ -374,13 +374,16 @@ int check_queries(const fusion_cache* c, const void* q, const int64_t* strides, 
   if (((uintptr_t)q | (uintptr_t)out) % 16) return bad("buffers must be 16-byte aligned");
   return FUSION_OK;
 }
-PagedArgs paged_args(const fusion_cache* c, const void* q, const int64_t* strides, int heads, int window,
+PagedArgs paged_args(const fusion_cache* c, const CacheArgs& ca, const void* q, const int64_t* strides, int heads, int window,
                      int sinks, int accumulate, void* out, void* ws) {
   PagedArgs a{};
   a.q = q; a.q_row = strides[0]; a.q_head = strides[1]; a.out = out;
   a.H = heads; a.group = heads / c->kv_heads;
   a.window = window; a.sinks = sinks; a.accumulate = accumulate;
   a.scale = (float)(1.0 / std::sqrt((double)c->dh)); a.ws = ws;
+  a.flat = ca.ks && window == 0 && c->page_size % 16 == 0 &&
+           ((ca.k_page | ca.v_page | ca.ks_page | ca.vs_page) >> 32) == 0 &&
+           ((ca.k_row | ca.v_row | ca.ks_row | ca.vs_row) >> 26) == 0;
   return a;
 }
 size_t paged_bytes(const fusion_cache* c, const CacheArgs& a, int heads, int accumulate) {
@@ -400,7 +403,7 @@ int paged_attention(const fusion_cache* c, const fusion_cache_scales* sc, const 
   if (accumulate != 0 && accumulate != 1) return bad("accumulate must be 0 or 1");
   if (int rc = check_queries(c, q, strides, out)) return rc;
   if (int rc = check_space(ws, ws_bytes, paged_bytes(c, ca, heads, accumulate))) return rc;
-  const PagedArgs a = paged_args(c, q, strides, heads, window, sinks, accumulate, out, ws);
+  const PagedArgs a = paged_args(c, ca, q, strides, heads, window, sinks, accumulate, out, ws);
   hipStream_t s = (hipStream_t)stream;
   hipError_t err;
   if (sc)
@@ -770,7 +773,7 @@ FUSION_API int fusion_block_attention(const fusion_cache* c, const fusion_cache_
   const size_t need = c->precision == 1 ? block_workspace_bytes<bf16_t>(ca, heads, blocks)
                                         : block_workspace_bytes<float>(ca, heads, blocks);
   if (int rc = check_space(ws, ws_bytes, need)) return rc;
-  BlockArgs a{paged_args(c, q, strides, heads, 0, 0, 0, out, ws), lo, hi, first, recent, chosen};
+  BlockArgs a{paged_args(c, ca, q, strides, heads, 0, 0, 0, out, ws), lo, hi, first, recent, chosen};
   a.p.blocks = blocks;
   hipStream_t s = (hipStream_t)stream;
   hipError_t err = c->precision == 1 ? launch_block_attention<bf16_t>(ca, a, s)

@@ -271,6 +271,7 @@ struct PagedArgs {
   float scale;
   void* ws;
   int blocks;  // pages that are chosen, at most (block attention)
+  int flat;    // 4 bits, no window, pages of whole 16 tokens, strides of 32 bits (rows: 26)
 };
 template <typename T>
 size_t paged_workspace_bytes(const CacheArgs& c, int H, int accumulate);

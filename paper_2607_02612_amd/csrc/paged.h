@@ -112,7 +112,8 @@ constexpr int PAGED_SPLIT = 1024;  // sequences up to which the work is split ov
 // heads, 64 sequences of 4,096 tokens, 12 heads: with 2,048 parts 2.5 % slower,
 // with 4,096 4 %).
 constexpr int PAGED_WAVES = 2048, PAGED_WAVES_64 = 3 * 1024;
-constexpr int FOUR_WAVES = 3;  // a SIMD, of a cache in 4 bits
+// Waves of a SIMD over a cache in 4 bits, as the registers allow without spills.
+template <typename T, int DP> constexpr int four_waves() { return sizeof(T) == 4 && DP == 128 ? 2 : 3; }
 
 constexpr int LIST = 512;  // tokens of a part that are gathered at a time
 
@@ -141,6 +142,26 @@ __device__ __forceinline__ void four_values(uint2 c, uint32_t scale, uint4* v) {
 __device__ __forceinline__ void four_values(uint4 c, uint32_t scale, uint4* v) {
   four_values(make_uint2(c.x, c.y), scale, v);
   four_values(make_uint2(c.z, c.w), scale, v + 2);
+}
+// Columns of 16 lanes: `from`'s first W into the x-th W of `to`, and back (the others
+// of the result hold anything).
+template <int W>
+__device__ __forceinline__ float columns_right(int x, float to, float from) {
+  const int t = __float_as_int(to), f = __float_as_int(from);
+  int r = t;
+  if (W == 8) r = __builtin_amdgcn_update_dpp(t, f, 0x118, 0xF, 0xC, false);  // row_shr 8
+  if (W == 4 && x == 1) r = __builtin_amdgcn_update_dpp(t, f, 0x114, 0xF, 0x2, false);
+  if (W == 4 && x == 2) r = __builtin_amdgcn_update_dpp(t, f, 0x118, 0xF, 0x4, false);
+  if (W == 4 && x == 3) r = __builtin_amdgcn_update_dpp(t, f, 0x11C, 0xF, 0x8, false);
+  return __int_as_float(r);
+}
+template <int W>
+__device__ __forceinline__ uint32_t columns_left(int x, uint32_t v) {
+  if (W == 8 && x) return __builtin_amdgcn_mov_dpp(v, 0x108, 0xF, 0xF, true);  // row_shl 8
+  if (W == 4 && x == 1) return __builtin_amdgcn_mov_dpp(v, 0x104, 0xF, 0xF, true);
+  if (W == 4 && x == 2) return __builtin_amdgcn_mov_dpp(v, 0x108, 0xF, 0xF, true);
+  if (W == 4 && x == 3) return __builtin_amdgcn_mov_dpp(v, 0x10C, 0xF, 0xF, true);
+  return v;
 }
 // Eight fp32 numbers as sums of three bf16 numbers.
 __device__ __forceinline__ void bf16_parts(float4 a, float4 b, uint4* part) {
@@ -207,8 +228,46 @@ __device__ __forceinline__ Visible visible(const CacheArgs& c, const PagedArgs& 
   return v;
 }
 
+// The wave's part of the line of tiles: runs segment(sequence, its first tile, the
+// one past its last, part) for each piece of it, and leaves the plan of the parts
+// (the first wave of each line).
+template <int KT, bool SEL, typename F>
+__device__ __forceinline__ void paged_walk(const CacheArgs& c, const PagedArgs& a, const PagedSpace& ws,
+                                           int unit, int range, int lane, F segment) {
+  // the sequences whose tiles form the line: all, or the part's own
+  const bool split = c.B <= PAGED_SPLIT;
+  const int b0 = split ? 0 : range, b1 = split ? c.B : range + 1;
+  auto tiles_of = [&](int b) { return b < b1 ? (visible<SEL>(c, a, b).nv + KT - 1) / KT : 0; };
+  int total = 0;
+  for (int b = b0; b < b1; b += 64)
+    total += __builtin_amdgcn_readfirstlane(wave_sum_i(tiles_of(b + lane)));
+  const int per = max(1, split ? (total + ws.ranges - 1) / ws.ranges : total);
+  const int first = split ? range * per : 0, last = min(first + per, total);
+  const bool planner = unit == 0 && (range == 0 || !split);
+  if (first >= total && !planner) return;
+  int before = 0;  // tiles of the sequences before b
+  for (int b = b0; b < b1 && (before < last || planner); b += 64) {
+    const int t = tiles_of(b + lane);
+    int p = t;  // inclusive, then exclusive sum over the lanes
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(p, o, 64);
+      if (lane >= o) p += v;
+    }
+    const int sum = __builtin_amdgcn_readlane(p, 63);
+    p += before - t;
+    before += sum;
+    if (planner && b + lane < b1)
+      ws.plan[b + lane] = make_int2(p / per + b + lane, t > 0 ? (p + t - 1) / per - p / per + 1 : 0);
+    for (uint64_t mine = __ballot(t > 0 && p < last && p + t > first); mine; mine &= mine - 1) {
+      const int i = __builtin_ctzll(mine);
+      const int tp = __builtin_amdgcn_readlane(p, i), tn = __builtin_amdgcn_readlane(t, i);
+      segment(b + i, max(first - tp, 0), min(last - tp, tn), split ? range + b + i : range);
+    }
+  }
+}
+
 template <typename T, int DP, bool PAD, bool ACC, bool FOUR, bool SEL>
-__global__ __launch_bounds__(256, FOUR ? FOUR_WAVES : 2) void paged_attention(CacheArgs c, PagedArgs a,
+__global__ __launch_bounds__(256, (FOUR ? four_waves<T, DP>() : 2)) void paged_attention(CacheArgs c, PagedArgs a,
                                                                               PagedSpace ws) {
   constexpr bool BF = sizeof(T) == 2 || FOUR;  // values are bf16 in LDS
   constexpr int KT = BF ? 32 : 16, NSUB = KT / 16;
@@ -222,7 +281,7 @@ __global__ __launch_bounds__(256, FOUR ? FOUR_WAVES : 2) void paged_attention(Ca
   __shared__ __attribute__((aligned(16))) char v_all[4 * KT * VROW];
   // LDS that a wave's values leave free: scores held back, or a list of tokens
   // (allocated in units of 1280 bytes, 160 KB a CU, for the workgroups that run at once)
-  constexpr int SHARE = 160 * 1024 / (FOUR ? FOUR_WAVES : DP <= 64 ? 3 : 2) / 1280 * 1280 / 4;
+  constexpr int SHARE = 160 * 1024 / (FOUR ? four_waves<T, DP>() : DP <= 64 ? 3 : 2) / 1280 * 1280 / 4;
   constexpr int SCORE_BYTES = (SHARE - KT * VROW) / 1024 * 1024;
   static_assert(SCORE_BYTES >= 2048 && SCORE_BYTES >= LIST * 4, "a tile of 16 heads, a list");
   constexpr int SPARE = ACC ? SCORE_BYTES : LIST * 4;
@@ -368,7 +427,7 @@ __global__ __launch_bounds__(256, FOUR ? FOUR_WAVES : 2) void paged_attention(Ca
     const int slots = SCORE_BYTES >> tile_shift;
     int held_from = ta;
     auto store_scores = [&](int t) {  // tiles held_from .. t
-#pragma unroll
+#pragma unroll(FOUR ? 1 : SCORE_BYTES / 1024)
       for (int i = 0; i < SCORE_BYTES / 1024; i++) {
         const int at = (i * 64 + lane) * 16, x = held_from + (at >> tile_shift);
         const int in = at & ((1 << tile_shift) - 1);
@@ -402,19 +461,15 @@ __global__ __launch_bounds__(256, FOUR ? FOUR_WAVES : 2) void paged_attention(Ca
       constexpr bool LAST = decltype(last_c)::value;
       const uint32_t mask = mask_next;
       f32x4_t S[NSUB];
-      if constexpr (FOUR) {
-        // (what a hidden token's place holds is masked below, and its values are cleared)
-        const bool in = !PAD || g * BL * 2 < dh;
-#pragma unroll
-        for (int u = 0; u < NSUB; u++) {
-          four_values(k4[u], in ? ks[u] : 0, kr[u]);
-          Four v = v4[u];
-          if (!see[u] || !in) v = Four{};
-          four_values(v, see[u] && in ? vs[u] : 0, vr[u]);
-        }
-      }
 #pragma unroll
       for (int u = 0; u < NSUB; u++) {
+        if constexpr (FOUR) {
+          // (what a hidden token's place holds is masked below, and its values are cleared)
+          const bool in = !PAD || g * BL * 2 < dh;
+          four_values(k4[u], in ? ks[u] : 0, kr[u]);
+          if (!see[u] || !in) v4[u] = Four{};
+          vs[u] = see[u] && in ? vs[u] : 0;
+        }
         S[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < NL; s++) {
@@ -434,7 +489,8 @@ __global__ __launch_bounds__(256, FOUR ? FOUR_WAVES : 2) void paged_attention(Ca
         }
       }
 #pragma unroll
-      for (int u = 0; u < NSUB; u++)
+      for (int u = 0; u < NSUB; u++) {
+        if constexpr (FOUR) four_values(v4[u], vs[u], vr[u]);
 #pragma unroll
         for (int s = 0; s < NL; s++) {
           const uint4 x = vr[u][s];
@@ -447,6 +503,7 @@ __global__ __launch_bounds__(256, FOUR ? FOUR_WAVES : 2) void paged_attention(Ca
           else
             *(uint4*)(Vs + r * VROW + p * 16) = v;
         }
+      }
       __builtin_amdgcn_sched_barrier(0);
       if constexpr (!LAST) {
         point(t + 1, ahead);
@@ -480,11 +537,13 @@ __global__ __launch_bounds__(256, FOUR ? FOUR_WAVES : 2) void paged_attention(Ca
       const bool grow = mt > m + 8.f;
       const float f = grow ? __builtin_amdgcn_exp2f(m - mt) : 1.f;
       m = grow ? mt : m;
-      l *= f;
+      if (!FOUR || __any(grow)) {
+        l *= f;
 #pragma unroll
-      for (int d = 0; d < ND; d++)
+        for (int d = 0; d < ND; d++)
 #pragma unroll
-        for (int j = 0; j < 4; j++) O[d][j] *= f;
+          for (int j = 0; j < 4; j++) O[d][j] *= f;
+      }
       const float mu = m == -INFINITY ? 0.f : m;
 #pragma unroll
       for (int u = 0; u < NSUB; u++) {
@@ -575,36 +634,298 @@ __global__ __launch_bounds__(256, FOUR ? FOUR_WAVES : 2) void paged_attention(Ca
     }
   };
 
-  // the sequences whose tiles form the line: all, or the part's own
-  const bool split = c.B <= PAGED_SPLIT;
-  const int b0 = split ? 0 : range, b1 = split ? c.B : range + 1;
-  auto tiles_of = [&](int b) { return b < b1 ? (visible<SEL>(c, a, b).nv + KT - 1) / KT : 0; };
-  int total = 0;
-  for (int b = b0; b < b1; b += 64)
-    total += __builtin_amdgcn_readfirstlane(wave_sum_i(tiles_of(b + lane)));
-  const int per = max(1, split ? (total + ws.ranges - 1) / ws.ranges : total);
-  const int first = split ? range * per : 0, last = min(first + per, total);
-  const bool planner = unit == 0 && (range == 0 || !split);
-  if (first >= total && !planner) return;
-  int before = 0;  // tiles of the sequences before b
-  for (int b = b0; b < b1 && (before < last || planner); b += 64) {
-    const int t = tiles_of(b + lane);
-    int p = t;  // inclusive, then exclusive sum over the lanes
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(p, o, 64);
-      if (lane >= o) p += v;
+  paged_walk<KT, SEL>(c, a, ws, unit, range, lane, segment);
+}
+
+// The same over 4 bits without a window, in pages of whole 16 tokens: tiles of 64
+// tokens whose sub-tiles of 16 lie in a page each, so that addresses are the
+// wave's and a lane adds what it always adds (the general kernel spends as much on
+// addresses as on arithmetic); rows past the end are read (their page has them) and
+// masked.
+//
+// A key head of up to 16 / R query heads fills 16 / R of the 16 columns of the
+// scores.  R sub-tiles are moved side by side, so that the softmax works on 64 tokens
+// in 16 / R registers where it took 16, and the weights move back for the product
+// with the values.  Keys are on their way while the softmax and the values are worked
+// on, values while the next scores are; the halves of a tile's values share the LDS.
+// Bound by the issue of vector instructions and its waits in turn: FLAT_FIGURES.
+constexpr int FLAT_KT = 64;
+template <typename T, int DP, int R> constexpr int flat_waves() { return R < 4 && DP == 128 ? 2 : four_waves<T, DP>(); }
+template <typename T, int DP, bool PAD, bool ACC, bool SEL, int R>
+__global__ __launch_bounds__(256, (flat_waves<T, DP, R>())) void paged4_flat(CacheArgs c, PagedArgs a,
+                                                                        PagedSpace ws) {
+  constexpr int KT = FLAT_KT, NSUB = 4, NS = NSUB / R, W = 16 / R;
+  constexpr int NL = DP / 32, ND = DP / 16, VROW = DP * 2, BL = DP / 8;
+  constexpr int NQ = sizeof(T) == 4 ? 3 : 1, NP = sizeof(T) == 4 ? 3 : 2;
+  typedef typename std::conditional<DP == 128, uint4, uint2>::type Four;
+  __shared__ __attribute__((aligned(16))) char v_all[4 * 32 * VROW];
+  constexpr int SHARE = 160 * 1024 / flat_waves<T, DP, R>() / 1280 * 1280 / 4;
+  constexpr int SCORE_BYTES = (SHARE - 32 * VROW) / 1024 * 1024;
+  static_assert(SCORE_BYTES >= 16 * KT * 4, "a tile of 16 heads");
+  __shared__ __attribute__((aligned(16))) char s_all[ACC ? 4 * SCORE_BYTES : 16];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int g = lane >> 4, cl = lane & 15;
+  const int id = (blockIdx.x + ws.block0) * 4 + wave, unit = id % ws.units, range = id / ws.units;
+  if (range >= ws.ranges) return;
+  char* Vs = v_all + wave * 32 * VROW;
+  char* Ss = s_all + (ACC ? wave * SCORE_BYTES : 0);
+  const int kh = unit / ws.qtiles, qt = unit % ws.qtiles;
+  const int h0 = kh * a.group + qt * 16, nq = min(16, a.group - qt * 16);
+  const float sc2 = a.scale * kLog2e;
+  const bool in = !PAD || g * BL * 2 < c.dh;
+  const uint32_t at4 = in ? g * BL : 0, block4 = at4 >> 4;
+  const uint32_t k_lane = cl * (uint32_t)c.k_row + at4, v_lane = cl * (uint32_t)c.v_row + at4;
+  const uint32_t ks_lane = cl * (uint32_t)c.ks_row + block4, vs_lane = cl * (uint32_t)c.vs_row + block4;
+  const uint8_t* k_base = (const uint8_t*)c.k + kh * c.k_head;
+  const uint8_t* v_base = (const uint8_t*)c.v + kh * c.v_head;
+  const uint8_t* ks_base = c.ks + kh * c.ks_head;
+  const uint8_t* vs_base = c.vs + kh * c.vs_head;
+  auto v_at = [](int r, int seg) {  // (as in paged_attention)
+    return r * VROW + ((seg ^ (DP == 128 ? r & 7 : r >> 1 & 3)) << 5);
+  };
+  const int tile_shift = 31 - __builtin_clz(2 * nq - 1) + 8, slots = SCORE_BYTES >> tile_shift;
+
+  auto segment = [&](int b, int t0, int t1, int part) {
+    const int limit = __builtin_amdgcn_readfirstlane(visible<SEL>(c, a, b).nv);
+    uint4 q[NQ][NL];
+#pragma unroll
+    for (int s = 0; s < NL; s++) {
+#pragma unroll
+      for (int i = 0; i < NQ; i++) q[i][s] = make_uint4(0, 0, 0, 0);
+      const int d = (NL * g + s) * 8;
+      if (cl < nq && (!PAD || d < c.dh)) {
+        const T* qp = (const T*)a.q + (int64_t)b * a.q_row + (int64_t)(h0 + cl) * a.q_head + d;
+        if constexpr (NQ == 1) {
+          q[0][s] = *(const uint4*)qp;
+        } else {
+          uint4 parts[3];
+          bf16_parts(*(const float4*)qp, *(const float4*)(qp + 4), parts);
+#pragma unroll
+          for (int i = 0; i < NQ; i++) q[i][s] = parts[i];
+        }
+      }
     }
-    const int sum = __builtin_amdgcn_readlane(p, 63);
-    p += before - t;
-    before += sum;
-    if (planner && b + lane < b1)
-      ws.plan[b + lane] = make_int2(p / per + b + lane, t > 0 ? (p + t - 1) / per - p / per + 1 : 0);
-    for (uint64_t mine = __ballot(t > 0 && p < last && p + t > first); mine; mine &= mine - 1) {
-      const int i = __builtin_ctzll(mine);
-      const int tp = __builtin_amdgcn_readlane(p, i), tn = __builtin_amdgcn_readlane(t, i);
-      segment(b + i, max(first - tp, 0), min(last - tp, tn), split ? range + b + i : range);
+    const int* table = SEL ? ws.sel + ((int64_t)b * c.Hkv + kh) * a.blocks
+                           : c.table + (int64_t)b * c.max_pages;
+    Four k4[NSUB], v4[NSUB];
+    uint32_t ks[NSUB], vs[NSUB];
+    const uint8_t *kp[NSUB], *vp[NSUB], *ksp[NSUB], *vsp[NSUB];
+    int here;  // sub-tiles whose page is there, one bit each
+    // pages of the sub-tiles, in the first lanes
+    auto find = [&](int t) {
+      return table[quot((uint32_t)min(t * KT + 16 * (lane & 3), limit - 1), c.page)];
+    };
+    auto aim = [&](int t, int found) {
+      here = 0;
+#pragma unroll
+      for (int u = 0; u < NSUB; u++) {
+        const int x = t * KT + 16 * u, page = __builtin_amdgcn_readlane(found, u);
+        const bool h = x < limit && (unsigned)page < (unsigned)c.pages;
+        const uint32_t p = h ? page : 0;
+        const uint32_t r = h ? x - quot((uint32_t)x, c.page) * c.page.d : 0;
+        here |= h << u;
+        kp[u] = k_base + (uint64_t)p * (uint32_t)c.k_page + (uint64_t)r * (uint32_t)c.k_row;
+        vp[u] = v_base + (uint64_t)p * (uint32_t)c.v_page + (uint64_t)r * (uint32_t)c.v_row;
+        ksp[u] = ks_base + (uint64_t)p * (uint32_t)c.ks_page + (uint64_t)r * (uint32_t)c.ks_row;
+        vsp[u] = vs_base + (uint64_t)p * (uint32_t)c.vs_page + (uint64_t)r * (uint32_t)c.vs_row;
+      }
+    };
+    auto load_k = [&]() {
+#pragma unroll
+      for (int u = 0; u < NSUB; u++) {
+        k4[u] = *(const Four*)(kp[u] + k_lane);
+        ks[u] = ksp[u][ks_lane];
+      }
+    };
+    auto load_v = [&]() {
+#pragma unroll
+      for (int u = 0; u < NSUB; u++) {
+        v4[u] = *(const Four*)(vp[u] + v_lane);
+        vs[u] = vsp[u][vs_lane];
+      }
+    };
+    float m = -INFINITY, l = 0.f;
+    f32x4_t O[ND];
+#pragma unroll
+    for (int d = 0; d < ND; d++) O[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    int held_from = t0;
+    auto store_scores = [&](int t) {  // tiles held_from .. t
+#pragma unroll 1
+      for (int i = 0; i < SCORE_BYTES / 1024; i++) {
+        const int at = (i * 64 + lane) * 16, x = held_from + (at >> tile_shift);
+        const int in_tile = at & ((1 << tile_shift) - 1);
+        if (x <= t && in_tile < nq * KT * 4)
+          *(uint4*)((char*)(ws.score + (((int64_t)b * ws.units + unit) * ws.tiles + x) * ws.heads * KT) +
+                    in_tile) = *(const uint4*)(Ss + at);
+      }
+      held_from = t + 1;
+    };
+    auto tile = [&](int t, int& ahead, auto last_c) {
+      constexpr bool LAST = decltype(last_c)::value;
+      const int left = limit - t * KT, there = here;
+      const bool whole = left >= KT && there == (1 << NSUB) - 1;
+      if (!whole) {
+#pragma unroll
+        for (int u = 0; u < NSUB; u++) {
+          const bool seen = 16 * u + cl < left && (there >> u & 1);
+          if (!seen) v4[u] = Four{};
+          vs[u] = seen ? vs[u] : 0;
+        }
+      }
+      if (PAD && !in) {
+#pragma unroll
+        for (int u = 0; u < NSUB; u++) {
+          v4[u] = Four{};
+          vs[u] = ks[u] = 0;
+        }
+      }
+      // scores: sub-tile i R + x of the columns x W .. x W + W - 1 of set i
+      f32x4_t S[NS];
+#pragma unroll
+      for (int u = 0; u < NSUB; u++) {
+        uint4 kr[NL];
+        four_values(k4[u], ks[u], kr);
+        f32x4_t x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < NL; s++)
+#pragma unroll
+          for (int i = NQ - 1; i >= 0; i--)
+            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kr[s]),
+                                                        __builtin_bit_cast(bf16x8_t, q[i][s]), x, 0, 0, 0);
+        if (u % R == 0) {
+          S[u / R] = x;
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; j++) S[u / R][j] = columns_right<W>(u % R, S[u / R][j], x[j]);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (!LAST) {
+        aim(t + 1, ahead);
+        __builtin_amdgcn_sched_barrier(0);
+        ahead = find(min(t + 2, t1 - 1));
+        load_k();
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      const int col = cl / W;  // sub-tile of the lane's column within its set
+#pragma unroll
+      for (int i = 0; i < NS; i++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) S[i][j] *= sc2;
+      if (!whole) {
+#pragma unroll
+        for (int i = 0; i < NS; i++) {
+          const int u = i * R + col;
+#pragma unroll
+          for (int j = 0; j < 4; j++)
+            S[i][j] = 16 * u + 4 * g + j < left && (there >> u & 1) ? S[i][j] : -INFINITY;
+        }
+      }
+      if constexpr (ACC) {
+        if (cl % W < nq) {
+#pragma unroll
+          for (int i = 0; i < NS; i++)
+            *(f32x4_t*)(Ss + ((t - held_from) << tile_shift) +
+                        (cl % W * KT + 16 * (i * R + col) + 4 * g) * 4) = S[i];
+        }
+        if (LAST || t - held_from == slots - 1) store_scores(t);
+      }
+      float mt = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < NS; i++)
+        mt = fmaxf(mt, fmaxf(fmaxf(S[i][0], S[i][1]), fmaxf(S[i][2], S[i][3])));
+      if (R == 4) mt = fmaxf(mt, dpp_peer<0x124>(mt));  // row_ror 4
+      if (R >= 2) mt = fmaxf(mt, dpp_peer<0x128>(mt));  // row_ror 8
+      mt = max_xor32(max_xor16(mt));
+      const bool grow = mt > m + 8.f;
+      if (__any(grow)) {
+        const float f = grow ? __builtin_amdgcn_exp2f(m - mt) : 1.f;
+        m = grow ? mt : m;
+        l *= f;
+        // (a lane's column of O is that of its own number: the factor of a head is the
+        // same in all its columns)
+#pragma unroll
+        for (int d = 0; d < ND; d++)
+#pragma unroll
+          for (int j = 0; j < 4; j++) O[d][j] *= f;
+      }
+      const float mu = m == -INFINITY ? 0.f : m;
+      uint32_t p[NS][NP][2];
+#pragma unroll
+      for (int i = 0; i < NS; i++) {
+        float e[4];
+#pragma unroll
+        for (int j = 0; j < 4; j++) e[j] = __builtin_amdgcn_exp2f(S[i][j] - mu);
+        l += (e[0] + e[1]) + (e[2] + e[3]);
+#pragma unroll
+        for (int w = 0; w < 2; w++)
+#pragma unroll
+          for (int k = 0; k < NP; k++) {
+            p[i][k][w] = pack_bf16x2(e[2 * w], e[2 * w + 1]);
+            e[2 * w] -= __uint_as_float(p[i][k][w] << 16);
+            e[2 * w + 1] -= __uint_as_float(p[i][k][w] & 0xFFFF0000u);
+          }
+      }
+#pragma unroll
+      for (int half = 0; half < 2; half++) {
+#pragma unroll
+        for (int z = 0; z < 2; z++) {
+          const int u = 2 * half + z, r = 16 * z + cl;
+          uint4 vr[NL];
+          four_values(v4[u], vs[u], vr);
+#pragma unroll
+          for (int s = 0; s < NL; s++) {
+            const int piece = NL * g + s;
+            *(uint4*)(Vs + v_at(r, piece >> 1) + ((piece & 1) << 4 ^ (r >> 3 & 1) << 4)) = vr[s];
+          }
+        }
+        union { uint32_t w[4]; bf16x8_t v; } pb[NP];
+#pragma unroll
+        for (int k = 0; k < NP; k++)
+#pragma unroll
+          for (int z = 0; z < 2; z++)
+#pragma unroll
+            for (int w = 0; w < 2; w++) {
+              const int u = 2 * half + z;
+              pb[k].w[2 * z + w] = columns_left<W>(u % R, p[u / R][k][w]);
+            }
+#pragma unroll
+        for (int d = 0; d < ND; d++) {
+          union { s16x4_t h[2]; bf16x8_t v; } vf;
+#pragma unroll
+          for (int z = 0; z < 2; z++) {
+            const int r = 16 * z + 4 * g + (cl >> 2);
+            vf.h[z] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) s16x4_t*)(
+                    Vs + v_at(r, d) + ((cl & 3) << 3 ^ (r >> 3 & 1) << 4)));
+          }
+#pragma unroll
+          for (int k = 0; k < NP; k++)
+            O[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.v, pb[k].v, O[d], 0, 0, 0);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (!LAST) load_v();
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    int ahead = find(t0);
+    aim(t0, ahead);
+    ahead = find(min(t0 + 1, t1 - 1));
+    load_k();
+    load_v();
+    for (int t = t0; t < t1 - 1; t++) tile(t, ahead, std::false_type{});
+    tile(t1 - 1, ahead, std::true_type{});
+    if (R == 4) l += dpp_peer<0x124>(l);
+    if (R >= 2) l += dpp_peer<0x128>(l);
+    l = sum_xor32(sum_xor16(l));
+    if (cl < nq) {
+      const int64_t o = (int64_t)part * a.H + h0 + cl;
+      if (g == 0) ws.ml[o] = make_float2(m, l);
+#pragma unroll
+      for (int d = 0; d < ND; d++) *(f32x4_t*)(ws.o + o * DP + 16 * d + 4 * g) = O[d];
     }
-  }
+  };
+  paged_walk<KT, SEL>(c, a, ws, unit, range, lane, segment);
 }
 
 // The parts of every sequence joined: the first workgroups add the weights of
@@ -626,10 +947,9 @@ __device__ __forceinline__ float2 join_ml(float2 a, float2 b) {
   return make_float2(m, a.y * __builtin_amdgcn_exp2f(a.x - mu) + b.y * __builtin_amdgcn_exp2f(b.x - mu));
 }
 
-template <typename T, int DP, bool FOUR, bool SEL>
+template <typename T, int DP, int KT, bool FOUR, bool SEL>
 __global__ __launch_bounds__(1024, 8) void paged_join(CacheArgs c, PagedArgs a, PagedSpace ws,
                                                    int weights, int chunks, int wpr) {
-  constexpr int KT = tile_tokens<T, FOUR>();
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   __shared__ __attribute__((aligned(16))) float part[16][256];
   __shared__ float2 s_ml[JOIN_HEADS];
@@ -802,17 +1122,19 @@ __global__ __launch_bounds__(1024, 8) void paged_join(CacheArgs c, PagedArgs a, 
 }
 
 // Layout of the workspace; `space` null: its size alone.
+// (4 bits: large enough for tiles of either kind)
 template <typename T, bool FOUR>
-size_t paged_space(const CacheArgs& c, int H, int accumulate, char* ws, PagedSpace* space) {
-  constexpr int KT = tile_tokens<T, FOUR>();
+size_t paged_space(const CacheArgs& c, int H, int accumulate, char* ws, PagedSpace* space, int KT) {
   PagedSpace p{};
   const int group = H / c.Hkv, DP = c.dh <= 64 ? 64 : 128;
   p.qtiles = (group + 15) / 16;
   p.units = c.Hkv * p.qtiles;
   const bool split = c.B <= PAGED_SPLIT;
-  const int waves = FOUR ? FOUR_WAVES * 1024 : DP == 64 ? PAGED_WAVES_64 : PAGED_WAVES;
+  const int waves = FOUR ? 1024 * (DP == 64 ? four_waves<T, 64>() : four_waves<T, 128>())
+                         : DP == 64 ? PAGED_WAVES_64 : PAGED_WAVES;
   p.ranges = split ? std::max(1, waves / p.units) : c.B;
   p.tiles = (c.cap + KT - 1) / KT;
+  const int64_t most = FOUR ? FLAT_KT : KT;
   p.heads = std::min(group, 16);
   const size_t parts = (size_t)p.ranges + (split ? c.B : 0);
   size_t n = 0;
@@ -824,9 +1146,31 @@ size_t paged_space(const CacheArgs& c, int H, int accumulate, char* ws, PagedSpa
   p.plan = (int2*)take((size_t)c.B * 8);
   p.ml = (float2*)take(parts * H * 8);
   p.o = (float*)take(parts * H * DP * 4);
-  p.score = (float*)take(accumulate ? (size_t)c.B * p.units * p.tiles * p.heads * KT * 4 : 0);
+  p.score = (float*)take(accumulate ? (size_t)c.B * p.units * p.heads * ((c.cap + most - 1) / most * most) * 4 : 0);
   if (space) *space = p;
   return n;
+}
+
+template <typename T, int DP, bool PAD, bool SEL>
+void launch_flat(const CacheArgs& c, const PagedArgs& a, const PagedSpace& w, unsigned grid, hipStream_t s) {
+  auto with = [&](auto acc, auto r) {
+    constexpr bool ACC = decltype(acc)::value;
+    constexpr int R = decltype(r)::value;
+    paged4_flat<T, DP, PAD, ACC, SEL, R><<<grid, 256, 0, s>>>(c, a, w);
+  };
+  auto by_group = [&](auto acc) {  // (more query heads than 16 make tiles of 16)
+    if (a.group <= 4) with(acc, std::integral_constant<int, 4>{});
+    else if (a.group <= 8) with(acc, std::integral_constant<int, 2>{});
+    else with(acc, std::integral_constant<int, 1>{});
+  };
+  if constexpr (!SEL) {
+    if (a.accumulate) return by_group(std::true_type{});
+  }
+  by_group(std::false_type{});
+}
+
+template <typename T, bool FOUR> int paged_tile(const PagedArgs& a) {
+  return FOUR && a.flat ? FLAT_KT : tile_tokens<T, FOUR>();
 }
 
 template <typename T, int DP, bool PAD, bool FOUR, bool SEL>
@@ -835,6 +1179,12 @@ hipError_t launch_paged(const CacheArgs& c, const PagedArgs& a, const PagedSpace
   PagedSpace w = ws;
   if (hipError_t e = in_launches(((int64_t)ws.units * ws.ranges + 3) / 4, 256, [&](int first, unsigned grid) {
         w.block0 = first;
+        if constexpr (FOUR) {
+          if (a.flat) {
+            launch_flat<T, DP, PAD, SEL>(c, a, w, grid, s);
+            return;
+          }
+        }
         if constexpr (!SEL) {
           if (a.accumulate) {
             paged_attention<T, DP, PAD, true, FOUR, SEL><<<grid, 256, 0, s>>>(c, a, w);
@@ -854,7 +1204,13 @@ hipError_t launch_paged(const CacheArgs& c, const PagedArgs& a, const PagedSpace
   const int64_t rows = ((int64_t)c.B * a.H * wpr + 15) / 16;
   return in_launches(weights + rows, 1024, [&](int first, unsigned grid) {
     w.block0 = first;
-    paged_join<T, DP, FOUR, SEL><<<grid, 1024, 0, s>>>(c, a, w, weights, chunks, wpr);
+    if constexpr (FOUR) {
+      if (a.flat) {
+        paged_join<T, DP, FLAT_KT, FOUR, SEL><<<grid, 1024, 0, s>>>(c, a, w, weights, chunks, wpr);
+        return;
+      }
+    }
+    paged_join<T, DP, tile_tokens<T, FOUR>(), FOUR, SEL><<<grid, 1024, 0, s>>>(c, a, w, weights, chunks, wpr);
   });
 }
 

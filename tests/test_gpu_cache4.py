@@ -197,6 +197,12 @@ FOURS = [c for c in PAGED if c[3] % 32 == 0] + [
     ([300, 0, 31, 32, 33], 4, 4, 32, 27, 300, None, 0, False),
     ([90, 500], 34, 2, 32, 16, 512, 60, 2, True),
     ([2000, 64, 7], 24, 8, 96, 64, 2048, None, 0, False),
+    ([513, 5, 64, 65, 0], 16, 2, 96, 128, 600, None, 0, True),
+    ([700, 64], 40, 2, 32, 48, 720, None, 0, False),
+    ([1300, 15], 17, 1, 128, 32, 1312, None, 0, False),
+    ([1300, 130, 63], 12, 2, 128, 16, 1312, None, 0, False),
+    ([4100], 8, 8, 32, 80, 4160, None, 0, False),
+    ([3000, 1], 33, 11, 64, 16, 3008, None, 0, True),
 ]
 
 
