@@ -185,6 +185,7 @@ struct PagedSpace {
   int units, qtiles, tiles, heads;  // (heads of a unit, at most 16)
   int block0;    // number of the launch's first workgroup
   const int* sel;  // [B][Hkv][blocks]: pages of the chosen blocks, in order
+  FastDiv by_group;
 };
 // Tokens of a tile.
 template <typename T, bool FOUR> __host__ __device__ constexpr int tile_tokens() {
@@ -651,7 +652,7 @@ __global__ __launch_bounds__(256, (FOUR ? four_waves<T, DP>() : 2)) void paged_a
 // Bound by the issue of vector instructions and its waits in turn: FLAT_FIGURES.
 constexpr int FLAT_KT = 64;
 template <typename T, int DP, int R> constexpr int flat_waves() { return R < 4 && DP == 128 ? 2 : four_waves<T, DP>(); }
-template <typename T, int DP, bool PAD, bool ACC, bool SEL, int R>
+template <typename T, int DP, bool PAD, bool ACC, bool SEL, int R, bool ONE>
 __global__ __launch_bounds__(256, (flat_waves<T, DP, R>())) void paged4_flat(CacheArgs c, PagedArgs a,
                                                                         PagedSpace ws) {
   constexpr int KT = FLAT_KT, NSUB = 4, NS = NSUB / R, W = 16 / R;
@@ -709,39 +710,47 @@ __global__ __launch_bounds__(256, (flat_waves<T, DP, R>())) void paged4_flat(Cac
                            : c.table + (int64_t)b * c.max_pages;
     Four k4[NSUB], v4[NSUB];
     uint32_t ks[NSUB], vs[NSUB];
-    const uint8_t *kp[NSUB], *vp[NSUB], *ksp[NSUB], *vsp[NSUB];
+    // addresses of the sub-tiles (ONE: of the tile, which lies in one page)
+    constexpr int NA = ONE ? 1 : NSUB;
+    const uint8_t *kp[NA], *vp[NA], *ksp[NA], *vsp[NA];
     int here;  // sub-tiles whose page is there, one bit each
     // pages of the sub-tiles, in the first lanes
     auto find = [&](int t) {
-      return table[quot((uint32_t)min(t * KT + 16 * (lane & 3), limit - 1), c.page)];
+      const int x = t * KT + (ONE ? 0 : 16 * (lane & 3));
+      return table[quot((uint32_t)min(x, limit - 1), c.page)];
     };
     auto aim = [&](int t, int found) {
       here = 0;
 #pragma unroll
-      for (int u = 0; u < NSUB; u++) {
+      for (int u = 0; u < NA; u++) {
         const int x = t * KT + 16 * u, page = __builtin_amdgcn_readlane(found, u);
         const bool h = x < limit && (unsigned)page < (unsigned)c.pages;
         const uint32_t p = h ? page : 0;
         const uint32_t r = h ? x - quot((uint32_t)x, c.page) * c.page.d : 0;
-        here |= h << u;
+        here |= (ONE ? h * ((1 << NSUB) - 1) : h << u);
         kp[u] = k_base + (uint64_t)p * (uint32_t)c.k_page + (uint64_t)r * (uint32_t)c.k_row;
         vp[u] = v_base + (uint64_t)p * (uint32_t)c.v_page + (uint64_t)r * (uint32_t)c.v_row;
         ksp[u] = ks_base + (uint64_t)p * (uint32_t)c.ks_page + (uint64_t)r * (uint32_t)c.ks_row;
         vsp[u] = vs_base + (uint64_t)p * (uint32_t)c.vs_page + (uint64_t)r * (uint32_t)c.vs_row;
       }
     };
+    // (the lanes' offsets are made anew for every tile: sixteen of them kept would spill)
     auto load_k = [&]() {
+      uint32_t kl = k_lane, sl = ks_lane;
+      if (ONE) asm volatile("" : "+v"(kl), "+v"(sl));
 #pragma unroll
       for (int u = 0; u < NSUB; u++) {
-        k4[u] = *(const Four*)(kp[u] + k_lane);
-        ks[u] = ksp[u][ks_lane];
+        k4[u] = *(const Four*)(kp[u % NA] + (kl + (ONE ? 16 * u * (uint32_t)c.k_row : 0)));
+        ks[u] = ksp[u % NA][sl + (ONE ? 16 * u * (uint32_t)c.ks_row : 0)];
       }
     };
     auto load_v = [&]() {
+      uint32_t vl = v_lane, sl = vs_lane;
+      if (ONE) asm volatile("" : "+v"(vl), "+v"(sl));
 #pragma unroll
       for (int u = 0; u < NSUB; u++) {
-        v4[u] = *(const Four*)(vp[u] + v_lane);
-        vs[u] = vsp[u][vs_lane];
+        v4[u] = *(const Four*)(vp[u % NA] + (vl + (ONE ? 16 * u * (uint32_t)c.v_row : 0)));
+        vs[u] = vsp[u % NA][sl + (ONE ? 16 * u * (uint32_t)c.vs_row : 0)];
       }
     };
     float m = -INFINITY, l = 0.f;
@@ -928,9 +937,9 @@ __global__ __launch_bounds__(256, (flat_waves<T, DP, R>())) void paged4_flat(Cac
   paged_walk<KT, SEL>(c, a, ws, unit, range, lane, segment);
 }
 
-// The parts of every sequence joined: the first workgroups add the weights of
+// The parts of every sequence joined: the last workgroups add the weights of
 // 1024 visible tokens of a sequence each (4 tokens a lane, a fourth of the
-// heads a wave, summed over the waves in order), the others write the output
+// heads a wave, summed over the waves in order), the first write the output
 // rows, `wpr` waves a row.  Bound by a chain of dependent loads, so they go out
 // JOIN_AHEAD at a time, the scores before the statistics that they wait for:
 // one stream alone has hundreds of parts (two of 131,072 tokens took 37 us with
@@ -949,14 +958,14 @@ __device__ __forceinline__ float2 join_ml(float2 a, float2 b) {
 
 template <typename T, int DP, int KT, bool FOUR, bool SEL>
 __global__ __launch_bounds__(1024, 8) void paged_join(CacheArgs c, PagedArgs a, PagedSpace ws,
-                                                   int weights, int chunks, int wpr) {
+                                                   int rows, int chunks, int wpr) {
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   __shared__ __attribute__((aligned(16))) float part[16][256];
   __shared__ float2 s_ml[JOIN_HEADS];
   __shared__ __attribute__((aligned(16))) char s_odd[16];
   const int block = blockIdx.x + ws.block0;
-  if (block >= weights) {
-    const int64_t row = ((int64_t)block - weights) * (16 / wpr) + wave / wpr;
+  if (block < rows) {
+    const int64_t row = (int64_t)block * (16 / wpr) + wave / wpr;
     const bool real = row < (int64_t)c.B * a.H;
     const int b = real ? (int)(row / a.H) : 0, h = real ? (int)(row % a.H) : 0;
     const int2 plan = ws.plan[b];
@@ -1049,18 +1058,21 @@ __global__ __launch_bounds__(1024, 8) void paged_join(CacheArgs c, PagedArgs a, 
     if (real && d < c.dh) ((T*)a.out)[row * c.dh + d] = St<T>::put(o);
     return;
   }
-  const int b = block / chunks, first = block % chunks * 1024;
+  const int b = (block - rows) / chunks, first = (block - rows) % chunks * 1024;
+  // (a chain of loads, so what does not wait for another goes out at once: the plan
+  // with the lengths, the old weights with the scores)
+  const int2 plan = ws.plan[b];
   const Visible vis = visible<SEL>(c, a, b);
   if (first >= vis.nv) return;
-  const int2 plan = ws.plan[b];
-  const int h0 = wave >> 2;  // the wave's heads: h0, h0 + 4, ..
+  const int h0 = __builtin_amdgcn_readfirstlane(wave >> 2);  // the wave's heads: h0, h0 + 4, ..
+  float* old = c.weight + (int64_t)b * c.cap + vis.slot(min(first + tid, vis.nv - 1));
   // scores of 4 tokens from x on under JOIN_AHEAD of the wave's heads from h on
   auto load_scores = [&](int x, int h, f32x4_t* s) {
     const float* sp = ws.score + (int64_t)b * ws.units * ws.tiles * ws.heads * KT +
                       (int64_t)(min(x, vis.nv - 1) / KT) * ws.heads * KT + x % KT;
 #pragma unroll
     for (int u = 0; u < JOIN_AHEAD; u++) {
-      const int hu = min(h + 4 * u, a.H - 1), kh = hu / a.group, r = hu - kh * a.group;
+      const int hu = min(h + 4 * u, a.H - 1), kh = quot(hu, ws.by_group), r = hu - kh * a.group;
       s[u] = *(const f32x4_t*)(sp + ((int64_t)(kh * ws.qtiles + r / 16) * ws.tiles * ws.heads + r % 16) * KT);
     }
   };
@@ -1068,6 +1080,7 @@ __global__ __launch_bounds__(1024, 8) void paged_join(CacheArgs c, PagedArgs a, 
     const int nh = min(JOIN_HEADS, a.H - hc);
     f32x4_t s[JOIN_AHEAD];
     load_scores(first + (wave & 3) * 256 + lane * 4, hc + h0, s);
+    float weight = *old;
     __syncthreads();
     // maximum and 1 / (sum H) of the heads, 32 lanes a head
     for (int h = tid >> 5; h < nh; h += 32) {
@@ -1113,8 +1126,9 @@ __global__ __launch_bounds__(1024, 8) void paged_join(CacheArgs c, PagedArgs a, 
       const int xt = x0 + tid;
       if (xt < vis.nv && vis.by_position(c.pos + (int64_t)b * c.cap, xt, a.sinks)) {
         const int t = tid >> 8, i = tid & 255;
-        c.weight[(int64_t)b * c.cap + vis.slot(xt)] +=
-            (part[t][i] + part[4 + t][i]) + (part[8 + t][i] + part[12 + t][i]);
+        float* w = c.weight + (int64_t)b * c.cap + vis.slot(xt);
+        *w = (x0 == first ? weight : *w) +
+             ((part[t][i] + part[4 + t][i]) + (part[8 + t][i] + part[12 + t][i]));
       }
       __syncthreads();
     }
@@ -1136,6 +1150,7 @@ size_t paged_space(const CacheArgs& c, int H, int accumulate, char* ws, PagedSpa
   p.tiles = (c.cap + KT - 1) / KT;
   const int64_t most = FOUR ? FLAT_KT : KT;
   p.heads = std::min(group, 16);
+  p.by_group = fast_div((uint32_t)group);
   const size_t parts = (size_t)p.ranges + (split ? c.B : 0);
   size_t n = 0;
   auto take = [&](size_t bytes) {
@@ -1156,7 +1171,10 @@ void launch_flat(const CacheArgs& c, const PagedArgs& a, const PagedSpace& w, un
   auto with = [&](auto acc, auto r) {
     constexpr bool ACC = decltype(acc)::value;
     constexpr int R = decltype(r)::value;
-    paged4_flat<T, DP, PAD, ACC, SEL, R><<<grid, 256, 0, s>>>(c, a, w);
+    if (c.page.d % FLAT_KT == 0)
+      paged4_flat<T, DP, PAD, ACC, SEL, R, true><<<grid, 256, 0, s>>>(c, a, w);
+    else
+      paged4_flat<T, DP, PAD, ACC, SEL, R, false><<<grid, 256, 0, s>>>(c, a, w);
   };
   auto by_group = [&](auto acc) {  // (more query heads than 16 make tiles of 16)
     if (a.group <= 4) with(acc, std::integral_constant<int, 4>{});
@@ -1206,11 +1224,11 @@ hipError_t launch_paged(const CacheArgs& c, const PagedArgs& a, const PagedSpace
     w.block0 = first;
     if constexpr (FOUR) {
       if (a.flat) {
-        paged_join<T, DP, FLAT_KT, FOUR, SEL><<<grid, 1024, 0, s>>>(c, a, w, weights, chunks, wpr);
+        paged_join<T, DP, FLAT_KT, FOUR, SEL><<<grid, 1024, 0, s>>>(c, a, w, (int)rows, chunks, wpr);
         return;
       }
     }
-    paged_join<T, DP, tile_tokens<T, FOUR>(), FOUR, SEL><<<grid, 1024, 0, s>>>(c, a, w, weights, chunks, wpr);
+    paged_join<T, DP, tile_tokens<T, FOUR>(), FOUR, SEL><<<grid, 1024, 0, s>>>(c, a, w, (int)rows, chunks, wpr);
   });
 }
 
