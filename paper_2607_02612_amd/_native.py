@@ -72,6 +72,7 @@ class FusionScales(ctypes.Structure):
 
 
 class FusionRotaryRows(ctypes.Structure):
+    """(The binding of every call packs it in one step.)"""
     _fields_ = [("q", c_void_p), ("k", c_void_p), ("v", c_void_p), ("q_strides", c_int64 * 2),
                 ("k_strides", c_int64 * 2), ("v_strides", c_int64 * 2), ("q_out", c_void_p),
                 ("k_out", c_void_p), ("freq", c_void_p), ("drop", c_void_p), ("heads", c_int32),
@@ -143,8 +144,8 @@ SIGNATURES = [
     ("fusion_cache_evict_workspace_bytes", c_size_t, [POINTER(FusionCache), c_int]),
     ("fusion_cache_evict", c_int, [POINTER(FusionCache), c_int, c_int, c_int, c_void_p,
                                    c_void_p, c_size_t, c_void_p]),
-    ("fusion_cache_append_rotary", c_int, [POINTER(FusionCache), POINTER(FusionScales),
-                                           POINTER(FusionRotaryRows), c_void_p, c_void_p]),
+    ("fusion_cache_append_rotary", c_int, [POINTER(FusionCache), POINTER(FusionScales), c_void_p,
+                                           c_void_p, c_void_p]),
     ("fusion_cache4_attention_workspace_bytes", c_size_t, [POINTER(FusionCache),
                                                            POINTER(FusionScales), c_int, c_int]),
     ("fusion_cache4_attention", c_int, [POINTER(FusionCache), POINTER(FusionScales), c_void_p,

@@ -454,7 +454,7 @@ hipError_t launch_page_bounds(const CacheArgs& c, const BoundsArgs& a, hipStream
   int64_t touched = c.max_pages;
   if (a.newest) touched = std::min<int64_t>(touched, ((int64_t)a.newest - 2 + ps) / ps + 1);
   const unsigned x = std::min(chunks, 256), z = std::min(c.B, 1024);
-  const dim3 grid(x, (unsigned)std::min<int64_t>(touched, std::max(1u, STRIDE_BLOCKS / (x * z))), z);
+  const dim3 grid(x, (unsigned)std::min<int64_t>(touched, std::min(65535u, STRIDE_BLOCKS / (x * z))), z);
   if (c.ks)
     page_bounds<T, true><<<grid, 256, 0, s>>>(c, a, pieces, (int)touched, chunks);
   else

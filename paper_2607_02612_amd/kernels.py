@@ -19,6 +19,7 @@ compute no gradients.
 from __future__ import annotations
 
 import ctypes
+import struct
 from ctypes import byref, c_double, c_float
 
 import numpy as np
@@ -26,8 +27,7 @@ import torch
 from torch.autograd import forward_ad
 
 from . import _native
-from ._native import (FusionCache, FusionPackedOut, FusionRagged, FusionRotaryRows, FusionScales,
-                      check)
+from ._native import FusionCache, FusionPackedOut, FusionRagged, FusionScales, check
 
 EPI = {"store": 0, "gelu": 1, "resid": 2, "f32": 3}
 
@@ -286,6 +286,7 @@ _LAST = (1 << 31) - 1  # position
 
 
 _Strides2, _Strides4, _Strides6 = (ctypes.c_int64 * n for n in (2, 4, 6))
+_rotary_rows = struct.Struct("13q3i4x").pack  # fusion_rotary_rows
 
 
 def _out(out, rows, heads, dh, like):
@@ -366,7 +367,7 @@ class TokenCache:
     too, in stream order.  Pages that a call writes must not be shared."""
 
     # entry points that take the cache, and what follows it in their arguments
-    _attention, _evict = "fusion_paged_attention", "fusion_cache_evict"
+    _names = "fusion_paged_attention", "fusion_cache_evict"
     _scales, _more = None, ()
 
     def __init__(self, k, v, table, length, seen, weight, pos):
@@ -375,7 +376,7 @@ class TokenCache:
                              "kv_heads, dh]")
         self._pages(k, v)
         self._take((k, v, table, length, seen, weight, pos), k.dtype, k.shape[3])
-        self._bytes(self._evict, 1)  # the library's checks
+        self._bytes(self._names[1], 1)  # the library's checks
 
     @staticmethod
     def _pages(k, v):
@@ -418,6 +419,7 @@ class TokenCache:
                               weight.data_ptr(), pos.data_ptr(), _PREC[dtype], batch, pages,
                               page_size, max_pages, kv_heads, dh)
         self._ref = byref(self._c)
+        self._attend, self._evict = (getattr(_native.lib(), name) for name in self._names)
         self._space, self._streams = {}, set()
         self.batch, self.kv_heads, self.dh, self.dtype = batch, kv_heads, dh, dtype
         self.capacity, self.device = max_pages * page_size, k.device
@@ -480,7 +482,7 @@ class TokenCache4(TokenCache):
     cache_append_rotary, paged_attention, cache_evict, PageBounds and
     block_attention take it as they take a TokenCache; rows are rounded to 4
     bits when they are appended."""
-    _attention, _evict = "fusion_cache4_attention", "fusion_cache4_evict"
+    _names = "fusion_cache4_attention", "fusion_cache4_evict"
 
     def __init__(self, k, v, k_scale, v_scale, table, length, seen, weight, pos,
                  dtype=torch.bfloat16):
@@ -502,7 +504,7 @@ class TokenCache4(TokenCache):
                                v_scale.stride()[:3])
         self._scales = byref(self._s)
         self._more = (self._scales,)
-        self._bytes(self._evict, 1)  # the library's checks
+        self._bytes(self._names[1], 1)  # the library's checks
 
     @classmethod
     def empty(cls, batch, capacity, kv_heads, dh, page_size=64, dtype=torch.bfloat16):
@@ -540,8 +542,8 @@ def cache_append(cache, k, v, cu=None):
     if v.shape[0] != rows or (rows != cache.batch if cu is None else rows < cu_h[-1]):
         raise ValueError("rows do not match the sequences")
     if cache._scales is not None:
-        rows = FusionRotaryRows(None, kp, vp, (0, 0), (k_row, k_head), (v_row, v_head))
-        check(_native.lib().fusion_cache_append_rotary(cache._ref, cache._scales, byref(rows), cu_p,
+        r = _rotary_rows(0, kp, vp, 0, 0, k_row, k_head, v_row, v_head, 0, 0, 0, 0, 0, 0, 0)
+        check(_native.lib().fusion_cache_append_rotary(cache._ref, cache._scales, r, cu_p,
                                                        cache._ready(k, v)))
         return
     check(_native.lib().fusion_cache_append(cache._ref, kp, vp,
@@ -566,8 +568,8 @@ def paged_attention(q, cache, window=None, sinks=0, accumulate=True, out=None):
     out = _out(out, cache.batch, heads, cache.dh, q)
     acc = 1 if accumulate else 0
     stream = cache._ready(q, None if fresh else out)
-    ws, n = cache._workspace(cache._attention, heads, acc)
-    check(getattr(_native.lib(), cache._attention)(
+    ws, n = cache._workspace(cache._names[0], heads, acc)
+    check(cache._attend(
         cache._ref, *cache._more, qp, _Strides2(q_row, q_head), heads, window,
         _count(sinks, "sinks", 0, _LAST), acc,
         out.data_ptr(), ws.data_ptr(), n, stream))
@@ -588,10 +590,10 @@ def cache_evict(cache, budget, sinks=0, recent=0):
     if sinks + recent > budget:
         raise ValueError("sinks and recent do not fit the budget")
     stream = cache._ready()
-    ws, n = cache._workspace(cache._evict, budget)
+    ws, n = cache._workspace(cache._names[1], budget)
     src = cache.table.new_empty((cache.batch, budget))
-    check(getattr(_native.lib(), cache._evict)(cache._ref, *cache._more, budget, sinks, recent,
-                                               src.data_ptr(), ws.data_ptr(), n, stream))
+    check(cache._evict(cache._ref, *cache._more, budget, sinks, recent, src.data_ptr(),
+                       ws.data_ptr(), n, stream))
     return src
 
 
@@ -617,7 +619,8 @@ def cache_append_rotary(cache, q, k, v, freq, cu=None, interleaved=False, drop=N
     vp, v_row, v_head = _heads(v, "v", cache.dtype, cache.kv_heads, dh)
     _need(freq, "freq", torch.float32)
     _no_grad(freq, "freq")
-    if freq.dim() != 1 or freq.shape[0] % 4 or 2 * freq.shape[0] > dh:
+    half = freq.shape[0] if freq.dim() == 1 else -1
+    if half < 0 or half % 4 or 2 * half > dh:
         raise ValueError("freq must hold a multiple of 4 frequencies, for no more dims than a head has")
     if drop is not None:
         _need(drop, "drop", torch.int32)
@@ -639,11 +642,11 @@ def cache_append_rotary(cache, q, k, v, freq, cu=None, interleaved=False, drop=N
         for t in (out if fresh else None, keys):
             if t is not None:
                 t[max(used, 0):].zero_()
-    r = FusionRotaryRows(qp, kp, vp, (q_row, q_head), (k_row, k_head), (v_row, v_head), out.data_ptr(),
-                         _ptr(keys), freq.data_ptr() or None, _ptr(drop), heads, freq.shape[0],
-                         1 if interleaved else 0)
+    r = _rotary_rows(qp, kp, vp, q_row, q_head, k_row, k_head, v_row, v_head, out.data_ptr(),
+                     0 if keys is None else keys.data_ptr(), freq.data_ptr(),
+                     0 if drop is None else drop.data_ptr(), heads, half, 1 if interleaved else 0)
     check(_native.lib().fusion_cache_append_rotary(
-        cache._ref, cache._scales, byref(r), cu_p,
+        cache._ref, cache._scales, r, cu_p,
         cache._ready(q, k, v, freq, drop, None if fresh else out)))
     return out, keys
 

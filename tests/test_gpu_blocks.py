@@ -112,6 +112,22 @@ def test_bounds(torch_cuda, bits, hkv, dh, page):
         assert np.array_equal(_np(b.lo), lo) and np.array_equal(_np(b.hi), hi), newest
 
 
+def test_bounds_of_more_pages_than_a_launch_has_rows(torch_cuda):
+    """70,000 pages of one token: bounds are the keys."""
+    torch = torch_cuda
+    rng = np.random.default_rng(3)
+    c = _cache(torch, rng, "bf16", [70000], 1, 16, 1, 70000)
+    b = _kern().PageBounds(c)
+    t = c.table[0].long()
+    assert torch.equal(b.lo[t], c.k[t, 0]) and torch.equal(b.hi[t], c.k[t, 0])
+    q = _normal(torch, rng, "bf16", 1, 2, 16)
+    got, chosen = _kern().block_attention(q, c, b, 1000, 3, 7)
+    want = choose_ref(_np(q), c, _np(b.lo), _np(b.hi), 1000, 3, 7)
+    assert np.array_equal(chosen.cpu().numpy(), want)
+    out, tol, _, _ = paged_ref(_np(q), c, None, 0, "bf16", want)
+    _close(_np(got), out, tol)
+
+
 BLOCKS = [  # lengths, heads, kv_heads, dh, page, capacity, blocks, first, recent
     ([1], 1, 1, 32, 16, 16, 1, 0, 1),
     ([300, 0, 17, 16, 1], 6, 6, 64, 16, 300, 4, 1, 1),
