@@ -565,7 +565,9 @@ FUSION_API int fusion_cache4_evict(const fusion_cache* c, const fusion_cache_sca
  * cache's precision, contiguous, receive the least and the greatest value of each
  * dim over the tokens of each page that a sequence holds (NaN has no part in
  * them), of the pages that hold its last `newest` slots or, with newest = 0, of all.
- * Other pages' bounds stay as they are.  Errors: FUSION_E_INVALID_ARG, FUSION_E_HIP. */
+ * Other pages' bounds stay as they are.  Of a page that sequences share each should
+ * hold all of it: its bounds are by what one of them, any one, holds.
+ * Errors: FUSION_E_INVALID_ARG, FUSION_E_HIP. */
 FUSION_API int fusion_page_bounds(const fusion_cache* c, const fusion_cache_scales* sc, void* lo,
                                   void* hi, int newest, void* stream);
 

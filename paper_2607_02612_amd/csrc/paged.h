@@ -244,8 +244,9 @@ __device__ __forceinline__ void paged_walk(const CacheArgs& c, const PagedArgs& 
   const bool split = c.B <= PAGED_SPLIT;
   const int b0 = split ? 0 : range, b1 = split ? c.B : range + 1;
   auto tiles_of = [&](int b) { return b < b1 ? (visible<SEL>(c, a, b).nv + KT - 1) / KT : 0; };
-  int total = 0;
-  for (int b = b0; b < b1; b += 64)
+  const int head = tiles_of(b0 + lane);  // of the first 64 sequences, kept
+  int total = __builtin_amdgcn_readfirstlane(wave_sum_i(head));
+  for (int b = b0 + 64; b < b1; b += 64)
     total += __builtin_amdgcn_readfirstlane(wave_sum_i(tiles_of(b + lane)));
   const int per = max(1, split ? (total + ws.ranges - 1) / ws.ranges : total);
   const int first = split ? range * per : 0, last = min(first + per, total);
@@ -253,12 +254,8 @@ __device__ __forceinline__ void paged_walk(const CacheArgs& c, const PagedArgs& 
   if (first >= total && !planner) return;
   int before = 0;  // tiles of the sequences before b
   for (int b = b0; b < b1 && (before < last || planner); b += 64) {
-    const int t = tiles_of(b + lane);
-    int p = t;  // inclusive, then exclusive sum over the lanes
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(p, o, 64);
-      if (lane >= o) p += v;
-    }
+    const int t = b == b0 ? head : tiles_of(b + lane);
+    int p = wave_scan(t);  // inclusive, then exclusive sum over the lanes
     const int sum = __builtin_amdgcn_readlane(p, 63);
     p += before - t;
     before += sum;

@@ -71,16 +71,16 @@ __device__ __forceinline__ void widen(uint4 u, float* x) {
   x[2] = __uint_as_float(u.z); x[3] = __uint_as_float(u.w);
 }
 
-// The piece's eight values, turned (turns: the row's angles).
-template <typename T, typename R>
+// The piece's eight values, turned in type C (turns: the row's angles).
+template <typename C, typename T, typename R>
 __device__ __forceinline__ void turn8(const RotaryArgs& a, const Piece<T>& p, int d, const Turn<R>* turns,
                                       float* x) {
   if (d >= 2 * a.half) return;
   if (a.pairs) {
 #pragma unroll
     for (int i = 0; i < 4; i++) {
-      const Turn<R> t = turns[d / 2 + i];
-      const R u = x[2 * i], v = x[2 * i + 1];
+      const Turn<C> t{(C)turns[d / 2 + i].c, (C)turns[d / 2 + i].s};
+      const C u = x[2 * i], v = x[2 * i + 1];
       x[2 * i] = (float)fma(u, t.c, -(v * t.s));
       x[2 * i + 1] = (float)fma(v, t.c, u * t.s);
     }
@@ -96,8 +96,8 @@ __device__ __forceinline__ void turn8(const RotaryArgs& a, const Piece<T>& p, in
     widen(p.y[h], y);
 #pragma unroll
     for (int i = 0; i < 4; i++) {
-      const Turn<R> t = turns[j + i];
-      const R u = x[4 * h + i], v = y[i], s = second ? t.s : -t.s;
+      const Turn<C> t{(C)turns[j + i].c, (C)turns[j + i].s};
+      const C u = x[4 * h + i], v = y[i], s = second ? t.s : -t.s;
       x[4 * h + i] = (float)fma(u, t.c, v * s);
     }
   }
@@ -169,13 +169,14 @@ __device__ __forceinline__ void store_task(const CacheArgs& c, const RotaryArgs&
   float x[8];
   widen(k.p.x[0], x);
   widen(k.p.x[1], x + 4);
-  if (value < 0) turn8(a, k.p, d, turns, x);
   if (key < 0) {
+    turn8<float>(a, k.p, d, turns, x);
     store8((T*)a.q_out + (r * a.H + k.vec) * c.dh + d, x);
     return;
   }
   const int h = value < 0 ? key : value;
   if (value < 0) {
+    turn8<R>(a, k.p, d, turns, x);
     if (sizeof(T) == 2 && FOUR)
 #pragma unroll
       for (int i = 0; i < 8; i++) x[i] = bf16_to_f32(f32_to_bf16(x[i]));

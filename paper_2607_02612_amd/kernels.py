@@ -656,7 +656,8 @@ class PageBounds:
     a cache, by which block_attention chooses pages: lo, hi [pages, kv_heads, dh]
     of the cache's dtype.  Made for what the cache holds, or from given tensors
     as they are.  update() brings them up to date: after the cache has changed
-    and before block_attention."""
+    and before block_attention.  A page that sequences share is bounded by what
+    one of them holds of it, so each should hold all of it."""
 
     def __init__(self, cache, lo=None, hi=None):
         shape = (cache.k.shape[0], cache.kv_heads, cache.dh)

@@ -139,6 +139,10 @@ BLOCKS = [  # lengths, heads, kv_heads, dh, page, capacity, blocks, first, recen
     ([9000, 8999], 4, 2, 32, 4, 9000, 257, 1, 1),
     ([600, 20], 3, 3, 128, 200, 600, 2, 1, 1),
     ([130, 77], 2, 2, 64, 16, 160, 50, 1, 1),
+    ([1500, 40], 40, 1, 64, 16, 1504, 12, 1, 2),
+    ([1500, 1499, 16], 16, 2, 128, 64, 1536, 6, 1, 1),
+    ([900, 33], 20, 4, 96, 48, 912, 7, 0, 2),
+    ([5000, 129, 64], 4, 1, 128, 64, 5056, 30, 1, 1),
 ]
 
 
