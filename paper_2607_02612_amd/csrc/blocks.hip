@@ -308,8 +308,8 @@ __global__ __launch_bounds__(256) void block_choose_few(CacheArgs c, BlockArgs a
 // One workgroup per sequence and key head: the blocks-th largest key from the
 // top by digits of 12, 10 and 10 bits (counts in LDS), then the chosen pages in
 // order; bound by its barriers, 9.0 us for 16 choices among up to 2,048 pages (17.8
-// with 256 threads that read the scores again in every round).  The threads hold CHOOSE_PAGES keys, 1024 apart; more are read again in
-// every round.
+// with 256 threads that read the scores again in every round).  The threads hold
+// CHOOSE_PAGES keys, 1024 apart; more are read again in every round.
 constexpr int CHOOSE_E = 4, CHOOSE_PAGES = 1024 * CHOOSE_E;
 __global__ __launch_bounds__(1024) void block_choose(CacheArgs c, BlockArgs a, const uint32_t* keys, int* sel) {
   __shared__ int bins[4096 + 2048], s_found[2], s_wave[16], s_count[16][2];
@@ -345,7 +345,7 @@ __global__ __launch_bounds__(1024) void block_choose(CacheArgs c, BlockArgs a, c
     int want = blocks;   // and the first `want` of those equal to it
     for (int round = 0; round < 3; round++) {
       const int shift = round == 0 ? 20 : round == 1 ? 10 : 0, nb = round ? 1024 : 4096;
-      int* bin = bins + (round == 0 ? 0 : 3072 + 1024 * round);
+      int* bin = bins + (round == 0 ? 0 : 4096 + 1024 * (round - 1));
       for (int ch = 0; ch < chunks; ch++) {
         if (chunks > 1 && (ch || round)) load(ch);
 #pragma unroll

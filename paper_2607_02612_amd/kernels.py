@@ -300,6 +300,16 @@ def _out(out, rows, heads, dh, like):
     return out
 
 
+def _beside(out, *inputs):
+    """A tensor that is written and the span of each other one, from its first
+    element to its last, have no memory in common."""
+    for t in inputs:
+        last = sum((n - 1) * s for n, s in zip(t.shape, t.stride())) if t.numel() else -1
+        if (t.data_ptr() < out.data_ptr() + out.nbytes
+                and out.data_ptr() < t.data_ptr() + (last + 1) * t.element_size()):
+            raise ValueError("tensors that are written must not overlap the others")
+
+
 def window_attention(q, k, v, cu, window=None, sinks=0, causal=True, size=None, out=None):
     """Attention of packed rows: row i of a sample sees its rows j <= i with
     i - j < window or j < sinks; with causal=False those with |i - j| < window
@@ -637,6 +647,8 @@ def cache_append_rotary(cache, q, k, v, freq, cu=None, interleaved=False, drop=N
         raise ValueError("rows do not match the sequences")
     fresh = out is None
     out = _out(out, rows, heads, dh, q)
+    if not fresh:
+        _beside(out, q, k, v)
     keys = k.new_empty((rows, cache.kv_heads, dh)) if rotated_k else None
     if used < rows:
         for t in (out if fresh else None, keys):
@@ -671,6 +683,7 @@ class PageBounds:
                 raise ValueError("bounds are written in place and have no gradients")
             if tuple(t.shape) != shape or t.device != cache.device or t.data_ptr() % 16:
                 raise ValueError(f"{name} must be a 16-byte aligned tensor {list(shape)} on the cache's GPU")
+        _beside(lo, hi, cache.k, cache.v)
         self.lo, self.hi, self._streams = lo, hi, set()
         if not given:
             self.update()
@@ -698,9 +711,9 @@ def block_attention(q, cache, bounds, blocks, first=0, recent=1, out=None):
     others those whose keys can score highest by their bounds with one of the key
     head's queries (equal ones: the lower page).  Sequences of no more pages
     are attended whole.  Weights stay as they are.  bounds: PageBounds of the
-    cache, up to date.  Returns (out like q, contiguous; chosen int32 [batch,
-    kv_heads, blocks], the pages by their place in the sequence, ascending, then
-    -1)."""
+    cache, up to date.  Returns (out like q, contiguous, a given one apart from
+    the inputs; chosen int32 [batch, kv_heads, blocks], the pages by their place in
+    the sequence, ascending, then -1)."""
     if not isinstance(q, torch.Tensor) or q.dim() != 3 or q.shape[0] != cache.batch:
         raise ValueError("q must be a tensor [batch, heads, dh]")
     heads = q.shape[1]
@@ -716,6 +729,8 @@ def block_attention(q, cache, bounds, blocks, first=0, recent=1, out=None):
     _here(q)
     fresh = out is None
     out = _out(out, cache.batch, heads, cache.dh, q)
+    if not fresh:
+        _beside(out, q, cache.k, cache.v, bounds.lo, bounds.hi)
     stream = bounds._ready(q, None if fresh else out)
     key = ("fusion_block_attention", heads, blocks)
     n = cache._space.get(key)

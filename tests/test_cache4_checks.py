@@ -143,3 +143,11 @@ def test_binding_refuses_what_is_no_count(v):
             kernels.block_attention(t, fake, bounds, *args)
     with pytest.raises(ValueError):
         bounds.update(v)
+
+
+def test_what_is_written_lies_apart():
+    t = torch.zeros(100)
+    kernels._beside(t[10:20], t[:10], t[20:], t[20:].view(8, 10)[:, ::2], t[:0], t[15:15])
+    for other in (t[19:], t[:11], t, t[15:16], t.view(10, 10)[:3, 0], t[12:14].expand(3, 2)):
+        with pytest.raises(ValueError):
+            kernels._beside(t[10:20], other)

@@ -384,6 +384,8 @@ def test_refusals(torch_cuda):
         lambda: kern.block_attention(q, c, b, 2.5), lambda: kern.block_attention(q, c, b, (1 << 30) + 1),
         lambda: kern.block_attention(q[:1], c, b, 2), lambda: kern.block_attention(q.float(), c, b, 2),
         lambda: kern.block_attention(q, c, b, 2, out=q[:, :2]),
+        lambda: kern.block_attention(q, c, b, 2, out=q), lambda: kern.PageBounds(c, lo, lo),
+        lambda: kern.block_attention(q, c, b, 2, out=lo.view(-1)[:512].view(2, 4, 64)),
         lambda: kern.block_attention(q.clone().requires_grad_(), c, b, 2),
     ]:
         with pytest.raises(ValueError):

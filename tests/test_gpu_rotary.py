@@ -11,7 +11,7 @@ import numpy as np
 import pytest
 
 from test_gpu_cache import U32, UNIT, _cache, _dt, _kern, _normal, _np, _paged_ref, _close, torch_cuda  # noqa: F401
-from test_gpu_cache4 import cache4, held, paged_ref, quantise
+from test_gpu_cache4 import cache4, paged_ref, quantise
 
 pytestmark = pytest.mark.gpu
 
@@ -288,5 +288,13 @@ def test_refusals(torch_cuda):
             bad()
     with pytest.raises(kern._native.FusionError):
         call(c, q, k, k, f, [0, 2, 1])
+    # in place, and behind the keys by one row of eight values
+    both = n(2 * 4 * 64 + 2 * 2 * 64)
+    queries, keys = both[256:768].view(2, 4, 64), both[:256].view(2, 2, 64)
+    for out, key in ((queries, keys), (both[8:520].view(2, 4, 64), keys), (both[:512].view(2, 4, 64), k)):
+        with pytest.raises(ValueError):
+            call(c, queries, key, k, f, out=out)
+        with pytest.raises(ValueError):
+            call(c, q, k, keys, f, out=both[248:760].view(2, 4, 64))
     assert all(torch.equal(a, b) for a, b in zip(c._tensors, state))
-    assert held is not None
+    call(c, q, k, keys, f, out=queries)  # beside the values, without a gap
