@@ -653,11 +653,12 @@ __global__ __launch_bounds__(256, (FOUR ? four_waves<T, DP>() : 2)) void paged_a
 // on, values while the next scores are; the halves of a tile's values share the LDS.
 //
 // 64 sequences of up to 8,192 tokens, 32 bf16 heads of 128 over 8 (290 MB of cache, 33 of
-// scores): 71 us, 4.6 TB/s, by paged_attention 90; 63 if the cache comes from the last
-// level, 52 without scores; with every tile read from L2 54 and 47, of which 14 are the
-// product with the values: memory and the issue of instructions bound it together
-// (vector instructions 19 us, matrix 10, LDS 29, a third of the cycles wait for
-// memory).  Scores written past the caches gain nothing.
+// scores): 69 us, 4.7 TB/s, by paged_attention 90.  When it took 71: 63 if the cache
+// came from the last level, 52 without scores; with every tile read from L2 54 and 47,
+// of which 14 were the product with the values.  Memory and the issue of instructions
+// bound it together: vector instructions 19 us, matrix 10, LDS 28; a quarter of the
+// waves' cycles wait for memory, half for issue.  Scores written past the caches gain
+// nothing.
 constexpr int FLAT_KT = 64;
 template <typename T, int DP, int R> constexpr int flat_waves() { return R < 4 && DP == 128 ? 2 : four_waves<T, DP>(); }
 template <typename T, int DP, bool PAD, bool ACC, bool SEL, int R, bool ONE>
