@@ -708,7 +708,7 @@ FUSION_API int fusion_cache_append_rotary(const fusion_cache* c, const fusion_ca
   if (int rc = check_cache(c, &ca, sc)) return rc;
   if (!r) return bad("rows are null");
   if (r->heads < 0 || r->heads > 4096) return bad("heads must be in 0 .. 4096");
-  if (r->half < 0 || r->half % 4 || 2 * r->half > c->dh)
+  if (r->half < 0 || r->half % 4 || r->half > c->dh / 2)
     return bad("the frequencies must be a multiple of 4, for no more dims than a head has");
   if (r->half > 0 && !r->freq) return bad("null frequencies");
   if (r->interleaved != 0 && r->interleaved != 1) return bad("interleaved must be 0 or 1");

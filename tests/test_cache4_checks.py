@@ -77,7 +77,8 @@ def test_four_bits_need_scales_and_whole_blocks():
 
 @pytest.mark.parametrize("bad", [
     dict(q=None), dict(k=None), dict(v=None), dict(q_out=None), dict(freq=None), dict(heads=-1),
-    dict(heads=4097), dict(half=-4), dict(half=30), dict(half=36), dict(interleaved=2), dict(q=P + 8),
+    dict(heads=4097), dict(half=-4), dict(half=30), dict(half=36), dict(half=1 << 30),
+    dict(half=3 << 29), dict(half=2**31 - 4), dict(interleaved=2), dict(q=P + 8),
     dict(k=P + 4), dict(q_out=P + 2), dict(k_out=P + 8), dict(q_strides=(256, 60)),
     dict(k_strides=(-128, 64)), dict(v_strides=(128, 65))])
 def test_append_rotary_refuses(bad):
