@@ -222,3 +222,52 @@ def test_scores_that_grow_along_a_sequence(torch_cuda, group, hkv, dh, page, dty
     top = (s / math.sqrt(dh) / math.log(2)).view(hkv, group, 9, 64).amax(-1).cummax(-1).values
     assert float(((top[..., 1:] - top[..., :-1] > 8).sum(-1) >= 2).double().mean()) > 0.5
     check(torch, c, q, dtype)
+
+
+FAR = [  # page and row strides of codes and of scales: at the last that the tiles of 64 take, and past it
+    ((1 << 32) - 16, 64, 1 << 20, 4), (1 << 32, 64, 1 << 20, 4),
+    (1 << 20, 64, (1 << 32) - 1, 4), (1 << 20, 64, 1 << 32, 4), (1 << 20, 64, (1 << 32) + 5, 4),
+    (1 << 32, (1 << 26) - 16, 1 << 20, 4), (1 << 32, 1 << 26, 1 << 20, 4),
+    ((1 << 32) - 16, (1 << 26) - 16, 1 << 20, 4), ((1 << 32) - 16, 1 << 26, 1 << 20, 4),
+    (1 << 20, 64, (1 << 32) - 1, (1 << 26) - 1), (1 << 20, 64, (1 << 32) - 1, 1 << 26),
+    (1 << 20, 64, (1 << 32) - 1, (1 << 26) + 3),
+]
+
+
+@pytest.mark.parametrize("part", ["k", "v"])
+@pytest.mark.parametrize("page,row,scale_page,scale_row", FAR)
+def test_strides_at_the_limits_of_the_tiles(torch_cuda, page, row, scale_page, scale_row, part):
+    """Strides on both sides of those that tiles of 64 tokens hold in 32 bits, of the
+    keys' codes and scales or of the values', give what a compact cache gives."""
+    torch = torch_cuda
+    print(f"[parts] strides {part} {page:#x} {row:#x} {scale_page:#x} {scale_row:#x}", flush=True)
+    places = 64  # (a page's places by row strides of 2^26: 4 GiB)
+    c, g = make(torch, 9, "bf16", [128, 70], 2, 64, places)
+    q = torch.randn((2, 8, 64), generator=g, device="cuda").to(c.dtype)
+    far, big = [], None
+    for i, t in enumerate((c.k, c.v, c.k_scale, c.v_scale)):
+        w, mine = t.shape[3], i % 2 == "kv".index(part)
+        st = (scale_page, scale_row) if i > 1 else (page, row)
+        if not mine or st in ((1 << 20, 64), (1 << 20, 4)):
+            far.append(t)
+            continue
+        st = (*st, w, 1)
+        big = torch.empty(1 + sum((n - 1) * s for n, s in zip(t.shape, st)), dtype=torch.uint8, device="cuda")
+        far.append(big.as_strided(t.shape, st))
+        far[-1].copy_(t)
+    kern = _kern()
+    f = kern.TokenCache4(*far, c.table, c.length.clone(), c.seen.clone(), c.weight.clone(), c.pos.clone())
+    out, tol, add, add_tol = reference(torch, q, c, "bf16")
+    close(torch, kern.paged_attention(q, f), out, tol, "out")
+    off = (f.weight.double() - c.weight.double() - add).abs() - (add_tol + U32 * (c.weight.double() + add))
+    assert float(off.max()) <= 0
+    got, chosen = kern.block_attention(q, f, kern.PageBounds(f), 1)
+    assert torch.equal(chosen[:, :, 0], torch.tensor([[1, 1], [1, 1]], device="cuda"))
+    out, tol, _, _ = reference(torch, q, c, "bf16", chosen=chosen)
+    close(torch, got, out, tol, "out")
+    new = [torch.randn((1, 2, 64), generator=g, device="cuda").to(c.dtype) for _ in "kv"]
+    for x in (f, c):
+        kern.cache_append(x, *new, [0, 0, 1])
+    assert all(torch.equal(a, b) for a, b in zip((f.k, f.v, f.k_scale, f.v_scale), c._tensors[:2] + c._tensors[7:]))
+    del f, far, big
+    torch.cuda.empty_cache()  # (the memory of one case at a time)
