@@ -537,7 +537,8 @@ typedef struct fusion_rotary_rows {
  * p the position of a row's token and t_j = p freq[j], a product in 64 bits, the
  * dims (x, y) = (j, j + half), or (2j, 2j + 1) with interleaved = 1, become
  * (x cos t_j - y sin t_j, y cos t_j + x sin t_j); dims from 2 half on stay (half:
- * a multiple of 4, 2 half <= dh; 0: nothing turns).  drop: so many of each
+ * a multiple of 4, 2 half <= dh; 0: nothing turns).  Past 2^50 radians, where 64
+ * bits hold no better than a quarter of one, a pair turns by whole quarters.  drop: so many of each
  * sequence's newest tokens (read as 0 .. len) leave before, with len and seen:
  * tokens drafted and not kept, for instance.  They must lie in its last slots,
  * where an append puts them and an eviction may not have left them.  Rows past

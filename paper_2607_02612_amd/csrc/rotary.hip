@@ -22,7 +22,7 @@ template <typename R> struct Turn {
   R c, s;
 };
 
-// The angle less the nearest multiple k of pi / 2 (pi / 2 as a sum of two numbers),
+// The angle, up to 2^50, less the nearest multiple k of pi / 2 (pi / 2 as a sum of two numbers),
 // then the series of sine and cosine, whose first terms left out are below 2^-54 of
 // the result at pi / 4; k tells which of the two, and its sign.  (A general sincos
 // carries the reduction of any angle, at the cost of half the registers.)
@@ -30,9 +30,15 @@ constexpr double kHalfPi = 1.570796326794896619;           // nearest to pi / 2
 constexpr double kHalfPiRest = 6.123233995736766036e-17;   // pi / 2 - kHalfPi
 template <typename R>
 __device__ __forceinline__ Turn<R> turn_of(double angle) {
-  const double k = rint(angle * (1.0 / kHalfPi));
+  double k = rint(angle * (1.0 / kHalfPi));
   double r = fma(-k, kHalfPiRest, fma(-k, kHalfPi, angle));
-  r = fabs(r) <= 0.8 ? r : r * 0.0;  // (beyond 2^50 an angle of 64 bits holds no part of a turn)
+  // (the rounding of that quotient leaves up to 1.2 at 2^50: a second step, exact, brings it
+  // within pi / 4)
+  const double more = rint(r * (1.0 / kHalfPi));
+  r = fma(-more, kHalfPiRest, fma(-more, kHalfPi, r));
+  k += more;
+  // (past 2^50 an angle of 64 bits holds no better than a quarter radian: whole quarters)
+  r = fabs(angle) <= 0x1p50 ? r : r * 0.0;
   const double z = r * r;
   double s = 1.0 / 355687428096000.0, c = 1.0 / 20922789888000.0;  // 17!, 16!
   s = fma(s, z, -1.0 / 1307674368000.0);

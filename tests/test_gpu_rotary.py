@@ -136,6 +136,35 @@ def test_far_positions(torch_cuda, bits):
     near(got_k, *turn(_np(k), np.array(seen), freq, False), dtype)
 
 
+@pytest.mark.parametrize("bits", ["fp32", "bf16/4"])
+def test_steep_frequencies(torch_cuda, bits):
+    """Angles of up to 2^50 radians are reduced as well as small ones; past it each pair
+    turns by whole quarters, and infinite or NaN frequencies give NaN."""
+    torch = torch_cuda
+    dtype, four = bits.split("/")[0], "/" in bits
+    rng = np.random.default_rng(46)
+    seen = rng.integers(1 << 30, (1 << 31) - 1, size=96)
+    make = cache4 if four else _cache
+    freq = (rng.uniform(1, 2, 32) * 2.0 ** np.repeat(np.arange(11, 19), 4)).astype(np.float32)
+    freq[31] = 2.0 ** 19
+    q, k = _normal(torch, rng, dtype, 96, 3, 64), _normal(torch, rng, dtype, 96, 1, 64)
+    call = lambda f: _kern().cache_append_rotary(make(torch, rng, dtype, [0] * 96, 1, 64, 16, 32, seen=seen),
+                                                 q, k, k, torch.from_numpy(f).cuda(), rotated_k=True)
+    got_q, got_k = call(freq)
+    near(got_q, *turn(_np(q), seen, freq, False), dtype)
+    near(got_k, *turn(_np(k), seen, freq, False), dtype)
+    steep = freq * np.float32(2.0 ** 22)
+    for got, x in zip(call(steep), (q, k)):
+        x, y = x[..., :32], x[..., 32:]
+        quarters = torch.stack([torch.cat(t, -1) for t in ((x, y), (-y, x), (-x, -y), (y, -x))])
+        pair = (quarters == got).view(4, *got.shape[:2], 2, 32).all(3)
+        assert bool(pair.any(0).all())
+    steep[3], steep[7] = np.inf, np.nan
+    for got in call(steep):
+        bad = torch.isnan(got)
+        assert bool(bad[..., [3, 7, 35, 39]].all()) and int(bad.sum()) == 4 * got[..., 0].numel()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_in_one_or_in_steps(torch_cuda, dtype):
     """Turned keys, appended as they are, are what the call itself appends; a
