@@ -300,14 +300,23 @@ def _out(out, rows, heads, dh, like):
     return out
 
 
+def _span(t):
+    """Address of a tensor's first element, and that past its last one."""
+    last = sum((n - 1) * s for n, s in zip(t.shape, t.stride())) if t.numel() else -1
+    return t.data_ptr(), t.data_ptr() + (last + 1) * t.element_size()
+
+
+def _clear(first, past, spans):
+    """Memory that is written and the spans of other tensors have no byte in common."""
+    for a, z in spans:
+        if a < past and first < z:
+            raise ValueError("tensors that are written must not overlap the others")
+
+
 def _beside(out, *inputs):
     """A tensor that is written and the span of each other one, from its first
     element to its last, have no memory in common."""
-    for t in inputs:
-        last = sum((n - 1) * s for n, s in zip(t.shape, t.stride())) if t.numel() else -1
-        if (t.data_ptr() < out.data_ptr() + out.nbytes
-                and out.data_ptr() < t.data_ptr() + (last + 1) * t.element_size()):
-            raise ValueError("tensors that are written must not overlap the others")
+    _clear(*_span(out), map(_span, inputs))
 
 
 def window_attention(q, k, v, cu, window=None, sinks=0, causal=True, size=None, out=None):
@@ -431,6 +440,7 @@ class TokenCache:
         self._ref = byref(self._c)
         self._attend, self._evict = (getattr(_native.lib(), name) for name in self._names)
         self._space, self._streams = {}, set()
+        self._spans = [_span(t) for t in tensors]
         self.batch, self.kv_heads, self.dh, self.dtype = batch, kv_heads, dh, dtype
         self.capacity, self.device = max_pages * page_size, k.device
         self._index = k.get_device()
@@ -667,7 +677,7 @@ class PageBounds:
     """The least and the greatest value of each dim of the keys of every page of
     a cache, by which block_attention chooses pages: lo, hi [pages, kv_heads, dh]
     of the cache's dtype.  Made for what the cache holds, or from given tensors
-    as they are.  update() brings them up to date: after the cache has changed
+    as they are, apart from each other and from the cache's.  update() brings them up to date: after the cache has changed
     and before block_attention.  A page that sequences share is bounded by what
     one of them holds of it, so each should hold all of it."""
 
@@ -683,7 +693,9 @@ class PageBounds:
                 raise ValueError("bounds are written in place and have no gradients")
             if tuple(t.shape) != shape or t.device != cache.device or t.data_ptr() % 16:
                 raise ValueError(f"{name} must be a 16-byte aligned tensor {list(shape)} on the cache's GPU")
-        _beside(lo, hi, cache.k, cache.v)
+        _beside(lo, hi)
+        for t in (lo, hi):
+            _clear(*_span(t), cache._spans)
         self.lo, self.hi, self._streams = lo, hi, set()
         if not given:
             self.update()

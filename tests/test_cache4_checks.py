@@ -152,3 +152,53 @@ def test_what_is_written_lies_apart():
     for other in (t[19:], t[:11], t, t[15:16], t.view(10, 10)[:3, 0], t[12:14].expand(3, 2)):
         with pytest.raises(ValueError):
             kernels._beside(t[10:20], other)
+
+
+def _on_the_host(monkeypatch):
+    """A cache of host tensors in one buffer, for the checks that come before any call
+    (those of the tensors' place left out)."""
+    monkeypatch.setattr(kernels, "_need", lambda *a: None)
+    monkeypatch.setattr(kernels, "_here", lambda *a: 0)
+    shapes = {"k": ((6, 16, 2, 32), torch.uint8), "v": ((6, 16, 2, 32), torch.uint8),
+              "k_scale": ((6, 16, 2, 2), torch.uint8), "v_scale": ((6, 16, 2, 2), torch.uint8),
+              "table": ((2, 3), torch.int32), "length": ((2,), torch.int32), "seen": ((2,), torch.int32),
+              "weight": ((2, 48), torch.float32), "pos": ((2, 48), torch.int32)}
+    room = torch.zeros(1 << 16, dtype=torch.uint8)
+    room = room[-room.data_ptr() % 16:]
+    ts, at = {}, 0
+    for name, (shape, dtype) in shapes.items():
+        n = torch.Size(shape).numel() * dtype.itemsize
+        ts[name] = room[at:at + n].view(dtype).view(shape)
+        at += -(-n // 16) * 16 + 4096  # (apart, so that a tensor can begin beside one)
+    c = type("Cache", (), dict(ts, dtype=torch.bfloat16, batch=2, kv_heads=2, dh=64, device=room.device))()
+    c._spans = [(t.data_ptr(), t.data_ptr() + t.nbytes) for t in ts.values()]
+    return c, ts
+
+
+def _over(t, shape, dtype, end=True):
+    """A tensor whose first 16 bytes hold the last one of another, or whose last 16
+    hold the first one."""
+    base, n = t.untyped_storage(), torch.Size(shape).numel() * dtype.itemsize
+    room = torch.tensor([], dtype=torch.uint8).set_(base)
+    at = (t.data_ptr() + t.nbytes - 1) // 16 * 16 if end else t.data_ptr() + 16 - n
+    at -= base.data_ptr()
+    return None if at < 0 or at + n > len(room) else room[at:at + n].view(dtype).view(shape)
+
+
+TENSORS = ["k", "v", "k_scale", "v_scale", "table", "length", "seen", "weight", "pos"]
+
+
+@pytest.mark.parametrize("end", [True, False])
+@pytest.mark.parametrize("name", TENSORS)
+def test_page_bounds_lie_apart_from_the_cache(monkeypatch, name, end):
+    c, ts = _on_the_host(monkeypatch)
+    free = [torch.zeros(6, 2, 64, dtype=torch.bfloat16) for _ in range(2)]
+    kernels.PageBounds(c, *free)
+    t = _over(ts[name], (6, 2, 64), torch.bfloat16, end)
+    if t is None:
+        pytest.skip("nothing lies there")
+    for lo, hi in ((t, free[0]), (free[0], t)):
+        with pytest.raises(ValueError, match="overlap"):
+            kernels.PageBounds(c, lo, hi)
+    with pytest.raises(ValueError, match="overlap"):
+        kernels.PageBounds(c, free[0], free[0])

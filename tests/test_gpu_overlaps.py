@@ -1,0 +1,51 @@
+"""Calls on token caches refuse tensors that are written and overlap others, and
+leave everything as it was (GPU)."""
+import numpy as np
+import pytest
+
+from test_gpu_cache import _cache, _kern, _normal, torch_cuda  # noqa: F401
+from test_gpu_cache4 import cache4
+
+pytestmark = pytest.mark.gpu
+
+
+def bytes_of(t):
+    """A tensor's whole storage."""
+    import torch
+    return torch.tensor([], dtype=torch.uint8, device=t.device).set_(t.untyped_storage())
+
+
+def over(t, dtype, *shape):
+    """A tensor over another's memory, from its first byte on."""
+    n = int(np.prod(shape)) * dtype.itemsize
+    b = bytes_of(t)
+    return b[:n].view(dtype).view(shape) if len(b) >= n else None
+
+
+def refuses(c, calls):
+    state = [t.clone() for t in c._tensors]
+    for call in calls:
+        with pytest.raises(ValueError, match="overlap"):
+            call()
+    assert all(bool((a == b).all()) for a, b in zip(c._tensors, state))
+
+
+def caches(torch):
+    rng = np.random.default_rng(31)
+    # (pages enough for bounds to fit into the scales)
+    for make in (_cache, cache4):
+        c = make(torch, rng, "bf16", [200, 250], 2, 64, 64, 2048)
+        yield c, rng
+
+
+def test_page_bounds(torch_cuda):
+    torch = torch_cuda
+    for c, rng in caches(torch):
+        P = c.k.shape[0]
+        free = torch.zeros((P, 2, 64), dtype=torch.bfloat16, device="cuda")
+        bad = [t for t in (over(t, c.dtype, P, 2, 64) for t in c._tensors) if t is not None]
+        assert len(bad) == (4 if c.k.dtype == torch.uint8 else 2)
+        refuses(c, [lambda t=t: _kern().PageBounds(c, t, free) for t in bad])
+        refuses(c, [lambda t=t: _kern().PageBounds(c, free, t) for t in bad])
+        refuses(c, [lambda: _kern().PageBounds(c, free, free)])
+        _kern().PageBounds(c, free, free.clone()).update()
