@@ -724,7 +724,7 @@ def block_attention(q, cache, bounds, blocks, first=0, recent=1, out=None):
     head's queries (equal ones: the lower page).  Sequences of no more pages
     are attended whole.  Weights stay as they are.  bounds: PageBounds of the
     cache, up to date.  Returns (out like q, contiguous, a given one apart from
-    the inputs; chosen int32 [batch, kv_heads, blocks], the pages by their place in
+    q, the bounds and the cache's tensors; chosen int32 [batch, kv_heads, blocks], the pages by their place in
     the sequence, ascending, then -1)."""
     if not isinstance(q, torch.Tensor) or q.dim() != 3 or q.shape[0] != cache.batch:
         raise ValueError("q must be a tensor [batch, heads, dh]")
@@ -742,7 +742,8 @@ def block_attention(q, cache, bounds, blocks, first=0, recent=1, out=None):
     fresh = out is None
     out = _out(out, cache.batch, heads, cache.dh, q)
     if not fresh:
-        _beside(out, q, cache.k, cache.v, bounds.lo, bounds.hi)
+        _beside(out, q, bounds.lo, bounds.hi)
+        _clear(*_span(out), cache._spans)
     stream = bounds._ready(q, None if fresh else out)
     key = ("fusion_block_attention", heads, blocks)
     n = cache._space.get(key)

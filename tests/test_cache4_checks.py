@@ -202,3 +202,17 @@ def test_page_bounds_lie_apart_from_the_cache(monkeypatch, name, end):
             kernels.PageBounds(c, lo, hi)
     with pytest.raises(ValueError, match="overlap"):
         kernels.PageBounds(c, free[0], free[0])
+
+
+@pytest.mark.parametrize("end", [True, False])
+@pytest.mark.parametrize("name", TENSORS)
+def test_block_attention_writes_apart_from_the_cache(monkeypatch, name, end):
+    c, ts = _on_the_host(monkeypatch)
+    bounds = kernels.PageBounds(c, *(torch.zeros(6, 2, 64, dtype=torch.bfloat16) for _ in range(2)))
+    q = torch.zeros(2, 4, 64, dtype=torch.bfloat16)
+    t = _over(ts[name], (2, 4, 64), torch.bfloat16, end)
+    if t is None:
+        pytest.skip("nothing lies there")
+    for out in (t, q, bounds.lo.view(-1)[512:1024].view(2, 4, 64), bounds.hi.view(-1)[:512].view(2, 4, 64)):
+        with pytest.raises(ValueError, match="overlap"):
+            kernels.block_attention(q, c, bounds, 2, out=out)

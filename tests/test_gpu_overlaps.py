@@ -49,3 +49,16 @@ def test_page_bounds(torch_cuda):
         refuses(c, [lambda t=t: _kern().PageBounds(c, free, t) for t in bad])
         refuses(c, [lambda: _kern().PageBounds(c, free, free)])
         _kern().PageBounds(c, free, free.clone()).update()
+
+
+def test_block_attention(torch_cuda):
+    torch = torch_cuda
+    kern = _kern()
+    for c, rng in caches(torch):
+        q, bounds = _normal(torch, rng, "bf16", 2, 4, 64), kern.PageBounds(c)
+        want, _ = kern.block_attention(q, c, bounds, 2)
+        bad = [t for t in (over(t, c.dtype, 2, 4, 64) for t in (*c._tensors, q, bounds.lo, bounds.hi))
+               if t is not None]
+        refuses(c, [lambda t=t: kern.block_attention(q, c, bounds, 2, out=t) for t in bad])
+        out = torch.empty_like(want)
+        assert kern.block_attention(q, c, bounds, 2, out=out)[0] is out and torch.equal(out, want)
