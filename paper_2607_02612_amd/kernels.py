@@ -629,7 +629,7 @@ def cache_append_rotary(cache, q, k, v, freq, cu=None, interleaved=False, drop=N
     moved them).  Returns (turned queries, turned keys): both contiguous, rows
     from cu[-1] on zero; the keys, as window_attention takes them, only with
     `rotated_k`, else None; a given out takes the queries, lies apart from the
-    inputs, and its rows from cu[-1] on are left as they were."""
+    inputs and the cache's tensors, and its rows from cu[-1] on are left as they were."""
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a tensor [rows, heads, dh]")
     rows, heads = q.shape[:2]
@@ -658,7 +658,8 @@ def cache_append_rotary(cache, q, k, v, freq, cu=None, interleaved=False, drop=N
     fresh = out is None
     out = _out(out, rows, heads, dh, q)
     if not fresh:
-        _beside(out, q, k, v)
+        _beside(out, q, k, v, freq, *(() if drop is None else (drop,)))
+        _clear(*_span(out), cache._spans)
     keys = k.new_empty((rows, cache.kv_heads, dh)) if rotated_k else None
     if used < rows:
         for t in (out if fresh else None, keys):

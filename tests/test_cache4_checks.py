@@ -216,3 +216,18 @@ def test_block_attention_writes_apart_from_the_cache(monkeypatch, name, end):
     for out in (t, q, bounds.lo.view(-1)[256:].view(2, 4, 64), bounds.hi.view(-1)[:512].view(2, 4, 64)):
         with pytest.raises(ValueError, match="overlap"):
             kernels.block_attention(q, c, bounds, 2, out=out)
+
+
+@pytest.mark.parametrize("end", [True, False])
+@pytest.mark.parametrize("name", TENSORS)
+def test_turned_queries_go_apart_from_the_cache(monkeypatch, name, end):
+    c, ts = _on_the_host(monkeypatch)
+    q, k, v = (torch.zeros(2, h, 64, dtype=torch.bfloat16) for h in (4, 2, 2))
+    room = torch.zeros(1024, dtype=torch.bfloat16)
+    freq, drop = room[:64].view(torch.float32), room[1020:].view(torch.int32)
+    t = _over(ts[name], (2, 4, 64), torch.bfloat16, end)
+    if t is None:
+        pytest.skip("nothing lies there")
+    for out in (t, q, room[:512].view(2, 4, 64), room[56:568].view(2, 4, 64), room[512:].view(2, 4, 64)):
+        with pytest.raises(ValueError, match="overlap"):
+            kernels.cache_append_rotary(c, q, k, v, freq, drop=drop, out=out)

@@ -62,3 +62,16 @@ def test_block_attention(torch_cuda):
         refuses(c, [lambda t=t: kern.block_attention(q, c, bounds, 2, out=t) for t in bad])
         out = torch.empty_like(want)
         assert kern.block_attention(q, c, bounds, 2, out=out)[0] is out and torch.equal(out, want)
+
+
+def test_turned_queries(torch_cuda):
+    torch = torch_cuda
+    call = _kern().cache_append_rotary
+    for c, rng in caches(torch):
+        q, k, v = (_normal(torch, rng, "bf16", 2, h, 64) for h in (4, 2, 2))
+        freq = torch.rand(512, device="cuda")[:32]
+        drop = torch.zeros(512, dtype=torch.int32, device="cuda")[:2]
+        bad = [t for t in (over(t, c.dtype, 2, 4, 64) for t in (*c._tensors, freq, drop, q)) if t is not None]
+        refuses(c, [lambda t=t: call(c, q, k, v, freq, drop=drop, out=t) for t in bad])
+        out = torch.empty_like(q)
+        assert call(c, q, k, v, freq, drop=drop, out=out)[0] is out
