@@ -543,7 +543,8 @@ typedef struct fusion_rotary_rows {
  * tokens drafted and not kept, for instance.  They must lie in its last slots,
  * where an append puts them and an eviction may not have left them.  Rows past
  * the capacity are dropped, but their turned queries and keys are given out.
- * Outputs lie apart from the inputs and the cache.
+ * Outputs lie apart from the inputs and the cache, and the inputs from the cache's
+ * tensors but table (drop may be len or seen).
  * Errors: FUSION_E_INVALID_ARG, FUSION_E_HIP. */
 FUSION_API int fusion_cache_append_rotary(const fusion_cache* c, const fusion_cache_scales* sc,
                                           const fusion_rotary_rows* r, const int32_t* cu, void* stream);

@@ -172,15 +172,18 @@ def _on_the_host(monkeypatch):
         at += -(-n // 16) * 16 + 4096  # (apart, so that a tensor can begin beside one)
     c = type("Cache", (), dict(ts, dtype=torch.bfloat16, batch=2, kv_heads=2, dh=64, device=room.device))()
     c._spans = [(t.data_ptr(), t.data_ptr() + t.nbytes) for t in ts.values()]
+    c._written = kernels._in_order([s for s, n in zip(c._spans, TENSORS) if n != "table"])
+    c._size = 2
+    c._c = _cache(len=c.length.data_ptr(), seen=c.seen.data_ptr())
     return c, ts
 
 
 def _over(t, shape, dtype, end=True):
     """A tensor whose first 16 bytes hold the last one of another, or whose last 16
-    hold the first one."""
+    (of fewer: all but 4) hold the first ones."""
     base, n = t.untyped_storage(), torch.Size(shape).numel() * dtype.itemsize
     room = torch.tensor([], dtype=torch.uint8).set_(base)
-    at = (t.data_ptr() + t.nbytes - 1) // 16 * 16 if end else t.data_ptr() + 16 - n
+    at = (t.data_ptr() + t.nbytes - 1) // 16 * 16 if end else t.data_ptr() + (16 if n >= 16 else 4) - n
     at -= base.data_ptr()
     return None if at < 0 or at + n > len(room) else room[at:at + n].view(dtype).view(shape)
 
@@ -231,3 +234,44 @@ def test_turned_queries_go_apart_from_the_cache(monkeypatch, name, end):
     for out in (t, q, room[:512].view(2, 4, 64), room[56:568].view(2, 4, 64), room[512:].view(2, 4, 64)):
         with pytest.raises(ValueError, match="overlap"):
             kernels.cache_append_rotary(c, q, k, v, freq, drop=drop, out=out)
+
+
+@pytest.mark.parametrize("end", [True, False])
+@pytest.mark.parametrize("name", TENSORS)
+def test_rows_lie_apart_from_what_an_append_writes(monkeypatch, name, end):
+    """(The table is read only; drop may be the lengths or the positions themselves.)"""
+    c, ts = _on_the_host(monkeypatch)
+    c._ready = lambda *a: None
+    c._ref, c._scales = byref(c._c), None
+    reached = []
+    monkeypatch.setattr(kernels._native.lib(), "fusion_cache_append_rotary",
+                        lambda *a: reached.append(a) or 0, raising=False)
+    rows = [torch.zeros(2, h, 64, dtype=torch.bfloat16) for h in (4, 2, 2)]
+    freq, drop = torch.zeros(32), torch.zeros(2, dtype=torch.int32)
+    kernels.cache_append_rotary(c, *rows, freq, drop=drop)
+    kernels.cache_append_rotary(c, *rows, freq, drop=c.length)
+    kernels.cache_append_rotary(c, *rows, freq, drop=c.seen)
+    kernels.cache_append_rotary(c, *(t[:0] for t in rows), freq, [0, 0, 0], drop=drop)
+    assert len(reached) == 4
+    for i in range(5):
+        args = [*rows, freq, drop]
+        shape = [2, (4, 2, 2)[i], 64] if i < 3 else args[i].shape
+        t = _over(ts[name], shape, args[i].dtype, end)
+        if t is None:
+            continue
+        args[i] = t
+        if i == 4 and t.data_ptr() in (c.length.data_ptr(), c.seen.data_ptr()):
+            continue
+        if name == "table":
+            kernels.cache_append_rotary(c, *args[:4], drop=args[4])
+            continue
+        with pytest.raises(ValueError, match="overlap"):
+            kernels.cache_append_rotary(c, *args[:4], drop=args[4])
+    # rows far apart, of which the second one is in the cache's values
+    far = torch.tensor([], dtype=torch.bfloat16).set_(c.v.untyped_storage())
+    at = (c.v.data_ptr() - far.data_ptr()) // 2 - 1024
+    rows[0] = far.as_strided((2, 4, 64), (2048, 64, 1), at)
+    with pytest.raises(ValueError, match="overlap"):
+        kernels.cache_append_rotary(c, *rows, freq, drop=drop)
+    rows[0] = far.as_strided((2, 4, 64), (512, 64, 1), at)
+    kernels.cache_append_rotary(c, *rows, freq, drop=drop)

@@ -75,3 +75,30 @@ def test_turned_queries(torch_cuda):
         refuses(c, [lambda t=t: call(c, q, k, v, freq, drop=drop, out=t) for t in bad])
         out = torch.empty_like(q)
         assert call(c, q, k, v, freq, drop=drop, out=out)[0] is out
+
+
+def test_rows_of_an_append(torch_cuda):
+    """Rows from the cache's own memory; all of a sequence's tokens dropped by its length."""
+    torch = torch_cuda
+    call = _kern().cache_append_rotary
+    for c, rng in caches(torch):
+        rows = [_normal(torch, rng, "bf16", 2, h, 64) for h in (4, 2, 2)]
+        freq, calls = torch.rand(32, device="cuda"), []
+        written = [t for t in c._tensors if t is not c.table]
+        for t in written:
+            for i, h in enumerate((4, 2, 2)):
+                bad = over(t, c.dtype, 2, h, 64)
+                if bad is not None:
+                    calls.append(lambda i=i, bad=bad: call(c, *rows[:i], bad, *rows[i + 1:], freq))
+            bad = over(t, torch.float32, 32)
+            if bad is not None:
+                calls.append(lambda bad=bad: call(c, *rows, bad))
+            if t is not c.length and t is not c.seen:
+                calls.append(lambda t=t: call(c, *rows, freq, drop=over(t, torch.int32, 2)))
+        assert len(calls) >= 20
+        refuses(c, calls)
+        for counts in ([0, 1, 2], [0, 20, 70]):
+            want = [call(x, *(t.repeat(35, 1, 1)[:counts[-1]] for t in rows), freq, counts, drop=d)[0]
+                    for x, d in ((c, c.length), (c, c.seen))]
+            assert torch.equal(*want)
+            assert c.length.tolist() == c.seen.tolist() == np.diff(counts).tolist()
