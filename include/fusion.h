@@ -467,7 +467,7 @@ FUSION_API int fusion_cache_append(const fusion_cache* c, const void* k, const v
  * attention probability (the token score of Eq. 8); the workspace then holds 4
  * bytes per query head and slot of the capacity, however many are in use.  A
  * sequence with nothing visible gets zeros; infinite and NaN values that are
- * visible as above.  Equal calls give equal bits; how the lengths of the other
+ * visible, and the range of sums, as above.  Equal calls give equal bits; how the lengths of the other
  * sequences cut a sequence into parts decides the order of its sums.
  * q: device [batch][heads][dh], strides: HOST int64 [2]; out: device
  * [batch][heads][dh], contiguous.  ws: device buffer of ws_bytes >=
@@ -509,7 +509,8 @@ FUSION_API int fusion_cache_evict(const fusion_cache* c, int budget, int sinks, 
  *         first three in bytes.
  * A block of 32 values comes in with the scale that brings its largest magnitude
  * to 4 .. 8 (s in 2 .. 252), each value rounded to the nearest number, ties to
- * the even code, above 6 to 6.  A block with an infinite or NaN value gets s =
+ * the even code, above 6 to 6.  (The largest of these s are kept, but their sums
+ * pass fp32's range: see fusion_cache4_attention.)  A block with an infinite or NaN value gets s =
  * 255: all 32 read as NaN.  Tokens that a caller writes have one of these s too
  * (by others a value would pass the range of bf16's normal numbers).  Wherever this
  * struct may be null, null means a cache that is not in 4 bits. */
@@ -550,7 +551,10 @@ FUSION_API int fusion_cache_append_rotary(const fusion_cache* c, const fusion_ca
                                           const fusion_rotary_rows* r, const int32_t* cu, void* stream);
 
 /* fusion_paged_attention and fusion_cache_evict over a cache in 4 bits.  Scores
- * and outputs are those of the values that the codes stand for, in fp32 sums. */
+ * and outputs are those of the values that the codes stand for, in fp32 sums with
+ * weights of up to 2^8: over n visible tokens values with s up to 244 - log2(n) (below
+ * 2^120 / n) are summed within range whatever they are; larger ones may give infinity
+ * or NaN. */
 FUSION_API size_t fusion_cache4_attention_workspace_bytes(const fusion_cache* c,
                                                           const fusion_cache_scales* sc, int heads,
                                                           int accumulate);

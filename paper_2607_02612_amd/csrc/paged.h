@@ -91,7 +91,9 @@ constexpr int APPEND_BLOCKS = 1 << 22;  // workgroups of a launch (2^32 threads 
 // Values of hidden tokens are cleared, so that 0 times infinity or NaN does
 // not arise.  Of a visible token it does: where a weight underflows, and where
 // the second of the two bf16 numbers that stand for it is 0 or negative; the
-// join mends it.
+// join mends it.  (Weights refer to a maximum that is raised only when it is passed by
+// 8 in base 2, so they reach 2^8: finite values whose sum times 2^8 passes fp32's range
+// overflow, in all types.)
 //
 // With a window over a cache whose slots are out of order a wave gathers the
 // visible ones of its part first, LIST at a time (16 sequences of up to 4,099

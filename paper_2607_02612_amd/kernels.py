@@ -507,6 +507,9 @@ class TokenCache4(TokenCache):
     dim in the lower half, dh a multiple of 32 up to 128; k_scale, v_scale uint8
     [pages, page_size, kv_heads, dh / 32], s in 2 .. 252 for a scale of
     2^(s - 127), 255: the block is NaN; strides as in a TokenCache, those of the scales in whole bytes.
+    Attention sums in fp32 with weights of up to 2^8: values of n visible tokens are
+    within its range up to s = 244 - log2(n) (magnitudes of 2^120 / n), larger ones may
+    give infinity or NaN.
     dtype: of the rows that come in, of queries and of outputs.  cache_append,
     cache_append_rotary, paged_attention, cache_evict, PageBounds and
     block_attention take it as they take a TokenCache; rows are rounded to 4

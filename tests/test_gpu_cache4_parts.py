@@ -271,3 +271,33 @@ def test_strides_at_the_limits_of_the_tiles(torch_cuda, page, row, scale_page, s
     assert all(torch.equal(a, b) for a, b in zip((f.k, f.v, f.k_scale, f.v_scale), c._tensors[:2] + c._tensors[7:]))
     del f, far, big
     torch.cuda.empty_cache()  # (the memory of one case at a time)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("page", [16, 64, 27])
+def test_values_at_the_ends_of_their_range(torch_cuda, page, dtype):
+    """Sums are fp32 and the weights in them up to 2^8: n visible values of up to
+    6 2^(s - 127) are summed within fp32's range for s up to 244 - log2 n, by windows and
+    over chosen pages too.  At the lower end a product of a weight's part (of up to three)
+    and a value, or a sum of two, that falls below 2^-126 is lost, 6 n + 4 of them at most
+    beside a sum of weights of at least 1."""
+    torch = torch_cuda
+    kern = _kern()
+    for lengths in ([1000, 64, 1, 2, 0], [40, 7, 1, 2, 16]):
+        n = max(lengths)
+        most = 244 - math.ceil(math.log2(n))
+        for scales in ((most, most), (most - 1, most), (2, 2), (2, 40)):
+            print(f"[ends] {dtype} {page} {n} {scales}", flush=True)
+            c, g = make(torch, n, dtype, lengths, 4, 64, page)
+            c.v_scale[...] = torch.randint(scales[0], scales[1] + 1, c.v_scale.shape, generator=g,
+                                           device="cuda").to(torch.uint8)
+            c.k_scale.add_(2)  # weights of many sizes
+            q = torch.randn((5, 16, 64), generator=g, device="cuda").to(c.dtype)
+            lost = 2.0 ** -126 * (6 * n + 4)
+            out, tol, _, _ = reference(torch, q, c, dtype)
+            close(torch, kern.paged_attention(q, c), out, tol + lost, scales)
+            out, tol, _, _ = reference(torch, q, c, dtype, 30, 1)
+            close(torch, kern.paged_attention(q, c, 30, 1), out, tol + lost, scales)
+            got, chosen = kern.block_attention(q, c, kern.PageBounds(c), 3)
+            out, tol, _, _ = reference(torch, q, c, dtype, chosen=chosen)
+            close(torch, got, out, tol + lost, scales)
