@@ -543,6 +543,8 @@ class TokenCache4(TokenCache):
         """An empty cache on the current GPU with pages for `capacity` tokens of
         every sequence.  In memory the heads of a page come before its tokens, so
         that what a key head reads of a page lies together."""
+        if dh < 32 or dh % 32:
+            raise ValueError("dh must be a multiple of 32")
         n = -(-capacity // page_size)
         dev = torch.device("cuda", torch.cuda.current_device())
         u8 = [torch.zeros((batch * n, kv_heads, page_size, w), dtype=torch.uint8,

@@ -275,3 +275,11 @@ def test_rows_lie_apart_from_what_an_append_writes(monkeypatch, name, end):
         kernels.cache_append_rotary(c, *rows, freq, drop=drop)
     rows[0] = far.as_strided((2, 4, 64), (512, 64, 1), at)
     kernels.cache_append_rotary(c, *rows, freq, drop=drop)
+
+
+@pytest.mark.parametrize("dh", [33, 48, 63, 65, 97, 0, -32])
+def test_empty_caches_of_odd_widths_are_refused(monkeypatch, dh):
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch, "zeros", lambda *a, **k: pytest.fail("memory was taken"))
+    with pytest.raises(ValueError, match="multiple of 32"):
+        kernels.TokenCache4.empty(1, 64, 2, dh)
