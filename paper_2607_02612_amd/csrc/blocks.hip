@@ -42,8 +42,8 @@ __device__ __forceinline__ void held8(const CacheArgs& c, int page, int place, i
 // sequence's newest slots), 16 lanes side by side and 16 tokens at a time; the
 // parts meet over the lanes and then in LDS.  Least and greatest are exact in
 // any order; NaN has no part in them.  Bound by latency: the newest page of 64
-// sequences (64 bf16 tokens, 8 heads of 128) takes 5.5 us, with one workgroup per
-// page 11.2.
+// sequences (64 bf16 tokens, 8 heads of 128) takes 5.1 us, so a page's pieces are spread
+// over workgroups.
 template <typename T, bool FOUR>
 __global__ __launch_bounds__(256) void page_bounds(CacheArgs c, BoundsArgs a, FastDiv pieces, int touched,
                                                    int chunks) {
@@ -216,11 +216,11 @@ __device__ __forceinline__ void choose_all(const CacheArgs& c, int b, int pages,
 
 // The keys, by workgroups of SCORE_PAGES pages.  A chain of loads (length, page,
 // bounds) hidden by many small workgroups: 4,096 of them, half past the ends of their
-// sequences, take 11.3 us for 17 MB of bounds (64 sequences of up to 128 pages, 32
-// heads over 8), 8.9 for two sequences of 2,048.  Sums in 32 bits take as long.  The
+// sequences, take 12.5 us for 17 MB of bounds (64 sequences of up to 128 pages, 32
+// heads over 8), 9.6 for two sequences of 2,048; 10.2 and 8.5 with sums in 32 bits.  The
 // key heads run fastest over the workgroups, since they are neighbours in memory
-// (2 us), then the sequences: with their chunks fastest the XCDs whose chunks lie
-// past most ends would have no work.
+// (slowest: 14.7), then the sequences: with their chunks fastest (13.4) the XCDs whose
+// chunks lie past most ends would have no work.
 constexpr int SCORE_PAGES = 16;
 template <typename T>
 __global__ __launch_bounds__(256) void block_scores(CacheArgs c, BlockArgs a, uint32_t* keys, FastDiv batch,
@@ -243,8 +243,8 @@ __global__ __launch_bounds__(256) void block_scores(CacheArgs c, BlockArgs a, ui
 
 // The choice among few pages, a wave per sequence and key head: the blocks-th
 // largest key is found bit by bit, with counts of ballots and no barrier (512
-// choices among up to 128 pages: 6.5 us, by block_choose 11.2; 48 among up to 417
-// with 8 keys a lane: 10.0, by block_choose 6.4).
+// choices among up to 128 pages: 5.3 us, by block_choose 10.9; 48 among up to 417
+// with 8 keys a lane: 10.3, by block_choose 6.4).
 constexpr int FEW_E = 4, FEW_PAGES = 64 * FEW_E;
 __global__ __launch_bounds__(256) void block_choose_few(CacheArgs c, BlockArgs a, const uint32_t* keys,
                                                         int* sel) {
@@ -307,9 +307,8 @@ __global__ __launch_bounds__(256) void block_choose_few(CacheArgs c, BlockArgs a
 
 // One workgroup per sequence and key head: the blocks-th largest key from the
 // top by digits of 12, 10 and 10 bits (counts in LDS), then the chosen pages in
-// order; bound by its barriers, 9.0 us for 16 choices among up to 2,048 pages (17.8
-// with 256 threads that read the scores again in every round).  The threads hold
-// CHOOSE_PAGES keys, 1024 apart; more are read again in every round.
+// order; bound by its barriers, 9.6 us for 16 choices among up to 2,048 pages.  The
+// threads hold CHOOSE_PAGES keys, 1024 apart; more are read again in every round.
 constexpr int CHOOSE_E = 4, CHOOSE_PAGES = 1024 * CHOOSE_E;
 __global__ __launch_bounds__(1024) void block_choose(CacheArgs c, BlockArgs a, const uint32_t* keys, int* sel) {
   __shared__ int bins[4096 + 2048], s_found[2], s_wave[16], s_count[16][2];

@@ -115,8 +115,8 @@ constexpr int PAGED_SPLIT = 1024;  // sequences up to which the work is split ov
 // with 4,096 4 %).
 constexpr int PAGED_WAVES = 2048, PAGED_WAVES_64 = 3 * 1024;
 // Waves of a SIMD over a cache in 4 bits, as the registers allow without spills: 16
-// windowed sequences of fp32 queries with 128-wide heads take 19.4 us with 2, 24.1 with
-// 3; the bf16 ones below (by paged_attention) 74.6 with 3, 83 with 2, 84 with 4.
+// windowed sequences of fp32 queries with 96-wide heads take 18.4 us with 2, 20.1 with
+// 3; the bf16 ones of paged4_flat's comment, by paged_attention, 77 with 3, 86 with 2.
 template <typename T, int DP> constexpr int four_waves() { return sizeof(T) == 4 && DP == 128 ? 2 : 3; }
 
 constexpr int LIST = 512;  // tokens of a part that are gathered at a time
@@ -655,7 +655,7 @@ __global__ __launch_bounds__(256, (FOUR ? four_waves<T, DP>() : 2)) void paged_a
 // on, values while the next scores are; the halves of a tile's values share the LDS.
 //
 // 64 sequences of up to 8,192 tokens, 32 bf16 heads of 128 over 8 (290 MB of cache, 33 of
-// scores): 69 us, 4.7 TB/s, by paged_attention 90.  When it took 71: 63 if the cache
+// scores): 69 us, 4.7 TB/s, by paged_attention 77.  When it took 71: 63 if the cache
 // came from the last level, 52 without scores; with every tile read from L2 54 and 47,
 // of which 14 were the product with the values.  Memory and the issue of instructions
 // bound it together: vector instructions 19 us, matrix 10, LDS 28; a quarter of the
@@ -960,7 +960,9 @@ __global__ __launch_bounds__(256, (flat_waves<T, DP, R>())) void paged4_flat(Cac
 // the output of a dimension with infinite or NaN ones is their sum, since weights
 // are positive.
 constexpr int JOIN_HEADS = 128;
-constexpr int JOIN_AHEAD = 4;  // (8 leave registers for one workgroup a CU: 17.5 us instead of 13.2)
+// (8 leave registers for one workgroup a CU: two sequences of 131,072 tokens, 32 heads, 23.3
+// us instead of 14.0)
+constexpr int JOIN_AHEAD = 4;
 // (maximum, sum) of two parts
 __device__ __forceinline__ float2 join_ml(float2 a, float2 b) {
   const float m = fmaxf(a.x, b.x), mu = m == -INFINITY ? 0.f : m;
@@ -1155,6 +1157,8 @@ size_t paged_space(const CacheArgs& c, int H, int accumulate, char* ws, PagedSpa
   p.qtiles = (group + 15) / 16;
   p.units = c.Hkv * p.qtiles;
   const bool split = c.B <= PAGED_SPLIT;
+  // (4 bits: by four_waves also where paged4_flat runs with fewer, flat_waves: of bf16
+  // queries of more than 4 heads a key head, wider than 64, two of three parts run at once)
   const int waves = FOUR ? 1024 * (DP == 64 ? four_waves<T, 64>() : four_waves<T, 128>())
                          : DP == 64 ? PAGED_WAVES_64 : PAGED_WAVES;
   p.ranges = split ? std::max(1, waves / p.units) : c.B;

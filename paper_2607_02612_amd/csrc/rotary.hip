@@ -271,10 +271,10 @@ __global__ __launch_bounds__(1024) void rotary_few(CacheArgs c, RotaryArgs a, Fa
 }
 
 // A wave per row, two tasks a lane at a time; the lengths move on in a launch of
-// their own.  Bound by its bytes: 16,384 bf16 rows of 48 heads of 128 (512 MB in and
-// out) take 112 us, 4.6 TB/s, where a copy reaches 5.1; 119 with one task at a
-// time.  A wave that goes on to further rows holds the series' constants and the
-// call's strides in registers that the tasks need (152).
+// their own.  Bound by its bytes: 19,234 bf16 rows of 48 heads of 128 (512 MB in and
+// out) take 102 us, 5.0 TB/s, where a copy reaches 5.2; 104 with one task at a
+// time.  (A wave that goes on to further rows would hold the series' constants and the
+// call's strides in registers that the tasks need.)
 template <typename T, bool FOUR>
 __global__ __launch_bounds__(256) void rotary_many(CacheArgs c, RotaryArgs a, FastDiv pieces, int tasks,
                                                    int block0, AppendSeqs sq) {

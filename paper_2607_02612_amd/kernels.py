@@ -506,7 +506,8 @@ class TokenCache4(TokenCache):
     k, v uint8 [pages, page_size, kv_heads, dh / 2], two codes a byte, the lower
     dim in the lower half, dh a multiple of 32 up to 128; k_scale, v_scale uint8
     [pages, page_size, kv_heads, dh / 32], s in 2 .. 252 for a scale of
-    2^(s - 127), 255: the block is NaN; strides as in a TokenCache, those of the scales in whole bytes.
+    2^(s - 127), 255: the block is NaN; strides as in a TokenCache, those of the
+    scales in whole bytes.
     Attention sums in fp32 with weights of up to 2^8: values of n visible tokens are
     within its range up to s = 244 - log2(n) (magnitudes of 2^120 / n), larger ones may
     give infinity or NaN.
@@ -562,7 +563,7 @@ class TokenCache4(TokenCache):
 def cache_append(cache, k, v, cu=None):
     """Append key and value rows [rows, kv_heads, dh]: one per sequence, or
     rows cu[i] .. cu[i+1]-1 to sequence i (cu: host offsets, rows from cu[-1]
-    on take no part).  Their weight starts at 0, that of a prompt's rows too;
+    on take no part; no row lies in a slot that the call writes).  Their weight starts at 0, that of a prompt's rows too;
     rows past a sequence's capacity are dropped."""
     kp, k_row, k_head = _heads(k, "k", cache.dtype, cache.kv_heads, cache.dh)
     vp, v_row, v_head = _heads(v, "v", cache.dtype, cache.kv_heads, cache.dh)
@@ -586,9 +587,9 @@ def cache_append(cache, k, v, cu=None):
 
 
 def paged_attention(q, cache, window=None, sinks=0, accumulate=True, out=None):
-    """Attention of each sequence's newest token (appended before) over its
-    cached tokens; with a window, over those among the last `window` positions
-    or the first `sinks`.  q [batch, heads, dh]; returns out like q,
+    """Attention of each sequence's newest token (appended before; of several
+    rows appended at once the last one) over its cached tokens; with a window,
+    over those among the last `window` positions or the first `sinks`.  q [batch, heads, dh]; returns out like q,
     contiguous (a given out does not overlap the inputs).  accumulate:
     cache.weight grows by the mean over the heads of the attention
     probabilities."""
@@ -651,8 +652,14 @@ def cache_append_rotary(cache, q, k, v, freq, cu=None, interleaved=False, drop=N
     moved them).  Returns (turned queries, turned keys): both contiguous, rows
     from cu[-1] on zero; the keys, as window_attention takes them, only with
     `rotated_k`, else None; a given out takes the queries, lies apart from the
-    inputs and the cache's tensors, and its rows from cu[-1] on are left as they were.
-    No input overlaps what the call writes of the cache (drop may be its length or seen)."""
+    inputs and the cache's tensors, and its rows from cu[-1] on are left as they
+    were.  No input overlaps what the call writes of the cache (drop may be its
+    length or seen).
+
+    Queries come back for all rows, but attention over the cache is that of one
+    query a sequence, its newest token's (paged_attention, block_attention), and
+    window_attention reads packed rows: drafts, or a later part of a prompt, all
+    attend what the cache holds only if they are appended one at a time."""
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a tensor [rows, heads, dh]")
     rows, heads = q.shape[:2]
