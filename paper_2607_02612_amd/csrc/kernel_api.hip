@@ -10,8 +10,10 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <mutex>
 #include <string>
+#include <utility>
 
 #include "../../include/fusion.h"
 #include "kernels.h"
@@ -365,6 +367,60 @@ int check_cache(const fusion_cache* c, CacheArgs* a, const fusion_cache_scales* 
     a->vs_page = sc->v_strides[0]; a->vs_row = sc->v_strides[1]; a->vs_head = sc->v_strides[2];
   }
   return FUSION_OK;
+}
+
+// Memory of a tensor, from its first byte to the one past its last (0 to 0: none); rows
+// of n elements at the strides of some dims.
+struct Span {
+  uintptr_t first, past;
+};
+Span span(const void* p, size_t bytes) { return p && bytes ? Span{(uintptr_t)p, (uintptr_t)p + bytes} : Span{0, 0}; }
+Span span(const void* p, std::initializer_list<std::pair<int64_t, int64_t>> dims, int64_t n, size_t size) {
+  if (!p) return {0, 0};
+  unsigned __int128 last = n;
+  for (auto [count, stride] : dims) {
+    if (count < 1) return {0, 0};
+    last += (unsigned __int128)(count - 1) * (uint64_t)stride;
+  }
+  const unsigned __int128 past = (uintptr_t)p + last * size;
+  return {(uintptr_t)p, past > UINTPTR_MAX ? UINTPTR_MAX : (uintptr_t)past};
+}
+bool overlap(Span a, Span b) { return a.first < b.past && b.first < a.past; }
+
+// What an append of turned rows reads and writes lies apart.
+int check_apart(const fusion_cache* c, const CacheArgs& ca, const fusion_cache_scales* sc,
+                const fusion_rotary_rows* r, int rows) {
+  const size_t size = c->precision == 1 ? 2 : 4, batch = c->batch, slots = batch * ca.cap;
+  auto pages = [&](const void* p, const int64_t* st, int64_t n, size_t bytes) {
+    return span(p, {{c->pages, st[0]}, {c->page_size, st[1]}, {c->kv_heads, st[2]}}, n, bytes);
+  };
+  const int64_t held = sc ? c->dh / 2 : c->dh;
+  const Span none{0, 0};
+  const Span cache[] = {
+      pages(c->k, c->k_strides, held, sc ? 1 : size), pages(c->v, c->v_strides, held, sc ? 1 : size),
+      sc ? pages(sc->k, sc->k_strides, c->dh / 32, 1) : none, sc ? pages(sc->v, sc->v_strides, c->dh / 32, 1) : none,
+      span(c->len, batch * 4), span(c->seen, batch * 4), span(c->weight, slots * 4), span(c->pos, slots * 4)};
+  auto heads = [&](const void* p, const int64_t* st, int n) {
+    return span(p, {{rows, st[0]}, {n, st[1]}}, c->dh, size);
+  };
+  // (a sequence's drop is read before its length and position are written)
+  const bool own = r->drop == c->len || r->drop == c->seen;
+  const Span in[] = {heads(r->q, r->q_strides, r->heads), heads(r->k, r->k_strides, c->kv_heads),
+                     heads(r->v, r->v_strides, c->kv_heads), span(r->freq, (size_t)r->half * 4),
+                     own ? none : span(r->drop, batch * 4)};
+  const Span out[] = {span(r->q_out, (size_t)rows * r->heads * c->dh * size),
+                      span(r->k_out, (size_t)rows * c->kv_heads * c->dh * size)};
+  const Span table = span(c->table, batch * c->max_pages * 4), drop = span(r->drop, batch * 4);
+  bool shared = overlap(out[0], out[1]);
+  for (const Span& w : out) {
+    for (const Span& x : in) shared |= overlap(w, x);
+    for (const Span& x : cache) shared |= overlap(w, x);
+    shared |= overlap(w, table) | overlap(w, drop);
+  }
+  for (const Span& w : cache)
+    for (const Span& x : in) shared |= overlap(w, x);
+  return shared ? bad("rows, freq or drop overlap what the call writes of the cache, or an output overlaps one of them")
+                : FUSION_OK;
 }
 
 // Queries, output and workspace of one new token per sequence.
@@ -724,6 +780,7 @@ FUSION_API int fusion_cache_append_rotary(const fusion_cache* c, const fusion_ca
   if (int rc = check_strides(c->precision, r->v_strides, 2)) return rc;
   if (((uintptr_t)r->q | (uintptr_t)r->k | (uintptr_t)r->v | (uintptr_t)r->q_out | (uintptr_t)r->k_out) % 16)
     return bad("buffers must be 16-byte aligned");
+  if (int rc = check_apart(c, ca, sc, r, cu ? cu[c->batch] : c->batch)) return rc;
   const RotaryArgs a{r->q, r->k, r->v, r->q_strides[0], r->q_strides[1], r->k_strides[0], r->k_strides[1],
                      r->v_strides[0], r->v_strides[1], r->q_out, r->k_out, r->freq, r->drop,
                      r->heads, r->half, r->interleaved};

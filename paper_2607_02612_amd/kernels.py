@@ -20,9 +20,7 @@ from __future__ import annotations
 
 import ctypes
 import struct
-from bisect import bisect_left
 from ctypes import byref, c_double, c_float
-from itertools import accumulate
 
 import numpy as np
 import torch
@@ -315,12 +313,6 @@ def _clear(first, past, spans):
             raise ValueError("tensors that are written must not overlap the others")
 
 
-def _in_order(spans):
-    """First bytes of spans in order, and the last byte past each or any before it."""
-    spans = sorted(spans)
-    return [a for a, _ in spans], list(accumulate((z for _, z in spans), max))
-
-
 def _beside(out, *inputs):
     """A tensor that is written and the span of each other one, from its first
     element to its last, have no memory in common."""
@@ -449,7 +441,6 @@ class TokenCache:
         self._attend, self._evict = (getattr(_native.lib(), name) for name in self._names)
         self._space, self._streams = {}, set()
         self._spans = [_span(t) for t in tensors]
-        self._size, self._written = dtype.itemsize, _in_order(self._spans[:2] + self._spans[3:])
         self.batch, self.kv_heads, self.dh, self.dtype = batch, kv_heads, dh, dtype
         self.capacity, self.device = max_pages * page_size, k.device
         self._index = k.get_device()
@@ -632,14 +623,6 @@ def cache_evict(cache, budget, sinks=0, recent=0):
     return src
 
 
-def _apart_from(written, first, past):
-    """Memory that a call reads and what it writes of the cache: (first bytes in order,
-    the last one past so far) have no byte in common."""
-    i = bisect_left(written[0], past)
-    if i and written[1][i - 1] > first:
-        raise ValueError("rows, freq and drop must not overlap what the call writes of the cache")
-
-
 def cache_append_rotary(cache, q, k, v, freq, cu=None, interleaved=False, drop=None, rotated_k=False,
                         out=None):
     """cache_append of rows whose queries q [rows, heads, dh] and keys are turned
@@ -685,18 +668,6 @@ def cache_append_rotary(cache, q, k, v, freq, cu=None, interleaved=False, drop=N
         used = int(cu_h[-1])
     if k.shape[0] != rows or v.shape[0] != rows or (rows != cache.batch if cu is None else rows < used):
         raise ValueError("rows do not match the sequences")
-    freq_p, drop_p = freq.data_ptr(), 0 if drop is None else drop.data_ptr()
-    written, size = cache._written, cache._size
-    if rows:
-        if heads:
-            _apart_from(written, qp, qp + ((rows - 1) * q_row + (heads - 1) * q_head + dh) * size)
-        most = cache.kv_heads - 1
-        _apart_from(written, kp, kp + ((rows - 1) * k_row + most * k_head + dh) * size)
-        _apart_from(written, vp, vp + ((rows - 1) * v_row + most * v_head + dh) * size)
-    _apart_from(written, freq_p, freq_p + 4 * half)
-    # (a sequence's count is read before its length and position are written)
-    if drop is not None and drop_p != cache._c.len and drop_p != cache._c.seen:
-        _apart_from(written, drop_p, drop_p + 4 * cache.batch)
     fresh = out is None
     out = _out(out, rows, heads, dh, q)
     if not fresh:
@@ -708,8 +679,8 @@ def cache_append_rotary(cache, q, k, v, freq, cu=None, interleaved=False, drop=N
             if t is not None:
                 t[max(used, 0):].zero_()
     r = _rotary_rows(qp, kp, vp, q_row, q_head, k_row, k_head, v_row, v_head, out.data_ptr(),
-                     0 if keys is None else keys.data_ptr(), freq_p, drop_p, heads, half,
-                     1 if interleaved else 0)
+                     0 if keys is None else keys.data_ptr(), freq.data_ptr(),
+                     0 if drop is None else drop.data_ptr(), heads, half, 1 if interleaved else 0)
     check(_native.lib().fusion_cache_append_rotary(
         cache._ref, cache._scales, r, cu_p,
         cache._ready(q, k, v, freq, drop, None if fresh else out)))

@@ -172,9 +172,6 @@ def _on_the_host(monkeypatch):
         at += -(-n // 16) * 16 + 4096  # (apart, so that a tensor can begin beside one)
     c = type("Cache", (), dict(ts, dtype=torch.bfloat16, batch=2, kv_heads=2, dh=64, device=room.device))()
     c._spans = [(t.data_ptr(), t.data_ptr() + t.nbytes) for t in ts.values()]
-    c._written = kernels._in_order([s for s, n in zip(c._spans, TENSORS) if n != "table"])
-    c._size = 2
-    c._c = _cache(len=c.length.data_ptr(), seen=c.seen.data_ptr())
     return c, ts
 
 
@@ -236,45 +233,66 @@ def test_turned_queries_go_apart_from_the_cache(monkeypatch, name, end):
             kernels.cache_append_rotary(c, q, k, v, freq, drop=drop, out=out)
 
 
-@pytest.mark.parametrize("end", [True, False])
-@pytest.mark.parametrize("name", TENSORS)
-def test_rows_lie_apart_from_what_an_append_writes(monkeypatch, name, end):
-    """(The table is read only; drop may be the lengths or the positions themselves.)"""
-    c, ts = _on_the_host(monkeypatch)
-    c._ready = lambda *a: None
-    c._ref, c._scales = byref(c._c), None
-    reached = []
-    monkeypatch.setattr(kernels._native.lib(), "fusion_cache_append_rotary",
-                        lambda *a: reached.append(a) or 0, raising=False)
-    rows = [torch.zeros(2, h, 64, dtype=torch.bfloat16) for h in (4, 2, 2)]
-    freq, drop = torch.zeros(32), torch.zeros(2, dtype=torch.int32)
-    kernels.cache_append_rotary(c, *rows, freq, drop=drop)
-    kernels.cache_append_rotary(c, *rows, freq, drop=c.length)
-    kernels.cache_append_rotary(c, *rows, freq, drop=c.seen)
-    kernels.cache_append_rotary(c, *(t[:0] for t in rows), freq, [0, 0, 0], drop=drop)
-    assert len(reached) == 4
-    for i in range(5):
-        args = [*rows, freq, drop]
-        shape = [2, (4, 2, 2)[i], 64] if i < 3 else args[i].shape
-        t = _over(ts[name], shape, args[i].dtype, end)
-        if t is None:
-            continue
-        args[i] = t
-        if i == 4 and t.data_ptr() in (c.length.data_ptr(), c.seen.data_ptr()):
-            continue
-        if name == "table":
-            kernels.cache_append_rotary(c, *args[:4], drop=args[4])
-            continue
-        with pytest.raises(ValueError, match="overlap"):
-            kernels.cache_append_rotary(c, *args[:4], drop=args[4])
-    # rows far apart, of which the second one is in the cache's values
-    far = torch.tensor([], dtype=torch.bfloat16).set_(c.v.untyped_storage())
-    at = (c.v.data_ptr() - far.data_ptr()) // 2 - 1024
-    rows[0] = far.as_strided((2, 4, 64), (2048, 64, 1), at)
-    with pytest.raises(ValueError, match="overlap"):
-        kernels.cache_append_rotary(c, *rows, freq, drop=drop)
-    rows[0] = far.as_strided((2, 4, 64), (512, 64, 1), at)
-    kernels.cache_append_rotary(c, *rows, freq, drop=drop)
+# Bytes of each tensor of a cache (in 4 bits) and of the rows that join it: 2, of 4 or 2 heads
+# of 64; 32 frequencies; 2 counts.
+HELD = {"k": 8 * 16 * 64, "v": 8 * 16 * 64, "ks": 8 * 16 * 4, "vs": 8 * 16 * 4, "table": 2 * 4 * 4,
+        "len": 8, "seen": 8, "weight": 2 * 64 * 4, "pos": 2 * 64 * 4}
+ROWS = {"q": 1024, "k": 512, "v": 512, "q_out": 1024, "k_out": 512, "freq": 128, "drop": 8}
+
+
+def _append(four, at):
+    """Status and message of an append whose tensors lie at the given addresses (those of
+    the rows with an r_ before their name), the others apart."""
+    if torch.cuda.is_available():
+        pytest.skip("a call that is not refused would run on these addresses")
+    where = {n: (i + 1) << 20 for i, n in enumerate([*HELD, *("r_" + n for n in ROWS)])}
+    where.update(at)
+    st = {n: (16 * 64, 64, 32) if four else (16 * 128, 128, 64) for n in ("k_strides", "v_strides")}
+    c = _cache(**{n: where[n] for n in HELD if n not in ("ks", "vs")}, **st)
+    s = _scales(k=where["ks"], v=where["vs"], k_strides=(64, 4, 2), v_strides=(64, 4, 2)) if four else None
+    r = _rows(**{n: where["r_" + n] for n in ROWS})
+    rc = _native.lib().fusion_cache_append_rotary(byref(c), s and byref(s), byref(r), None, None)
+    return rc, _native.lib().fusion_last_error().decode()
+
+
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("held", HELD)
+@pytest.mark.parametrize("row", ROWS)
+def test_appends_refuse_rows_that_overlap_the_cache(row, held, four):
+    """From the first byte, and by the last 16 of either (calls without a fault, which would
+    start a kernel, are in test_gpu_overlaps.py)."""
+    if held in ("ks", "vs") and not four or held == "table" and not row.endswith("_out"):
+        pytest.skip("not written")
+    n = HELD[held] * (4 if not four and held in "kv" else 1)
+    base = 1 << 28
+    for at in (base, base + (n - 1) // 16 * 16, base + 16 - ROWS[row]):
+        if row == "drop" and at != base:
+            at = base + (4 if at > base else -4)  # (one count beside)
+        elif row == "drop" and held in ("len", "seen"):
+            continue  # drop may be these themselves
+        rc, message = _append(four, {held: base, "r_" + row: at})
+        assert rc == -1 and "overlap" in message, (hex(at), message)
+
+
+def test_appends_refuse_outputs_that_overlap_rows():
+    for out in ("q_out", "k_out"):
+        for row in ROWS:
+            if row == out:
+                continue
+            for at in (1 << 28, (1 << 28) + (ROWS[row] - 1) // 16 * 16, (1 << 28) + 16 - ROWS[out]):
+                rc, message = _append(False, {"r_" + row: 1 << 28, "r_" + out: at})
+                assert rc == -1 and "overlap" in message, (out, row, hex(at), message)
+
+
+def test_appends_refuse_rows_whose_span_reaches_the_cache():
+    """The second of two rows far apart, or a head, lies in the cache."""
+    if torch.cuda.is_available():
+        pytest.skip("a call that is not refused would run on these addresses")
+    for strides in ((1 << 20, 64), (256, 1 << 20), (1 << 62, 64)):
+        c, r = _cache(k=1 << 28, v=1 << 32, table=64, len=128, seen=192, weight=256, pos=1024), \
+            _rows(q=(1 << 28) - (1 << 21), k=1 << 40, v=1 << 41, q_out=1 << 42, freq=1 << 43, q_strides=strides)
+        assert _native.lib().fusion_cache_append_rotary(byref(c), None, byref(r), None, None) == -1
+        assert "overlap" in _native.lib().fusion_last_error().decode()
 
 
 @pytest.mark.parametrize("dh", [33, 48, 63, 65, 97, 0, -32])

@@ -25,7 +25,7 @@ def over(t, dtype, *shape):
 def refuses(c, calls):
     state = [t.clone() for t in c._tensors]
     for call in calls:
-        with pytest.raises(ValueError, match="overlap"):
+        with pytest.raises((ValueError, _kern()._native.FusionError), match="overlap"):
             call()
     assert all(bool((a == b).all()) for a, b in zip(c._tensors, state))
 
@@ -95,6 +95,8 @@ def test_rows_of_an_append(torch_cuda):
                 calls.append(lambda bad=bad: call(c, *rows, bad))
             if t is not c.length and t is not c.seen:
                 calls.append(lambda t=t: call(c, *rows, freq, drop=over(t, torch.int32, 2)))
+            if c.k.dtype == torch.uint8 and t.nbytes >= 512:
+                calls.append(lambda t=t: _kern().cache_append(c, over(t, c.dtype, 2, 2, 64), rows[2]))
         assert len(calls) >= 20
         refuses(c, calls)
         for counts in ([0, 1, 2], [0, 20, 70]):
