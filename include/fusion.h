@@ -573,7 +573,8 @@ FUSION_API int fusion_cache4_evict(const fusion_cache* c, const fusion_cache_sca
  * dim over the tokens of each page that a sequence holds (NaN has no part in
  * them), of the pages that hold its last `newest` slots or, with newest = 0, of all.
  * Other pages' bounds stay as they are.  Of a page that sequences share each should
- * hold all of it: its bounds are by what one of them, any one, holds.
+ * hold all of it: its bounds are by what one of them, any one, holds.  lo and hi lie
+ * apart from each other and the cache.
  * Errors: FUSION_E_INVALID_ARG, FUSION_E_HIP. */
 FUSION_API int fusion_page_bounds(const fusion_cache* c, const fusion_cache_scales* sc, void* lo,
                                   void* hi, int newest, void* stream);
@@ -586,7 +587,8 @@ FUSION_API int fusion_page_bounds(const fusion_cache* c, const fusion_cache_scal
  * recent <= blocks) and those with the highest scores are attended, `blocks` in
  * all (ties to the lower page; a page whose score is NaN ranks above the others,
  * one that the table does not name below them).  Weights are left as they are.
- * q, strides, out and ws as in fusion_paged_attention.
+ * q, strides, out and ws as in fusion_paged_attention; out, chosen and ws lie apart
+ * from each other and from what is read.
  * chosen: device int32 [batch][kv_heads][blocks], the chosen pages (their place in
  * the sequence's row of the table) in ascending order, then -1.
  * Errors: FUSION_E_INVALID_ARG, FUSION_E_CAPACITY, FUSION_E_HIP. */

@@ -387,38 +387,55 @@ Span span(const void* p, std::initializer_list<std::pair<int64_t, int64_t>> dims
 }
 bool overlap(Span a, Span b) { return a.first < b.past && b.first < a.past; }
 
-// What an append of turned rows reads and writes lies apart.
-int check_apart(const fusion_cache* c, const CacheArgs& ca, const fusion_cache_scales* sc,
-                const fusion_rotary_rows* r, int rows) {
-  const size_t size = c->precision == 1 ? 2 : 4, batch = c->batch, slots = batch * ca.cap;
+// A cache's tensors: those that an append writes, then the table.
+constexpr int kCacheSpans = 9;
+struct CacheSpans {
+  Span s[kCacheSpans];
+};
+CacheSpans cache_spans(const fusion_cache* c, const CacheArgs& ca, const fusion_cache_scales* sc) {
+  const size_t size = sc ? 1 : c->precision == 1 ? 2 : 4, batch = c->batch, slots = batch * ca.cap;
   auto pages = [&](const void* p, const int64_t* st, int64_t n, size_t bytes) {
     return span(p, {{c->pages, st[0]}, {c->page_size, st[1]}, {c->kv_heads, st[2]}}, n, bytes);
   };
   const int64_t held = sc ? c->dh / 2 : c->dh;
   const Span none{0, 0};
-  const Span cache[] = {
-      pages(c->k, c->k_strides, held, sc ? 1 : size), pages(c->v, c->v_strides, held, sc ? 1 : size),
-      sc ? pages(sc->k, sc->k_strides, c->dh / 32, 1) : none, sc ? pages(sc->v, sc->v_strides, c->dh / 32, 1) : none,
-      span(c->len, batch * 4), span(c->seen, batch * 4), span(c->weight, slots * 4), span(c->pos, slots * 4)};
+  return {{pages(c->k, c->k_strides, held, size), pages(c->v, c->v_strides, held, size),
+           sc ? pages(sc->k, sc->k_strides, c->dh / 32, 1) : none,
+           sc ? pages(sc->v, sc->v_strides, c->dh / 32, 1) : none, span(c->len, batch * 4),
+           span(c->seen, batch * 4), span(c->weight, slots * 4), span(c->pos, slots * 4),
+           span(c->table, batch * c->max_pages * 4)}};
+}
+// Outputs overlap neither each other nor the cache nor what else is read.
+bool outputs_apart(std::initializer_list<Span> out, const CacheSpans& cache, std::initializer_list<Span> in) {
+  bool shared = false;
+  for (const Span& w : out) {
+    for (const Span& x : out) shared |= &x != &w && overlap(w, x);
+    for (const Span& x : in) shared |= overlap(w, x);
+    for (const Span& x : cache.s) shared |= overlap(w, x);
+  }
+  return !shared;
+}
+
+// What an append of turned rows reads and writes lies apart.
+int check_apart(const fusion_cache* c, const CacheArgs& ca, const fusion_cache_scales* sc,
+                const fusion_rotary_rows* r, int rows) {
+  const size_t size = c->precision == 1 ? 2 : 4;
+  const CacheSpans cache = cache_spans(c, ca, sc);
   auto heads = [&](const void* p, const int64_t* st, int n) {
     return span(p, {{rows, st[0]}, {n, st[1]}}, c->dh, size);
   };
+  const Span q = heads(r->q, r->q_strides, r->heads), k = heads(r->k, r->k_strides, c->kv_heads),
+             v = heads(r->v, r->v_strides, c->kv_heads), freq = span(r->freq, (size_t)r->half * 4),
+             drop = span(r->drop, (size_t)c->batch * 4);
+  bool shared = !outputs_apart({span(r->q_out, (size_t)rows * r->heads * c->dh * size),
+                                span(r->k_out, (size_t)rows * c->kv_heads * c->dh * size)},
+                               cache, {q, k, v, freq, drop});
   // (a sequence's drop is read before its length and position are written)
   const bool own = r->drop == c->len || r->drop == c->seen;
-  const Span in[] = {heads(r->q, r->q_strides, r->heads), heads(r->k, r->k_strides, c->kv_heads),
-                     heads(r->v, r->v_strides, c->kv_heads), span(r->freq, (size_t)r->half * 4),
-                     own ? none : span(r->drop, batch * 4)};
-  const Span out[] = {span(r->q_out, (size_t)rows * r->heads * c->dh * size),
-                      span(r->k_out, (size_t)rows * c->kv_heads * c->dh * size)};
-  const Span table = span(c->table, batch * c->max_pages * 4), drop = span(r->drop, batch * 4);
-  bool shared = overlap(out[0], out[1]);
-  for (const Span& w : out) {
-    for (const Span& x : in) shared |= overlap(w, x);
-    for (const Span& x : cache) shared |= overlap(w, x);
-    shared |= overlap(w, table) | overlap(w, drop);
+  for (int i = 0; i < kCacheSpans - 1; i++) {
+    const Span& w = cache.s[i];
+    shared |= overlap(w, q) | overlap(w, k) | overlap(w, v) | overlap(w, freq) | (!own && overlap(w, drop));
   }
-  for (const Span& w : cache)
-    for (const Span& x : in) shared |= overlap(w, x);
   return shared ? bad("rows, freq or drop overlap what the call writes of the cache, or an output overlaps one of them")
                 : FUSION_OK;
 }
@@ -797,6 +814,9 @@ FUSION_API int fusion_page_bounds(const fusion_cache* c, const fusion_cache_scal
   if (newest < 0) return bad("newest must not be negative");
   if (!lo || !hi) return bad("null buffer");
   if (((uintptr_t)lo | (uintptr_t)hi) % 16) return bad("buffers must be 16-byte aligned");
+  const size_t bytes = (size_t)c->pages * c->kv_heads * c->dh * (c->precision == 1 ? 2 : 4);
+  if (!outputs_apart({span(lo, bytes), span(hi, bytes)}, cache_spans(c, ca, sc), {}))
+    return bad("bounds overlap each other or the cache");
   const BoundsArgs a{lo, hi, newest};
   hipStream_t s = (hipStream_t)stream;
   hipError_t err = c->precision == 1 ? launch_page_bounds<bf16_t>(ca, a, s)
@@ -830,6 +850,13 @@ FUSION_API int fusion_block_attention(const fusion_cache* c, const fusion_cache_
   const size_t need = c->precision == 1 ? block_workspace_bytes<bf16_t>(ca, heads, blocks)
                                         : block_workspace_bytes<float>(ca, heads, blocks);
   if (int rc = check_space(ws, ws_bytes, need)) return rc;
+  const size_t size = c->precision == 1 ? 2 : 4, bytes = (size_t)c->pages * c->kv_heads * c->dh * size;
+  if (!outputs_apart({span(out, (size_t)c->batch * heads * c->dh * size),
+                      span(chosen, (size_t)c->batch * c->kv_heads * blocks * 4), span(ws, need)},
+                     cache_spans(c, ca, sc),
+                     {span(lo, bytes), span(hi, bytes),
+                      span(q, {{c->batch, strides[0]}, {heads, strides[1]}}, c->dh, size)}))
+    return bad("out, chosen or ws overlap each other or what the call reads");
   BlockArgs a{paged_args(c, ca, q, strides, heads, 0, 0, 0, out, ws), lo, hi, first, recent, chosen};
   a.p.blocks = blocks;
   hipStream_t s = (hipStream_t)stream;

@@ -295,6 +295,47 @@ def test_appends_refuse_rows_whose_span_reaches_the_cache():
         assert "overlap" in _native.lib().fusion_last_error().decode()
 
 
+@pytest.mark.parametrize("four", [False, True])
+def test_bounds_and_blocks_refuse_overlaps(four):
+    """Bounds, and the output, choice and workspace of block attention, over each other and
+    each tensor that is read."""
+    if torch.cuda.is_available():
+        pytest.skip("a call that is not refused would run on these addresses")
+    lib = _native.lib()
+    st = {n: (16 * 64, 64, 32) if four else (16 * 128, 128, 64) for n in ("k_strides", "v_strides")}
+    size = dict(HELD, lo=8 * 2 * 128, hi=8 * 2 * 128, q=1024, out=1024, chosen=2 * 2 * 4 * 4)
+    if not four:
+        size = dict(size, k=4 * size["k"], v=4 * size["v"])
+        del size["ks"], size["vs"]
+
+    def call(blocks, at):
+        where = {n: (i + 1) << 24 for i, n in enumerate([*size, "ws"])}
+        where.update(at)
+        c = byref(_cache(**{n: where[n] for n in HELD if n not in ("ks", "vs")}, **st))
+        s = byref(_scales(k=where["ks"], v=where["vs"], k_strides=(64, 4, 2), v_strides=(64, 4, 2))) if four else None
+        if not blocks:
+            rc = lib.fusion_page_bounds(c, s, where["lo"], where["hi"], 0, None)
+        else:
+            size["ws"] = lib.fusion_block_attention_workspace_bytes(c, s, 4, 4)
+            rc = lib.fusion_block_attention(c, s, where["lo"], where["hi"], where["q"], _i64(256, 64), 4, 4, 1, 1,
+                                            where["out"], where["chosen"], where["ws"], BIG, None)
+        return rc, lib.fusion_last_error().decode()
+
+    for blocks, written in ((False, ("lo", "hi")), (True, ("out", "chosen", "ws"))):
+        call(blocks, {"lo": None})  # (a refusal: the workspace's size)
+        read = [n for n in size if blocks or n not in ("q", "out", "chosen", "ws")]
+        for w in written:
+            for x in read:
+                if x == w:
+                    continue
+                base, align = 1 << 40, 256 if "ws" in (w, x) else 16
+                for at in (base, base + (size[x] - 1) // align * align, base + align - -(-size[w] // align) * align):
+                    if at + size[w] <= base:
+                        continue
+                    rc, message = call(blocks, {x: base, w: at})
+                    assert rc == -1 and "overlap" in message, (w, x, at - base, message)
+
+
 @pytest.mark.parametrize("dh", [33, 48, 63, 65, 97, 0, -32])
 def test_empty_caches_of_odd_widths_are_refused(monkeypatch, dh):
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
