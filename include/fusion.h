@@ -510,10 +510,10 @@ FUSION_API int fusion_cache_evict(const fusion_cache* c, int budget, int sinks, 
  * A block of 32 values comes in with the scale that brings its largest magnitude
  * to 4 .. 8 (s in 2 .. 252), each value rounded to the nearest number, ties to
  * the even code, above 6 to 6.  (The largest of these s are kept, but their sums
- * pass fp32's range: see fusion_cache4_attention.)  A block with an infinite or NaN value gets s =
- * 255: all 32 read as NaN.  Tokens that a caller writes have one of these s too
- * (by others a value would pass the range of bf16's normal numbers).  Wherever this
- * struct may be null, null means a cache that is not in 4 bits. */
+ * pass fp32's range: see fusion_cache4_attention.)  A block with an infinite or NaN
+ * value gets s = 255: all 32 read as NaN.  Tokens that a caller writes have one of
+ * these s too (by others a value would pass the range of bf16's normal numbers).
+ * Wherever this struct may be null, null means a cache that is not in 4 bits. */
 typedef struct fusion_cache_scales {
   uint8_t* k;
   uint8_t* v;

@@ -554,8 +554,9 @@ class TokenCache4(TokenCache):
 def cache_append(cache, k, v, cu=None):
     """Append key and value rows [rows, kv_heads, dh]: one per sequence, or
     rows cu[i] .. cu[i+1]-1 to sequence i (cu: host offsets, rows from cu[-1]
-    on take no part; no row lies in a slot that the call writes).  Their weight starts at 0, that of a prompt's rows too;
-    rows past a sequence's capacity are dropped."""
+    on take no part; no row lies in a slot that the call writes).  Their weight
+    starts at 0, that of a prompt's rows too; rows past a sequence's capacity are
+    dropped."""
     kp, k_row, k_head = _heads(k, "k", cache.dtype, cache.kv_heads, cache.dh)
     vp, v_row, v_head = _heads(v, "v", cache.dtype, cache.kv_heads, cache.dh)
     _here(k, v)
@@ -580,10 +581,10 @@ def cache_append(cache, k, v, cu=None):
 def paged_attention(q, cache, window=None, sinks=0, accumulate=True, out=None):
     """Attention of each sequence's newest token (appended before; of several
     rows appended at once the last one) over its cached tokens; with a window,
-    over those among the last `window` positions or the first `sinks`.  q [batch, heads, dh]; returns out like q,
-    contiguous (a given out does not overlap the inputs).  accumulate:
-    cache.weight grows by the mean over the heads of the attention
-    probabilities."""
+    over those among the last `window` positions or the first `sinks`.
+    q [batch, heads, dh]; returns out like q, contiguous (a given out does not
+    overlap the inputs).  accumulate: cache.weight grows by the mean over the
+    heads of the attention probabilities."""
     if not isinstance(q, torch.Tensor) or q.dim() != 3 or q.shape[0] != cache.batch:
         raise ValueError("q must be a tensor [batch, heads, dh]")
     heads = q.shape[1]
@@ -691,9 +692,10 @@ class PageBounds:
     """The least and the greatest value of each dim of the keys of every page of
     a cache, by which block_attention chooses pages: lo, hi [pages, kv_heads, dh]
     of the cache's dtype.  Made for what the cache holds, or from given tensors
-    as they are, apart from each other and from the cache's.  update() brings them up to date: after the cache has changed
-    and before block_attention.  A page that sequences share is bounded by what
-    one of them holds of it, so each should hold all of it."""
+    as they are, apart from each other and from the cache's.  update() brings
+    them up to date: after the cache has changed and before block_attention.  A
+    page that sequences share is bounded by what one of them holds of it, so each
+    should hold all of it."""
 
     def __init__(self, cache, lo=None, hi=None):
         shape = (cache.k.shape[0], cache.kv_heads, cache.dh)
@@ -738,8 +740,8 @@ def block_attention(q, cache, bounds, blocks, first=0, recent=1, out=None):
     head's queries (equal ones: the lower page).  Sequences of no more pages
     are attended whole.  Weights stay as they are.  bounds: PageBounds of the
     cache, up to date.  Returns (out like q, contiguous, a given one apart from
-    q, the bounds and the cache's tensors; chosen int32 [batch, kv_heads, blocks], the pages by their place in
-    the sequence, ascending, then -1)."""
+    q, the bounds and the cache's tensors; chosen int32 [batch, kv_heads, blocks],
+    the pages by their place in the sequence, ascending, then -1)."""
     if not isinstance(q, torch.Tensor) or q.dim() != 3 or q.shape[0] != cache.batch:
         raise ValueError("q must be a tensor [batch, heads, dh]")
     heads = q.shape[1]
